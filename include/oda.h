@@ -439,6 +439,112 @@ oda_status oda_rms_norm_rows(int32_t batch, int32_t row_len, const float *x, con
 oda_status oda_argmax(int32_t batch, int32_t n, const float *x, int32_t *index, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Many tenants, drafted tokens.  A step in which each request brings T current
+ * tokens (its last sampled token and up to T - 1 drafts of what follows), rows
+ * of one tenant use that tenant's low-rank adapters, and the tokens that the
+ * target's probabilities refuse are drawn anew.  Rows (b, t) of every buffer
+ * are row b * T + t of the calls above (batch * T rows).
+ * ------------------------------------------------------------------------- */
+
+#define ODA_LORA_MAX_PARTS 4
+
+/* Low-rank adapters of a dense layer (host struct holding device pointers).  A
+ * fused projection has parts (query, key and value; gate and up), each with
+ * rank rows of A of its own: output row r of part p of a request with adapter
+ * a gets  scale[a] * sum_i B[a][r][i] (A[a] x')[p * rank + i].
+ * Adapters of lower rank are padded with zero rows of A or columns of B. */
+typedef struct {
+  int32_t num_adapters;      /* >= 1                                                */
+  int32_t rank;              /* a multiple of 8, at most 128                         */
+  int32_t num_parts;         /* 1..ODA_LORA_MAX_PARTS                                */
+  int32_t part_rows[ODA_LORA_MAX_PARTS]; /* rows of each part (>= 1); their sum is the
+                                weight's rows: N, or 2N for SWIGLU                   */
+  const uint16_t *a;         /* device bf16 [num_adapters][num_parts * rank][K]      */
+  const uint16_t *b;         /* device bf16 [num_adapters][rows][rank]               */
+  const float *scale;        /* device fp32 [num_adapters] (alpha / rank)            */
+} oda_lora_desc;
+
+/* Bytes of workspace oda_dense_lora_bf16 needs for `batch` requests (host out).
+ * Its contents between calls do not matter. */
+oda_status oda_lora_workspace_size(const oda_lora_desc *lora, int32_t batch, size_t *bytes);
+
+/* oda_dense_bf16 with a low-rank adapter beside the weight, per request:
+ *   PLAIN:  y[b] = (W + s_a B_a A_a) x'[b]  (+ residual[b])
+ *   SWIGLU: the same sum before SiLU and the product
+ * where a = adapter_ids[b] and x' is the (normalised) input.
+ *   adapter_ids: int32 [batch]; -1: no adapter (the shared layer alone); an id
+ *                outside [-1, num_adapters) gives a row of NaN
+ *   workspace:   >= oda_lora_workspace_size bytes, 256-byte aligned; calls that
+ *                may overlap in time need separate workspaces
+ * Everything else (modes, residual, list, alignment) as in oda_dense_bf16; a and
+ * b 16-byte aligned.  Sums are fp32. */
+oda_status oda_dense_lora_bf16(const oda_dense_desc *desc, const oda_lora_desc *lora, int32_t batch,
+                               const float *x, const float *residual, float *y, const int32_t *adapter_ids,
+                               const int32_t *work_list, const int32_t *n_work, void *workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+
+/* Drafts to verify (host struct holding device pointers).  Row i of a request's
+ * logits is the target's distribution of the token at draft i's place (the last
+ * one in use: of the token after the drafts). */
+typedef struct {
+  int32_t vocab;               /* V >= 1                                            */
+  int32_t max_drafts;          /* K, 0..63 (0: draws one token from one row)        */
+  const float *logits;         /* fp32 [batch][K + 1][V]; NaN counts as -infinity    */
+  const float *draft_probs;    /* fp32 [batch][K][V]: the probabilities each draft was
+                                  drawn from (negative or NaN counts as 0); NULL:
+                                  drafts that were not drawn (probability 1 each)   */
+  const int32_t *draft_tokens; /* int32 [batch][K]; NULL iff K == 0                  */
+  const int32_t *n_drafts;     /* int32 [batch], clamped to [0, K]; NULL: K each     */
+  const float *temperature;    /* fp32 [batch]; NULL: 1.  Above 0: softmax of logits /
+                                  temperature; else (0, negative, NaN) greedy       */
+  const float *uniform;        /* fp32 [batch][K + 1] in [0, 1): u_0..u_{K-1} for the
+                                  drafts, u_K for the next token                    */
+} oda_verify_desc;
+
+/* Bytes of workspace oda_verify_drafts needs (host out).  Zero-fill it before
+ * its first use (ticket words; every call leaves them zero); it serves any later
+ * call on the stream with the same batch and at most the same V and K. */
+oda_status oda_verify_workspace_size(int32_t batch, int32_t vocab, int32_t max_drafts, size_t *bytes);
+
+/* Verification of drafted tokens by rejection sampling, which keeps the target's
+ * distribution.  With p_i = softmax(logits_i / temperature) (greedy: all on the
+ * first largest logit) and q_i the draft's probabilities, draft x_i is accepted
+ * iff u_i q_i(x_i) < p_i(x_i), up to the first refusal, at j.  The next token is
+ * then the smallest v whose cumulative weight exceeds u_K times the sum of all,
+ * with the weights max(p_j - q_j, 0) after a refusal (p_j where these are all
+ * zero), p_n when all n drafts were accepted.
+ *   n_accepted: int32 [batch] out
+ *   tokens:     int32 [batch][K + 1] out: the accepted drafts, the next token,
+ *               then -1
+ * A draft outside [0, V) is refused.  A row with no logit above -infinity
+ * refuses its draft and gives the next token -1; logits of +infinity share the
+ * row's probability evenly.  Weights and sums are fp64.  Rows past n_drafts are
+ * not read.  work_list / n_work as in oda_dense_bf16. */
+oda_status oda_verify_drafts(const oda_verify_desc *desc, int32_t batch, int32_t *n_accepted, int32_t *tokens,
+                             const int32_t *work_list, const int32_t *n_work, void *workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
+/* oda_commit_kv of several tokens per request: the first n_accepted[b] + 1
+ * (clamped to [0, tokens]) current tokens' candidates of every layer go to
+ * positions n_b - 1, n_b, ... of the paged cache, and to the rings if given;
+ * then, if advance != 0, seq_lens[b] grows by that number.
+ *   tokens:       T, 1..64
+ *   k_cand, v_cand: bf16 [L][B][T][Hkv][D]
+ *   n_accepted:   int32 [B], as oda_verify_drafts writes it (-1: nothing is
+ *                 committed for the request), or NULL: all T tokens
+ *   row_lens:     NULL, or int32 [B][T] out (advance != 0): the new seq_lens[b]
+ *                 + t, the lengths of the next step's rows (oda_qk_norm_rope)
+ *   k_ring, v_ring, n_sink, window: as in oda_commit_kv_ring, or NULL, 0, 0
+ * Workspace, shape fields and the rest as in oda_commit_kv.  A table entry
+ * outside [0, num_blocks), or a position outside the table, drops that token's
+ * candidates (the length still grows). */
+oda_status oda_commit_drafts(const oda_attn_shape *shape, int32_t tokens, uint16_t *k_cache, uint16_t *v_cache,
+                             const int32_t *block_table, int32_t *seq_lens, const uint16_t *k_cand,
+                             const uint16_t *v_cand, const int32_t *n_accepted, int32_t advance, int32_t *row_lens,
+                             void *workspace, size_t workspace_bytes, uint16_t *k_ring, uint16_t *v_ring,
+                             int32_t n_sink, int32_t window, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aid (not a step of the method): the streaming-read ceiling that
  * the attention kernels' bandwidth is quoted against.
  * ------------------------------------------------------------------------- */

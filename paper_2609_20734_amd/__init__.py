@@ -22,7 +22,9 @@ _EXPORTS = ("HEAD_MLP", "HEAD_PAPER", "OdaError", "Shape", "attn_workspace_size"
             "argmax", "prepare_dense", "prepare_qk_norm_rope", "prepare_embed", "prepare_copy_rows",
             "prepare_argmax", "stream_read", "prepare_stream_read", "rms_norm_rows", "prepare_rms_norm_rows",
             "recall_gate_static", "qkv_prep", "prepare_local_qkv", "prepare_full_qkv",
-            "ring_elements", "ring_fill", "local_decode_attn_ring", "commit_kv_ring", "prepare_local_ring")
+            "ring_elements", "ring_fill", "local_decode_attn_ring", "commit_kv_ring", "prepare_local_ring",
+            "lora_desc", "lora_workspace_size", "dense_lora_bf16", "prepare_dense_lora", "verify_desc",
+            "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts")
 
 
 def __getattr__(name):

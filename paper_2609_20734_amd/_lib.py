@@ -45,7 +45,8 @@ EXPORTED = ("oda_attn_workspace_size", "oda_local_decode_attn", "oda_full_decode
             "oda_commit_workspace_size", "oda_commit_kv",
             "oda_ring_elements", "oda_ring_fill", "oda_local_decode_attn_ring", "oda_commit_kv_ring",
             "oda_dense_bf16", "oda_qk_norm_rope", "oda_embed_bf16", "oda_copy_rows", "oda_rms_norm_rows",
-            "oda_argmax", "oda_stream_read", "oda_status_string", "oda_last_error")
+            "oda_argmax", "oda_lora_workspace_size", "oda_dense_lora_bf16", "oda_verify_workspace_size",
+            "oda_verify_drafts", "oda_commit_drafts", "oda_stream_read", "oda_status_string", "oda_last_error")
 
 
 class OdaError(RuntimeError):
@@ -84,6 +85,18 @@ class GateDesc(ctypes.Structure):
 class DenseDesc(ctypes.Structure):
     _fields_ = [("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("rms_eps", ctypes.c_float), ("weight", ctypes.c_void_p), ("norm_gain", ctypes.c_void_p)]
+
+
+class LoraDesc(ctypes.Structure):
+    _fields_ = [("num_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("num_parts", ctypes.c_int32),
+                ("part_rows", ctypes.c_int32 * 4), ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
+
+
+class VerifyDesc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("max_drafts", ctypes.c_int32), ("logits", ctypes.c_void_p),
+                ("draft_probs", ctypes.c_void_p), ("draft_tokens", ctypes.c_void_p), ("n_drafts", ctypes.c_void_p),
+                ("temperature", ctypes.c_void_p), ("uniform", ctypes.c_void_p)]
 
 
 _P = ctypes.POINTER
@@ -147,6 +160,18 @@ _lib.oda_rms_norm_rows.argtypes = [ctypes.c_int32, ctypes.c_int32, _V, _V, ctype
 _lib.oda_rms_norm_rows.restype = ctypes.c_int
 _lib.oda_argmax.argtypes = [ctypes.c_int32, ctypes.c_int32, _V, _V, _V]
 _lib.oda_argmax.restype = ctypes.c_int
+_lib.oda_lora_workspace_size.argtypes = [_P(LoraDesc), ctypes.c_int32, _P(ctypes.c_size_t)]
+_lib.oda_lora_workspace_size.restype = ctypes.c_int
+_lib.oda_dense_lora_bf16.argtypes = [_P(DenseDesc), _P(LoraDesc), ctypes.c_int32, _V, _V, _V, _V, _V, _V, _V,
+                                     ctypes.c_size_t, _V]
+_lib.oda_dense_lora_bf16.restype = ctypes.c_int
+_lib.oda_verify_workspace_size.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P(ctypes.c_size_t)]
+_lib.oda_verify_workspace_size.restype = ctypes.c_int
+_lib.oda_verify_drafts.argtypes = [_P(VerifyDesc), ctypes.c_int32, _V, _V, _V, _V, _V, ctypes.c_size_t, _V]
+_lib.oda_verify_drafts.restype = ctypes.c_int
+_lib.oda_commit_drafts.argtypes = [_P(AttnShape), ctypes.c_int32, _V, _V, _V, _V, _V, _V, _V, ctypes.c_int32, _V, _V,
+                                   ctypes.c_size_t, _V, _V, ctypes.c_int32, ctypes.c_int32, _V]
+_lib.oda_commit_drafts.restype = ctypes.c_int
 _lib.oda_stream_read.argtypes = [_V, ctypes.c_size_t, _V, ctypes.c_int32, _V]
 _lib.oda_stream_read.restype = ctypes.c_int
 _lib.oda_status_string.argtypes = [ctypes.c_int]
@@ -365,6 +390,54 @@ def argmax(batch: int, n: int, x, index, stream=None) -> None:
     _check(_lib.oda_argmax(batch, n, _ptr(x), _ptr(index), _stream(stream)))
 
 
+def lora_desc(num_adapters: int, rank: int, part_rows, a, b, scale) -> LoraDesc:
+    """The C adapter description; it keeps the factors and scales alive."""
+    if not 1 <= len(part_rows) <= 4:
+        raise ValueError(f"an adapter has 1 to 4 parts (got {len(part_rows)})")
+    s = LoraDesc(num_adapters, rank, len(part_rows), (ctypes.c_int32 * 4)(*part_rows), _ptr(a), _ptr(b), _ptr(scale))
+    s._keep = (a, b, scale)
+    return s
+
+
+def lora_workspace_size(lora: LoraDesc, batch: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_lora_workspace_size(ctypes.byref(lora), batch, ctypes.byref(out)))
+    return out.value
+
+
+def dense_lora_bf16(desc: DenseDesc, lora: LoraDesc, batch: int, x, residual, y, adapter_ids, workspace, work_list=None,
+                    n_work=None, workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_dense_lora(desc, lora, batch, x, residual, y, adapter_ids, workspace, work_list, n_work, workspace_bytes,
+                       stream)()
+
+
+def verify_desc(vocab: int, max_drafts: int, logits, draft_tokens, uniform, draft_probs=None, n_drafts=None,
+                temperature=None) -> VerifyDesc:
+    """The C description of drafts to verify; it keeps the tensors alive."""
+    s = VerifyDesc(vocab, max_drafts, _ptr(logits), _ptr(draft_probs), _ptr(draft_tokens), _ptr(n_drafts),
+                   _ptr(temperature), _ptr(uniform))
+    s._keep = (logits, draft_probs, draft_tokens, n_drafts, temperature, uniform)
+    return s
+
+
+def verify_workspace_size(batch: int, vocab: int, max_drafts: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_verify_workspace_size(batch, vocab, max_drafts, ctypes.byref(out)))
+    return out.value
+
+
+def verify_drafts(desc: VerifyDesc, batch: int, n_accepted, tokens, workspace, work_list=None, n_work=None,
+                  workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_verify_drafts(desc, batch, n_accepted, tokens, workspace, work_list, n_work, workspace_bytes, stream)()
+
+
+def commit_drafts(shape: Shape, tokens: int, k_cache, v_cache, block_table, seq_lens, k_cand, v_cand, n_accepted=None,
+                  advance: bool = True, row_lens=None, workspace=None, k_ring=None, v_ring=None, n_sink: int = 0,
+                  window: int = 0, workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_commit_drafts(shape, tokens, k_cache, v_cache, block_table, seq_lens, k_cand, v_cand, n_accepted, advance,
+                          row_lens, workspace, k_ring, v_ring, n_sink, window, workspace_bytes, stream)()
+
+
 def stream_read(src, nbytes: int, sink, groups: int = 0, stream=None) -> None:
     """Measurement aid: read nbytes of src once (the streaming-read ceiling)."""
     _check(_lib.oda_stream_read(_ptr(src), int(nbytes), _ptr(sink), groups, _stream(stream)))
@@ -497,6 +570,32 @@ def prepare_rms_norm_rows(batch: int, row_len: int, x, gain, rms_eps: float, y, 
 def prepare_argmax(batch: int, n: int, x, index, stream=None) -> Call:
     args = (batch, n, _ptr(x), _ptr(index), _stream(stream))
     return Call(_lib.oda_argmax, args, (x, index))
+
+
+def prepare_dense_lora(desc: DenseDesc, lora: LoraDesc, batch: int, x, residual, y, adapter_ids, workspace,
+                       work_list=None, n_work=None, workspace_bytes: int | None = None, stream=None) -> Call:
+    args = (ctypes.byref(desc), ctypes.byref(lora), batch, _ptr(x), _ptr(residual), _ptr(y), _ptr(adapter_ids),
+            _ptr(work_list), _ptr(n_work), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+    return Call(_lib.oda_dense_lora_bf16, args, (desc, lora, x, residual, y, adapter_ids, work_list, n_work, workspace))
+
+
+def prepare_verify_drafts(desc: VerifyDesc, batch: int, n_accepted, tokens, workspace, work_list=None, n_work=None,
+                          workspace_bytes: int | None = None, stream=None) -> Call:
+    args = (ctypes.byref(desc), batch, _ptr(n_accepted), _ptr(tokens), _ptr(work_list), _ptr(n_work), _ptr(workspace),
+            _nbytes(workspace, workspace_bytes), _stream(stream))
+    return Call(_lib.oda_verify_drafts, args, (desc, n_accepted, tokens, work_list, n_work, workspace))
+
+
+def prepare_commit_drafts(shape: Shape, tokens: int, k_cache, v_cache, block_table, seq_lens, k_cand, v_cand,
+                          n_accepted=None, advance: bool = True, row_lens=None, workspace=None, k_ring=None,
+                          v_ring=None, n_sink: int = 0, window: int = 0, workspace_bytes: int | None = None,
+                          stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), tokens, _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens), _ptr(k_cand),
+            _ptr(v_cand), _ptr(n_accepted), 1 if advance else 0, _ptr(row_lens), _ptr(workspace),
+            _nbytes(workspace, workspace_bytes), _ptr(k_ring), _ptr(v_ring), n_sink, window, _stream(stream))
+    return Call(_lib.oda_commit_drafts, args, (cs, k_cache, v_cache, block_table, seq_lens, k_cand, v_cand, n_accepted,
+                                               row_lens, workspace, k_ring, v_ring))
 
 
 def prepare_stream_read(src, nbytes: int, sink, groups: int = 0, stream=None) -> Call:

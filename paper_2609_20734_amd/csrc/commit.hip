@@ -17,6 +17,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kBlock = 16;
 constexpr int kThreads = 256;
 constexpr int kTargetGroups = 256;   // workgroups the launch aims for (one per CU)
+constexpr int kMaxTokens = 64;       // candidates per request of one commit
 
 struct CommitArgs {
   uint16_t* k_cache;
@@ -107,6 +108,101 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   }
 }
 
+// The commit of several tokens per request (oda_commit_drafts): the first
+// `count` candidates [L][B][T][Hkv][D] of request b go to positions n - 1 ..
+// n - 2 + count.  Work split and ticket as in commit_kernel.  K: one 16-byte
+// store per (unit, 8 dims, token), the tokens of a block next to each other;
+// V: a thread walks the tokens of one dim, whose slots are neighbours in the
+// block's [D][16] row.
+struct CommitDraftsArgs {
+  uint16_t* k_cache;
+  uint16_t* v_cache;
+  const int32_t* block_table;
+  int32_t* seq_lens;
+  const uint16_t* k_cand;
+  const uint16_t* v_cand;
+  const int32_t* n_accepted;   // NULL: all T tokens
+  int32_t* row_lens;           // [B][T] or NULL
+  uint32_t* tickets;           // NULL: no advance
+  int64_t kv_layer_stride;
+  int64_t NB;
+  int32_t L, B, T, Hkv, D, MB;
+  int32_t chunks, units_per_chunk;
+  uint16_t* k_ring;
+  uint16_t* v_ring;
+  int32_t ring_sb, ring_rb;
+};
+
+// Where token t of the request goes: its block in the cache (-1: nowhere) and
+// in the ring (-1: not kept: a later token of this commit takes the place).
+struct Slot {
+  int64_t blk;
+  int32_t ring, at;
+};
+__device__ __forceinline__ Slot slot_of(const CommitDraftsArgs& a, int b, int64_t pos, int64_t last) {
+  Slot s;
+  const int64_t j = pos / kBlock;
+  const bool in_table = pos >= 0 && j < a.MB;
+  s.blk = in_table ? a.block_table[(int64_t)b * a.MB + j] : -1;
+  if (s.blk >= a.NB) s.blk = -1;
+  s.at = (int)(pos & (kBlock - 1));
+  s.ring = -1;
+  if (a.k_ring != nullptr && s.blk >= 0) {
+    if (j < a.ring_sb) s.ring = (int)j;
+    else if (j + a.ring_rb > last / kBlock) s.ring = a.ring_sb + (int)(j % a.ring_rb);
+  }
+  return s;
+}
+
+__global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArgs a) {
+  const int b = blockIdx.x / a.chunks;
+  const int c = blockIdx.x - b * a.chunks;
+  const int n = a.seq_lens[b];
+  const int count = a.n_accepted != nullptr ? min(max(a.n_accepted[b], -1), a.T - 1) + 1 : a.T;
+  const int64_t pos0 = (int64_t)n - 1, last = pos0 + count - 1;
+  const int units = a.L * a.Hkv;
+  const int u0 = c * a.units_per_chunk;
+  const int nu = max(0, min(units - u0, a.units_per_chunk));
+  const int groups = a.D / 8;
+  const int nr = a.ring_sb + a.ring_rb;
+  for (int i = threadIdx.x; i < nu * groups * count; i += kThreads) {
+    const int e = i / count, t = i - e * count;
+    const int u = u0 + e / groups, d8 = e % groups;
+    const int l = u / a.Hkv, g = u - l * a.Hkv;
+    const Slot s = slot_of(a, b, pos0 + t, last);
+    if (s.blk < 0) continue;
+    const u32x4 k8 = *reinterpret_cast<const u32x4*>(a.k_cand + ((((int64_t)l * a.B + b) * a.T + t) * a.Hkv + g) * a.D + d8 * 8);
+    const int64_t in = ((int64_t)d8 * kBlock + s.at) * 8;
+    *reinterpret_cast<u32x4*>(a.k_cache + (int64_t)l * a.kv_layer_stride + (s.blk * a.Hkv + g) * kBlock * a.D + in) = k8;
+    if (s.ring >= 0)
+      *reinterpret_cast<u32x4*>(a.k_ring + ((((int64_t)l * a.B + b) * nr + s.ring) * a.Hkv + g) * kBlock * a.D + in) = k8;
+  }
+  for (int i = threadIdx.x; i < nu * a.D; i += kThreads) {
+    const int u = u0 + i / a.D, d = i % a.D;
+    const int l = u / a.Hkv, g = u - l * a.Hkv;
+    for (int t = 0; t < count; ++t) {
+      const Slot s = slot_of(a, b, pos0 + t, last);
+      if (s.blk < 0) continue;
+      const uint16_t v1 = a.v_cand[((((int64_t)l * a.B + b) * a.T + t) * a.Hkv + g) * a.D + d];
+      const int64_t in = (int64_t)d * kBlock + s.at;
+      a.v_cache[(int64_t)l * a.kv_layer_stride + (s.blk * a.Hkv + g) * kBlock * a.D + in] = v1;
+      if (s.ring >= 0) a.v_ring[((((int64_t)l * a.B + b) * nr + s.ring) * a.Hkv + g) * kBlock * a.D + in] = v1;
+    }
+  }
+  if (a.tickets == nullptr) return;
+  __shared__ int last_chunk;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t t =
+        __builtin_amdgcn_atomic_inc32(a.tickets + b, (uint32_t)(a.chunks - 1), __ATOMIC_RELAXED, "agent");
+    last_chunk = t == (uint32_t)(a.chunks - 1) ? 1 : 0;
+    if (last_chunk) __hip_atomic_store(a.seq_lens + b, n + count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (last_chunk && a.row_lens != nullptr)
+    for (int t = threadIdx.x; t < a.T; t += kThreads) a.row_lens[(int64_t)b * a.T + t] = n + count + t;
+}
+
 oda_status check_commit_shape(const oda_attn_shape* shape) {
   if (shape == nullptr) return oda::fail(ODA_ERR_NULL, "shape is NULL");
   if (shape->num_layers < 1 || shape->batch < 1 || shape->num_kv_heads < 1 || shape->num_blocks < 1 ||
@@ -123,6 +219,20 @@ oda_status check_commit_shape(const oda_attn_shape* shape) {
 }
 
 size_t commit_ws_bytes(const oda_attn_shape* shape) { return (size_t)oda::round_up((int64_t)shape->batch * 4, 256); }
+
+oda_status check_commit_workspace(const oda_attn_shape* shape, const void* workspace, size_t workspace_bytes) {
+  const size_t need = commit_ws_bytes(shape);
+  if (workspace == nullptr) return oda::fail(ODA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (workspace_bytes < need)
+    return oda::fail(ODA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  if (!oda::aligned(workspace, 256)) return oda::fail(ODA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return ODA_OK;
+}
+
+int64_t layer_stride(const oda_attn_shape* shape) {
+  return shape->layer_stride_kv != 0 ? shape->layer_stride_kv
+                                     : shape->num_blocks * shape->num_kv_heads * kBlock * shape->head_dim;
+}
 
 }  // namespace
 
@@ -151,11 +261,8 @@ oda_status run_commit(const oda_attn_shape* shape, uint16_t* k_cache, uint16_t* 
       !oda::aligned(v_local, 16) || (k_full && (!oda::aligned(k_full, 16) || !oda::aligned(v_full, 16))))
     return oda::fail(ODA_ERR_SHAPE, "caches and candidates must be 16-byte aligned");
   if (advance != 0) {
-    const size_t need = commit_ws_bytes(shape);
-    if (workspace == nullptr) return oda::fail(ODA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
-    if (workspace_bytes < need)
-      return oda::fail(ODA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
-    if (!oda::aligned(workspace, 256)) return oda::fail(ODA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    st = check_commit_workspace(shape, workspace, workspace_bytes);
+    if (st != ODA_OK) return st;
   }
   CommitArgs a;
   a.k_cache = k_cache;
@@ -168,8 +275,7 @@ oda_status run_commit(const oda_attn_shape* shape, uint16_t* k_cache, uint16_t* 
   a.v_full = v_full ? v_full : v_local;
   a.flags = flags;
   a.tickets = advance != 0 ? static_cast<uint32_t*>(workspace) : nullptr;
-  a.kv_layer_stride = shape->layer_stride_kv != 0 ? shape->layer_stride_kv
-                                                  : shape->num_blocks * shape->num_kv_heads * kBlock * shape->head_dim;
+  a.kv_layer_stride = layer_stride(shape);
   a.L = shape->num_layers;
   a.B = shape->batch;
   a.Hkv = shape->num_kv_heads;
@@ -219,4 +325,62 @@ extern "C" oda_status oda_commit_kv_ring(const oda_attn_shape* shape, uint16_t* 
   if (n_sink < 0 || window < 1) return oda::fail(ODA_ERR_SHAPE, "n_sink >= 0 and window >= 1 required");
   return run_commit(shape, k_cache, v_cache, block_table, seq_lens, k_local, v_local, k_full, v_full, flags, advance,
                     workspace, workspace_bytes, k_ring, v_ring, n_sink, window, stream);
+}
+
+extern "C" oda_status oda_commit_drafts(const oda_attn_shape* shape, int32_t tokens, uint16_t* k_cache,
+                                       uint16_t* v_cache, const int32_t* block_table, int32_t* seq_lens,
+                                       const uint16_t* k_cand, const uint16_t* v_cand, const int32_t* n_accepted,
+                                       int32_t advance, int32_t* row_lens, void* workspace, size_t workspace_bytes,
+                                       uint16_t* k_ring, uint16_t* v_ring, int32_t n_sink, int32_t window,
+                                       hipStream_t stream) {
+  oda_status st = check_commit_shape(shape);
+  if (st != ODA_OK) return st;
+  if (tokens < 1 || tokens > kMaxTokens) return oda::fail(ODA_ERR_SHAPE, "tokens %d not in 1..%d", tokens, kMaxTokens);
+  if (!k_cache || !v_cache || !block_table || !seq_lens || !k_cand || !v_cand)
+    return oda::fail(ODA_ERR_NULL, "k_cache, v_cache, block_table, seq_lens, k_cand and v_cand are required");
+  if ((k_ring == nullptr) != (v_ring == nullptr))
+    return oda::fail(ODA_ERR_NULL, "k_ring and v_ring must both be NULL or both be set");
+  if (!oda::aligned(k_cache, 16) || !oda::aligned(v_cache, 16) || !oda::aligned(k_cand, 16) || !oda::aligned(v_cand, 16) ||
+      (k_ring && (!oda::aligned(k_ring, 16) || !oda::aligned(v_ring, 16))))
+    return oda::fail(ODA_ERR_SHAPE, "caches, candidates and rings must be 16-byte aligned");
+  if (k_ring && (n_sink < 0 || window < 1)) return oda::fail(ODA_ERR_SHAPE, "n_sink >= 0 and window >= 1 required");
+  if (row_lens && advance == 0) return oda::fail(ODA_ERR_SHAPE, "row_lens needs advance != 0");
+  if (advance != 0) {
+    st = check_commit_workspace(shape, workspace, workspace_bytes);
+    if (st != ODA_OK) return st;
+  }
+  CommitDraftsArgs a;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.block_table = block_table;
+  a.seq_lens = seq_lens;
+  a.k_cand = k_cand;
+  a.v_cand = v_cand;
+  a.n_accepted = n_accepted;
+  a.row_lens = row_lens;
+  a.tickets = advance != 0 ? static_cast<uint32_t*>(workspace) : nullptr;
+  a.kv_layer_stride = layer_stride(shape);
+  a.NB = shape->num_blocks;
+  a.L = shape->num_layers;
+  a.B = shape->batch;
+  a.T = tokens;
+  a.Hkv = shape->num_kv_heads;
+  a.D = shape->head_dim;
+  a.MB = shape->max_blocks_per_seq;
+  a.k_ring = k_ring;
+  a.v_ring = v_ring;
+  const oda::RingGeometry rg = oda::ring_geometry(k_ring ? n_sink : 0, k_ring ? window : 1);
+  a.ring_sb = rg.sink_blocks;
+  a.ring_rb = rg.ring_blocks;
+  const int64_t units = (int64_t)a.L * a.Hkv;
+  const int64_t want = std::min<int64_t>(units, oda::ceil_div(kTargetGroups, a.B));
+  a.units_per_chunk = (int)oda::ceil_div(units, want);
+  a.chunks = (int)oda::ceil_div(units, a.units_per_chunk);
+  const int64_t groups = (int64_t)a.B * a.chunks;
+  if (groups > 0x7fffffffLL || units * a.D * tokens > 0x7fffffffLL) return oda::fail(ODA_ERR_SHAPE, "grid too large");
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(commit_drafts_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return oda::fail(ODA_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return oda::ok();
 }

@@ -6,6 +6,7 @@
 //
 //   oda_dense_bf16    y = W . RMSNorm(x) (optional), + residual (optional), or
 //                     the SwiGLU pair SiLU(W_g . x') * (W_u . x')
+//   oda_dense_lora_bf16  the same with a low-rank adapter per request beside W
 //   oda_qk_norm_rope  per-head RMSNorm of q and k, rotary embedding at each
 //                     request's current position, bf16 q / K / V candidates
 //   oda_embed_bf16    embedding rows of the step's tokens
@@ -22,8 +23,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "oda.h"
 #include "oda_device.h"
@@ -72,14 +75,108 @@ struct DenseArgs {
   float eps;
 };
 
+// A dense layer with low-rank adapters: t = scale A x' of every selected request
+// (lora_shrink_kernel, without the norm's factor, which the epilogue applies to
+// the sum) and the adapters' second factors.
+struct DenseLoraArgs : DenseArgs {
+  const uint16_t* lora_b;    // [num][rows][rank]
+  const float* t;            // [B][parts * rank]
+  const int32_t* ids;        // [B]
+  int64_t adapter_stride;    // rows * rank
+  int num, rank, parts;
+  int part_end[ODA_LORA_MAX_PARTS];
+};
+
+// The adapter of request b: -1 for none, -2 for an id outside the range.
+__device__ __forceinline__ int adapter_of(const int32_t* ids, int num, int b) {
+  const int id = ids[b];
+  return id >= -1 && id < num ? id : -2;
+}
+// The row of t that output row r multiplies.
+__device__ __forceinline__ const float* lora_t(const DenseLoraArgs& p, int b, int r) {
+  int part = 0;
+#pragma unroll
+  for (int q = 0; q + 1 < ODA_LORA_MAX_PARTS; ++q) part += (q + 1 < p.parts && r >= p.part_end[q]) ? 1 : 0;
+  return p.t + ((int64_t)b * p.parts + part) * p.rank;
+}
+// Eight terms of a row of the second factor with t.
+__device__ __forceinline__ float lora_dot8(const uint16_t* b8, const float* t8) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(b8);
+  const float4 t0 = *reinterpret_cast<const float4*>(t8), t1 = *reinterpret_cast<const float4*>(t8 + 4);
+  return bf16_lo(w[0]) * t0.x + bf16_hi(w[0]) * t0.y + bf16_lo(w[1]) * t0.z + bf16_hi(w[1]) * t0.w +
+         bf16_lo(w[2]) * t1.x + bf16_hi(w[2]) * t1.y + bf16_lo(w[3]) * t1.z + bf16_hi(w[3]) * t1.w;
+}
+
+// t[b][r] = scale[a] * sum_k A[a][r][k] gain[k] x[b][k] for the rank rows r of all
+// parts, a = the request's adapter.  One wavefront per R rows of one request.
+struct LoraShrinkArgs {
+  const uint16_t* a;         // [num][rows][K], rows = parts * rank
+  const float* scale;
+  const float* gain;         // or NULL
+  const float* x;
+  const int32_t* ids;
+  float* t;                  // [B][rows]
+  const int32_t* work_list;
+  const int32_t* n_work;
+  int num, rows, K, B;
+};
+
+template <int R>
+__global__ __launch_bounds__(256) void lora_shrink_kernel(LoraShrinkArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int row0 = (blockIdx.x * kWaves + wave) * R;   // rows is a multiple of R
+  if (row0 >= p.rows || (int)blockIdx.y >= selected_count(p.n_work, p.B)) return;
+  const int b = selected_request(p.work_list, blockIdx.y);
+  if (b < 0 || b >= p.B) return;
+  const int id = uniform(adapter_of(p.ids, p.num, b));
+  if (id < 0) return;
+  const float* xr = p.x + (int64_t)b * p.K;
+  const uint16_t* wrow = p.a + ((int64_t)id * p.rows + row0) * p.K;
+  float acc[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) acc[j] = 0.f;
+  const int nchunks = (p.K + 511) / 512;
+#pragma unroll 4
+  for (int c = 0; c < nchunks; ++c) {
+    const int k0 = c * 512 + 8 * lane;
+    const bool in = k0 < p.K;
+    const int k = in ? k0 : 0;
+    u32x4 w[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) w[j] = *reinterpret_cast<const u32x4*>(wrow + (int64_t)j * p.K + k);
+    const float4 x0 = *reinterpret_cast<const float4*>(xr + k), x1 = *reinterpret_cast<const float4*>(xr + k + 4);
+    float xv[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+    if (p.gain != nullptr) {
+      const float4 g0 = *reinterpret_cast<const float4*>(p.gain + k), g1 = *reinterpret_cast<const float4*>(p.gain + k + 4);
+      const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xv[e] *= g[e];
+    }
+    if (!in) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < R; ++j) acc[j] += ((e & 1) ? bf16_hi(w[j][e >> 1]) : bf16_lo(w[j][e >> 1])) * xv[e];
+  }
+  float v = 0.f;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const float sum = wave_sum(acc[j]);
+    if (lane == j) v = sum;
+  }
+  if (lane < R) p.t[(int64_t)b * p.rows + row0 + lane] = v * p.scale[id];
+}
+
 // One request per grid row, one wavefront per group of R output rows.  Lanes take 8
 // consecutive weights of each row (one 16-byte load per row), so a wavefront
 // reads R KiB per 512-element chunk, several chunks in flight; every input
 // load serves all R rows.  The inputs come from cache.  The input's sum of
 // squares (for RMSNorm) accumulates in the same pass.  R > 1 makes the
 // wavefronts of a layer with many short rows fewer and longer.
-template <bool kSwiGLU, int R>
-__global__ __launch_bounds__(256) void dense_kernel(DenseArgs p) {
+template <bool kSwiGLU, int R, class Args>
+__global__ __launch_bounds__(256) void dense_kernel(Args p) {
+  constexpr bool kLora = std::is_same<Args, DenseLoraArgs>::value;
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const int item = blockIdx.x * kWaves + wave;
@@ -155,6 +252,23 @@ __global__ __launch_bounds__(256) void dense_kernel(DenseArgs p) {
           const uint32_t we2 = w2[j][e >> 1];
           acc2[j] += ((e & 1) ? bf16_hi(we2) : bf16_lo(we2)) * xg;
         }
+      }
+    }
+  }
+
+  // the adapter: rank / 8 lanes hold eight more terms of every row's sum
+  if constexpr (kLora) {
+    const int id = uniform(adapter_of(p.ids, p.num, b));
+    if (id == -2) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) acc[j] = __builtin_nanf("");
+    } else if (id >= 0 && 8 * lane < p.rank) {
+      const uint16_t* lb = p.lora_b + (int64_t)id * p.adapter_stride + 8 * lane;
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        acc[j] += lora_dot8(lb + (int64_t)(row0 + j) * p.rank, lora_t(p, b, row0 + j) + 8 * lane);
+        if (kSwiGLU)
+          acc2[j] += lora_dot8(lb + (int64_t)(p.N + row0 + j) * p.rank, lora_t(p, b, p.N + row0 + j) + 8 * lane);
       }
     }
   }
@@ -257,9 +371,10 @@ __device__ __forceinline__ void split_bf16x3(const float (&x)[8], bf16x8 (&p)[3]
 //           rows and columns 8..15 hold the same rows and requests over the
 //           second half of K (the two off-diagonal quadrants are not used), so
 //           that a layer of few rows still fills the chip
-template <bool kSwiGLU, bool kNorm, int P, bool kHalf>
+template <bool kSwiGLU, bool kNorm, int P, bool kHalf, class Args>
 __global__ __launch_bounds__(kMfmaWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
-void dense_mfma_kernel(DenseArgs p) {
+void dense_mfma_kernel(Args p) {
+  constexpr bool kLora = std::is_same<Args, DenseLoraArgs>::value;
   constexpr int S = kSwiGLU ? 2 * P : P;              // weight streams: stream P + i is tile i's up projection
   constexpr int kEdge = kHalf ? 8 : kMfmaRows;        // rows and requests per tile
   constexpr int U = kChunk / 32;                      // steps per chunk
@@ -495,22 +610,40 @@ void dense_mfma_kernel(DenseArgs p) {
         if (kNorm) sq += sm_ss[wv][hcol];
       }
     }
+    if constexpr (kLora) {
+      const int id = adapter_of(p.ids, p.num, out_b[q]);
+      if (id == -2) {
+        v = __builtin_nanf("");
+      } else if (id >= 0) {
+        const int r = row0 + tile * kEdge + row;
+        const uint16_t* lb = p.lora_b + (int64_t)id * p.adapter_stride + (int64_t)r * p.rank;
+        const float* lt = lora_t(p, out_b[q], r);
+        float d = 0.f, d2 = 0.f;
+        const float* lt2 = kSwiGLU ? lora_t(p, out_b[q], p.N + r) : nullptr;
+        for (int i = 0; i < p.rank; i += 8) {
+          d += lora_dot8(lb + i, lt + i);
+          if (kSwiGLU) d2 += lora_dot8(lb + (int64_t)p.N * p.rank + i, lt2 + i);
+        }
+        v += d;
+        v2 += d2;
+      }
+    }
     const float inv = kNorm ? rsqrtf(sq / (float)p.K + p.eps) : 1.f;
     const float out = kSwiGLU ? silu(v * inv) * (v2 * inv) : v * inv + res[q];
     p.y[(int64_t)out_b[q] * p.N + row0 + tile * kEdge + row] = out;
   }
 }
 
-template <bool kSwiGLU, int P, bool kHalf>
-oda_status launch_dense_mfma(const DenseArgs& a, hipStream_t stream) {
+template <bool kSwiGLU, int P, bool kHalf, class Args>
+oda_status launch_dense_mfma(const Args& a, hipStream_t stream) {
   constexpr int kEdge = kHalf ? 8 : kMfmaRows;
   const int64_t groups = oda::ceil_div(oda::ceil_div(a.N, P * kEdge), 8) * 8 * oda::ceil_div(a.B, kEdge);
   if (groups > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "layer too large");
   const dim3 grid((unsigned)groups), block(kMfmaWaves * 64);
   if (a.gain)
-    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, true, P, kHalf>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, true, P, kHalf, Args>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, false, P, kHalf>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, false, P, kHalf, Args>), grid, block, 0, stream, a);
   return ODA_OK;
 }
 
@@ -716,11 +849,8 @@ oda_status launch_status() {
   return oda::ok();
 }
 
-}  // namespace
-
-extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, const float* x,
-                                    const float* residual, float* y, const int32_t* work_list,
-                                    const int32_t* n_work, hipStream_t stream) {
+oda_status check_dense(const oda_dense_desc* desc, int32_t batch, const float* x, const float* residual, const float* y,
+                       const int32_t* work_list, const int32_t* n_work) {
   if (desc == nullptr) return oda::fail(ODA_ERR_NULL, "desc is NULL");
   if (!desc->weight || !x || !y) return oda::fail(ODA_ERR_NULL, "weight, x and y are required");
   if ((work_list == nullptr) != (n_work == nullptr))
@@ -735,11 +865,19 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
   if (!(desc->rms_eps >= 0.f) || !std::isfinite(desc->rms_eps)) return oda::fail(ODA_ERR_SHAPE, "rms_eps must be >= 0");
   if (!oda::aligned(desc->weight, 16) || !oda::aligned(x, 16) || (desc->norm_gain && !oda::aligned(desc->norm_gain, 16)))
     return oda::fail(ODA_ERR_SHAPE, "weight, x and norm_gain must be 16-byte aligned");
-  const int N = desc->out_features;
-  const bool swiglu = desc->mode == ODA_DENSE_SWIGLU;
-  DenseArgs a{desc->weight, desc->norm_gain, x, residual, y, work_list, n_work, N, desc->in_features, batch,
-              desc->rms_eps};
-  (void)hipGetLastError();
+  return ODA_OK;
+}
+
+DenseArgs dense_args(const oda_dense_desc* desc, int32_t batch, const float* x, const float* residual, float* y,
+                     const int32_t* work_list, const int32_t* n_work) {
+  return DenseArgs{desc->weight, desc->norm_gain, x, residual, y, work_list, n_work, desc->out_features,
+                   desc->in_features, batch, desc->rms_eps};
+}
+
+// The layer's launch, with (DenseLoraArgs) or without (DenseArgs) adapters.
+template <class Args>
+oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
+  const int N = a.N;
   // Several requests: the narrowest workgroup (row tiles and tile edge) that
   // still needs no more than one per CU, so that the launch is one even round;
   // layers too large for that take the widest.  Narrower ones re-split and
@@ -752,11 +890,11 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
   // against 240, 1536 -> 65536 35.1 against 35.8, but 1624 -> 151936 97 against
   // 83 and 2112 -> 151936 112 against 106.
   const auto groups_of = [&](int tiles, int edge) {
-    return oda::ceil_div(N, tiles * edge) * oda::ceil_div(batch, edge);
+    return oda::ceil_div(N, tiles * edge) * oda::ceil_div(a.B, edge);
   };
   const bool one = !swiglu && groups_of(2, kMfmaRows) >= 8 * kTargetGroups && a.K >= 3 * kMfmaWaves * kChunk &&
                    a.K % (kMfmaWaves * kChunk) == 0;
-  if ((batch > 1 || one) && a.K < kMfmaMaxK) {
+  if ((a.B > 1 || one) && a.K < kMfmaMaxK) {
     oda_status st;
     const auto fits = [&](int tiles, int edge) { return groups_of(tiles, edge) <= kTargetGroups; };
     if (swiglu) {
@@ -783,8 +921,8 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
       break;
     }
   const int64_t groups = oda::ceil_div(N / rows, kWaves);
-  const dim3 grid((unsigned)groups, (unsigned)batch), block(256);
-#define ODA_DENSE_LAUNCH(SW, R) hipLaunchKernelGGL((dense_kernel<SW, R>), grid, block, 0, stream, a)
+  const dim3 grid((unsigned)groups, (unsigned)a.B), block(256);
+#define ODA_DENSE_LAUNCH(SW, R) hipLaunchKernelGGL((dense_kernel<SW, R, Args>), grid, block, 0, stream, a)
   if (swiglu) {
     if (rows == 4) ODA_DENSE_LAUNCH(true, 4);
     else if (rows == 2) ODA_DENSE_LAUNCH(true, 2);
@@ -797,6 +935,98 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
   }
 #undef ODA_DENSE_LAUNCH
   return launch_status();
+}
+
+}  // namespace
+
+extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, const float* x,
+                                    const float* residual, float* y, const int32_t* work_list,
+                                    const int32_t* n_work, hipStream_t stream) {
+  const oda_status st = check_dense(desc, batch, x, residual, y, work_list, n_work);
+  if (st != ODA_OK) return st;
+  (void)hipGetLastError();
+  return launch_dense(dense_args(desc, batch, x, residual, y, work_list, n_work), desc->mode == ODA_DENSE_SWIGLU, stream);
+}
+
+namespace {
+
+constexpr int kMaxRank = 128;   // rank / 8 lanes of a wavefront hold a row of the second factor
+
+oda_status check_lora(const oda_lora_desc* lora, int64_t* rows) {
+  if (lora == nullptr) return oda::fail(ODA_ERR_NULL, "lora is NULL");
+  if (lora->num_adapters < 1) return oda::fail(ODA_ERR_SHAPE, "num_adapters must be >= 1");
+  if (lora->rank < 8 || lora->rank % 8 || lora->rank > kMaxRank)
+    return oda::fail(ODA_ERR_UNSUPPORTED, "rank %d: a multiple of 8 from 8 to %d required", lora->rank, kMaxRank);
+  if (lora->num_parts < 1 || lora->num_parts > ODA_LORA_MAX_PARTS)
+    return oda::fail(ODA_ERR_SHAPE, "num_parts %d not in 1..%d", lora->num_parts, ODA_LORA_MAX_PARTS);
+  *rows = 0;
+  for (int p = 0; p < lora->num_parts; ++p) {
+    if (lora->part_rows[p] < 1) return oda::fail(ODA_ERR_SHAPE, "part_rows[%d] must be >= 1", p);
+    *rows += lora->part_rows[p];
+  }
+  return ODA_OK;
+}
+
+size_t lora_ws_bytes(const oda_lora_desc* lora, int64_t batch) {
+  return (size_t)oda::round_up(batch * lora->num_parts * lora->rank * 4, 256);
+}
+
+}  // namespace
+
+extern "C" oda_status oda_lora_workspace_size(const oda_lora_desc* lora, int32_t batch, size_t* bytes) {
+  int64_t rows = 0;
+  const oda_status st = check_lora(lora, &rows);
+  if (st != ODA_OK) return st;
+  if (bytes == nullptr) return oda::fail(ODA_ERR_NULL, "bytes is NULL");
+  if (batch < 1) return oda::fail(ODA_ERR_SHAPE, "batch must be >= 1");
+  *bytes = lora_ws_bytes(lora, batch);
+  return oda::ok();
+}
+
+extern "C" oda_status oda_dense_lora_bf16(const oda_dense_desc* desc, const oda_lora_desc* lora, int32_t batch,
+                                         const float* x, const float* residual, float* y, const int32_t* adapter_ids,
+                                         const int32_t* work_list, const int32_t* n_work, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream) {
+  oda_status st = check_dense(desc, batch, x, residual, y, work_list, n_work);
+  if (st != ODA_OK) return st;
+  int64_t rows = 0;
+  st = check_lora(lora, &rows);
+  if (st != ODA_OK) return st;
+  if (!lora->a || !lora->b || !lora->scale || !adapter_ids)
+    return oda::fail(ODA_ERR_NULL, "a, b, scale and adapter_ids are required");
+  const bool swiglu = desc->mode == ODA_DENSE_SWIGLU;
+  if (rows != (int64_t)desc->out_features * (swiglu ? 2 : 1))
+    return oda::fail(ODA_ERR_SHAPE, "part_rows sum to %lld, the weight has %lld rows", (long long)rows,
+                     (long long)desc->out_features * (swiglu ? 2 : 1));
+  if (!oda::aligned(lora->a, 16) || !oda::aligned(lora->b, 16))
+    return oda::fail(ODA_ERR_SHAPE, "a and b must be 16-byte aligned");
+  const size_t need = lora_ws_bytes(lora, batch);
+  if (workspace == nullptr) return oda::fail(ODA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (workspace_bytes < need)
+    return oda::fail(ODA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  if (!oda::aligned(workspace, 256)) return oda::fail(ODA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const int t_rows = lora->num_parts * lora->rank;
+  LoraShrinkArgs sh{lora->a, lora->scale, desc->norm_gain, x, adapter_ids, static_cast<float*>(workspace), work_list,
+                    n_work, lora->num_adapters, t_rows, desc->in_features, batch};
+  DenseLoraArgs a;
+  static_cast<DenseArgs&>(a) = dense_args(desc, batch, x, residual, y, work_list, n_work);
+  a.lora_b = lora->b;
+  a.t = sh.t;
+  a.ids = adapter_ids;
+  a.adapter_stride = rows * lora->rank;
+  a.num = lora->num_adapters;
+  a.rank = lora->rank;
+  a.parts = lora->num_parts;
+  int64_t end = 0;
+  for (int p = 0; p < ODA_LORA_MAX_PARTS; ++p) {
+    if (p < lora->num_parts) end += lora->part_rows[p];
+    a.part_end[p] = (int)std::min<int64_t>(end, INT_MAX);
+  }
+  if (batch > 65535) return oda::fail(ODA_ERR_SHAPE, "batch %d above 65535", batch);
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(lora_shrink_kernel<1>, dim3((unsigned)oda::ceil_div(t_rows, kWaves), (unsigned)batch), dim3(256), 0,
+                     stream, sh);
+  return launch_dense(a, swiglu, stream);
 }
 
 extern "C" oda_status oda_qk_norm_rope(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
