@@ -82,7 +82,7 @@ def test_verify_refusals(L, kw, status):
     (dict(k_ring=0x9000, v_ring=0xb000), -2), (dict(k_ring=0x9000, v_ring=0xb000, n_sink=-1, window=4), -2),
     (dict(k_ring=0x9001, v_ring=0xb000, window=4), -2),
     (dict(ws=None), -4), (dict(wb=255), -4), (dict(ws=0x100010), -4), (dict(head_dim=96), -3), (dict(batch=0), -2),
-    (dict(num_layers=1 << 20, batch=1 << 14, wb=1 << 20), -2)])
+    (dict(num_layers=1 << 24), -2)])
 def test_commit_drafts_refusals(L, kw, status):
     a = dict(T=4, k=0x1000, v=0x2000, table=0x3000, seq=0x4000, kc=0x5000, vc=0x6000, ws=0x100000, wb=256, advance=True,
              rows=None, k_ring=None, v_ring=None, n_sink=0, window=0, head_dim=64, batch=3, num_layers=2)
