@@ -446,6 +446,61 @@ oda_status oda_argmax(int32_t batch, int32_t n, const float *x, int32_t *index, 
  * are row b * T + t of the calls above (batch * T rows).
  * ------------------------------------------------------------------------- */
 
+/* Requests whose histories begin with the same blocks (host struct holding
+ * device pointers).  Group j holds the requests members[group_start[j] ..
+ * group_start[j + 1] - 1]; the first prefix_blocks[j] entries of all their block
+ * table rows name the same blocks (the call reads the first attended member's).
+ * prefix_blocks[j] == 0: a group that shares nothing, such as a single request.
+ * A request belongs to one group; requests in none are left alone. */
+typedef struct {
+  int32_t num_groups;           /* 1..2048                                          */
+  int32_t tokens;               /* T: current tokens per request, 1..16             */
+  const int32_t *group_start;   /* int32 [num_groups + 1], ascending, within [0, B] */
+  const int32_t *members;       /* int32 [B]: request ids in group order            */
+  const int32_t *prefix_blocks; /* int32 [num_groups]                               */
+  const int32_t *n_tokens;      /* int32 [B]: current tokens of each request, clamped
+                                   to [0, T]; NULL: T each                          */
+  const int32_t *flags;         /* int32 [B]: members with flags[b] == 0 are left alone
+                                   (oda_recall_gate's flags); NULL: all             */
+} oda_prefix_groups;
+
+/* Bytes of the plan buffer and of the workspace of calls with these sizes (the
+ * shape, num_groups and tokens) (host out).  Neither needs to be cleared. */
+oda_status oda_prefix_plan_size(const oda_attn_shape *shape, const oda_prefix_groups *groups, size_t *bytes);
+oda_status oda_prefix_workspace_size(const oda_attn_shape *shape, const oda_prefix_groups *groups, size_t *bytes);
+
+/* Plans oda_prefix_decode_attn on the device: which rows are attended, and how
+ * their histories are split over the chip.  One plan serves every call of a step
+ * whose shape, groups, lengths and kind of candidate are the plan's (all layers
+ * of a stack or one call per layer: num_layers counts, so plan with the shape
+ * that is called).  Of `in`, seq_lens and whether k_cur is NULL are used.  When
+ * lengths, members, token counts or flags change, plan again: the attention reads
+ * them from the plan.  shape->split_blocks must be 0; batch at most 2048.
+ *   plan: >= oda_prefix_plan_size bytes, 256-byte aligned */
+oda_status oda_prefix_plan(const oda_attn_shape *shape, const oda_attn_inputs *in, const oda_prefix_groups *groups,
+                           void *plan, size_t plan_bytes, hipStream_t stream);
+
+/* Full decode attention (whole histories) of T current tokens per request, with
+ * the K/V of a group's prefix read once for all its members.  Row (b, t) attends
+ * positions 0 .. seq_lens[b] - 1 + t:
+ *   q        bf16 [L][B][T][Hq][D];  out fp32 [L][B][T][Hq][D];  lse fp32 [L][B][T][Hq]
+ *   k_cur, v_cur  bf16 [L][B][T][Hkv][D]: the current tokens' candidates; the cache
+ *            holds positions 0 .. seq_lens[b] - 2, row t attends candidates 0..t.
+ *            NULL: the cache holds the current tokens too, positions up to
+ *            seq_lens[b] - 2 + n_tokens[b]
+ * The result of each row is that of oda_full_decode_attn for a request of length
+ * seq_lens[b] + t, up to rounding.  Only rows of the groups' flagged members with
+ * t < n_tokens[b] are written.
+ * A request whose length (with its current tokens in the cache, their last
+ * position) is outside [1, max_seq_len] or shorter than its group's prefix, or
+ * that uses a table entry outside [0, num_blocks), gets NaN rows; an entry of the
+ * prefix does that to the whole group.  A plan made for other sizes gives NaN
+ * throughout.  workspace: >= oda_prefix_workspace_size bytes, 256-byte aligned;
+ * calls that may overlap in time need separate ones (a plan may be shared). */
+oda_status oda_prefix_decode_attn(const oda_attn_shape *shape, const oda_attn_inputs *in,
+                                  const oda_prefix_groups *groups, const void *plan, size_t plan_bytes, float *out,
+                                  float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 #define ODA_LORA_MAX_PARTS 4
 
 /* Low-rank adapters of a dense layer (host struct holding device pointers).  A

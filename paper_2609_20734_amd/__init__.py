@@ -23,7 +23,8 @@ _EXPORTS = ("HEAD_MLP", "HEAD_PAPER", "OdaError", "Shape", "attn_workspace_size"
             "prepare_argmax", "stream_read", "prepare_stream_read", "rms_norm_rows", "prepare_rms_norm_rows",
             "recall_gate_static", "qkv_prep", "prepare_local_qkv", "prepare_full_qkv",
             "ring_elements", "ring_fill", "local_decode_attn_ring", "commit_kv_ring", "prepare_local_ring",
-            "lora_desc", "lora_workspace_size", "dense_lora_bf16", "prepare_dense_lora", "verify_desc",
+            "prefix_groups", "prefix_plan_size", "prefix_workspace_size", "prefix_plan", "prefix_decode_attn",
+            "prepare_prefix_plan", "prepare_prefix_decode_attn", "lora_desc", "lora_workspace_size", "dense_lora_bf16", "prepare_dense_lora", "verify_desc",
             "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts")
 
 

@@ -45,7 +45,8 @@ EXPORTED = ("oda_attn_workspace_size", "oda_local_decode_attn", "oda_full_decode
             "oda_commit_workspace_size", "oda_commit_kv",
             "oda_ring_elements", "oda_ring_fill", "oda_local_decode_attn_ring", "oda_commit_kv_ring",
             "oda_dense_bf16", "oda_qk_norm_rope", "oda_embed_bf16", "oda_copy_rows", "oda_rms_norm_rows",
-            "oda_argmax", "oda_lora_workspace_size", "oda_dense_lora_bf16", "oda_verify_workspace_size",
+            "oda_argmax", "oda_prefix_plan_size", "oda_prefix_workspace_size", "oda_prefix_plan",
+            "oda_prefix_decode_attn", "oda_lora_workspace_size", "oda_dense_lora_bf16", "oda_verify_workspace_size",
             "oda_verify_drafts", "oda_commit_drafts", "oda_stream_read", "oda_status_string", "oda_last_error")
 
 
@@ -85,6 +86,12 @@ class GateDesc(ctypes.Structure):
 class DenseDesc(ctypes.Structure):
     _fields_ = [("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("rms_eps", ctypes.c_float), ("weight", ctypes.c_void_p), ("norm_gain", ctypes.c_void_p)]
+
+
+class PrefixGroups(ctypes.Structure):
+    _fields_ = [("num_groups", ctypes.c_int32), ("tokens", ctypes.c_int32), ("group_start", ctypes.c_void_p),
+                ("members", ctypes.c_void_p), ("prefix_blocks", ctypes.c_void_p), ("n_tokens", ctypes.c_void_p),
+                ("flags", ctypes.c_void_p)]
 
 
 class LoraDesc(ctypes.Structure):
@@ -160,6 +167,14 @@ _lib.oda_rms_norm_rows.argtypes = [ctypes.c_int32, ctypes.c_int32, _V, _V, ctype
 _lib.oda_rms_norm_rows.restype = ctypes.c_int
 _lib.oda_argmax.argtypes = [ctypes.c_int32, ctypes.c_int32, _V, _V, _V]
 _lib.oda_argmax.restype = ctypes.c_int
+for _fn in (_lib.oda_prefix_plan_size, _lib.oda_prefix_workspace_size):
+    _fn.argtypes = [_P(AttnShape), _P(PrefixGroups), _P(ctypes.c_size_t)]
+    _fn.restype = ctypes.c_int
+_lib.oda_prefix_plan.argtypes = [_P(AttnShape), _P(AttnInputs), _P(PrefixGroups), _V, ctypes.c_size_t, _V]
+_lib.oda_prefix_plan.restype = ctypes.c_int
+_lib.oda_prefix_decode_attn.argtypes = [_P(AttnShape), _P(AttnInputs), _P(PrefixGroups), _V, ctypes.c_size_t, _V, _V, _V,
+                                        ctypes.c_size_t, _V]
+_lib.oda_prefix_decode_attn.restype = ctypes.c_int
 _lib.oda_lora_workspace_size.argtypes = [_P(LoraDesc), ctypes.c_int32, _P(ctypes.c_size_t)]
 _lib.oda_lora_workspace_size.restype = ctypes.c_int
 _lib.oda_dense_lora_bf16.argtypes = [_P(DenseDesc), _P(LoraDesc), ctypes.c_int32, _V, _V, _V, _V, _V, _V, _V,
@@ -390,6 +405,37 @@ def argmax(batch: int, n: int, x, index, stream=None) -> None:
     _check(_lib.oda_argmax(batch, n, _ptr(x), _ptr(index), _stream(stream)))
 
 
+def prefix_groups(num_groups: int, tokens: int, group_start, members, prefix_blocks, n_tokens=None,
+                  flags=None) -> PrefixGroups:
+    """The C description of groups that share a prefix; it keeps the tensors alive."""
+    s = PrefixGroups(num_groups, tokens, _ptr(group_start), _ptr(members), _ptr(prefix_blocks), _ptr(n_tokens),
+                     _ptr(flags))
+    s._keep = (group_start, members, prefix_blocks, n_tokens, flags)
+    return s
+
+
+def prefix_plan_size(shape: Shape, groups: PrefixGroups) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_prefix_plan_size(ctypes.byref(shape.c()), ctypes.byref(groups), ctypes.byref(out)))
+    return out.value
+
+
+def prefix_workspace_size(shape: Shape, groups: PrefixGroups) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_prefix_workspace_size(ctypes.byref(shape.c()), ctypes.byref(groups), ctypes.byref(out)))
+    return out.value
+
+
+def prefix_plan(shape: Shape, inp: AttnInputs, groups: PrefixGroups, plan, plan_bytes: int | None = None,
+                stream=None) -> None:
+    prepare_prefix_plan(shape, inp, groups, plan, plan_bytes, stream)()
+
+
+def prefix_decode_attn(shape: Shape, inp: AttnInputs, groups: PrefixGroups, plan, out, lse, workspace,
+                       plan_bytes: int | None = None, workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_prefix_decode_attn(shape, inp, groups, plan, out, lse, workspace, plan_bytes, workspace_bytes, stream)()
+
+
 def lora_desc(num_adapters: int, rank: int, part_rows, a, b, scale) -> LoraDesc:
     """The C adapter description; it keeps the factors and scales alive."""
     if not 1 <= len(part_rows) <= 4:
@@ -570,6 +616,22 @@ def prepare_rms_norm_rows(batch: int, row_len: int, x, gain, rms_eps: float, y, 
 def prepare_argmax(batch: int, n: int, x, index, stream=None) -> Call:
     args = (batch, n, _ptr(x), _ptr(index), _stream(stream))
     return Call(_lib.oda_argmax, args, (x, index))
+
+
+def prepare_prefix_plan(shape: Shape, inp: AttnInputs, groups: PrefixGroups, plan, plan_bytes: int | None = None,
+                        stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), ctypes.byref(inp), ctypes.byref(groups), _ptr(plan), _nbytes(plan, plan_bytes),
+            _stream(stream))
+    return Call(_lib.oda_prefix_plan, args, (cs, inp, groups, plan))
+
+
+def prepare_prefix_decode_attn(shape: Shape, inp: AttnInputs, groups: PrefixGroups, plan, out, lse, workspace,
+                               plan_bytes: int | None = None, workspace_bytes: int | None = None, stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), ctypes.byref(inp), ctypes.byref(groups), _ptr(plan), _nbytes(plan, plan_bytes), _ptr(out),
+            _ptr(lse), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+    return Call(_lib.oda_prefix_decode_attn, args, (cs, inp, groups, plan, out, lse, workspace))
 
 
 def prepare_dense_lora(desc: DenseDesc, lora: LoraDesc, batch: int, x, residual, y, adapter_ids, workspace,

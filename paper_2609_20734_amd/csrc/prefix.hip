@@ -1,0 +1,942 @@
+// Decode attention of requests that share a prefix (oda_prefix_plan,
+// oda_prefix_decode_attn): the K/V of a group's common blocks is read once for
+// all of the group's rows, each request's own blocks once for its rows.
+//
+// A row is (request, current token); its G query heads of a KV head are G
+// columns of a score tile S^T = K Q^T.  Work of one (layer, KV head) unit comes
+// in items: a range of blocks against up to 256 columns, either a group's
+// (prefix) or one request's (the rest of its history).  An item's eight
+// wavefronts form a grid of position ranges times column pairs of tiles; each
+// keeps a running maximum and sum per column (one pass over the data) and its
+// share of O = P V in registers, and the position ranges are joined in LDS.  An
+// item writes an unnormalised partial (m, l, o) per column; the merge joins a
+// row's partials of both parts in order and adds the positions that only this
+// row or later ones see (the current tokens), one at a time.
+//
+// The plan (which rows, items and splits) is made on the device from lengths,
+// members and flags, by one workgroup, once for all layers of a step.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <cmath>
+
+#include "oda.h"
+#include "oda_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBlock = 16;            // positions per KV block, columns per MFMA tile
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * 64;
+constexpr int kWaveTiles = 2;         // column tiles a wavefront holds
+constexpr int kMaxCols = kWaves * kWaveTiles * kBlock;   // columns of an item
+constexpr int kMaxTokens = 16;
+constexpr int kMaxBatch = 2048;       // members and groups that the plan's workgroup holds in LDS
+constexpr int kCus = 256;
+constexpr int kPlanThreads = 256;
+constexpr uint32_t kMagic = 0x0da9f1u;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Plan buffer, int32 words: the header, then a Row per current token of the
+// batch, then the items.
+struct PlanHeader {
+  uint32_t magic;
+  int32_t batch, tokens, group, max_blocks, cached, part_cols;   // what the plan was made for
+  int32_t n_items, n_rows, n_bad;    // items; rows with work; rows after them that become NaN
+  int32_t reserved[6];
+};
+struct Row {
+  int32_t id;                        // request * tokens + token
+  int32_t len;                       // positions before the row's own: below len for all rows of the request
+  int32_t pre_part, pre_splits, pre_stride;   // partial columns of the prefix: head h of split s at part + s * stride + h
+  int32_t own_part, own_splits, own_stride;   // of the request's own blocks
+};
+struct Item {
+  int32_t row0;                      // first row of the columns' rows
+  int32_t col0, ncols;               // columns: col = row * G + head, counted from row0
+  int32_t request;                   // whose block table
+  int32_t blk_lo, blk_hi;
+  int32_t limit;                     // positions from here on are not attended
+  int32_t part;                      // first partial column
+};
+
+__host__ __device__ constexpr int rows_at() { return (int)(sizeof(PlanHeader) / 4); }
+__host__ __device__ constexpr int items_at(int rows) { return rows_at() + rows * (int)(sizeof(Row) / 4); }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// ---------------------------------------------------------------------------
+// the plan
+// ---------------------------------------------------------------------------
+
+struct PlanArgs {
+  const int32_t* seq_lens;
+  const int32_t* group_start;
+  const int32_t* members;
+  const int32_t* prefix_blocks;
+  const int32_t* n_tokens;
+  const int32_t* flags;
+  int32_t* plan;
+  int32_t B, NG, T, G, MB, max_len, cached;   // cached: the current tokens are in the cache
+  int32_t units;                              // (layer, KV head) pairs
+  int32_t extra_items;                        // items beyond one per piece
+  int32_t chunk_cols;                         // columns of a whole prefix item: a multiple of G
+  int32_t part_cols;
+};
+
+// Cost of an item: blocks times what a block takes, in eighths of the time in
+// which one CU's share of HBM delivers it: a tile's products and softmax take
+// about an eighth of that, so up to eight tiles are free.
+constexpr float kBlockCost = 8.f;
+constexpr float kItemCost = 80.f;       // start-up, the join and the partial's share of the merge
+constexpr float kLeastCost = 16 * kBlockCost;   // shortest split: two blocks per wavefront
+
+__device__ __forceinline__ float block_cost(int cols) { return fmaxf(kBlockCost, (float)((cols + kBlock - 1) / kBlock)); }
+
+// Splits of a piece of `blocks` blocks for items of cost t, and their length.
+__device__ __forceinline__ int split_count(int blocks, float cost, float t) {
+  return blocks <= 0 ? 0 : max(1, (int)ceilf((float)blocks * cost / t));
+}
+__device__ __forceinline__ int split_length(int blocks, int splits) {
+  return splits <= 0 ? 2 : ((blocks + splits - 1) / splits + 1) & ~1;
+}
+
+// Exclusive sums of x over the workgroup's threads, and the total.
+__device__ __forceinline__ int block_scan(int x, int* s_wave, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int v = x;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int y = __shfl_up(v, s);
+    if (lane >= s) v += y;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = v;
+  __syncthreads();
+  int base = 0;
+  total = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) base += s_wave[w];
+    total += s_wave[w];
+  }
+  return base + v - x;
+}
+
+struct PlanSlot {
+  int32_t request;      // -1: not attended
+  int32_t tokens;       // rows (0: none)
+  int32_t len;          // positions common to the request's rows
+  int32_t row;          // first row
+  int32_t group;
+  int32_t blocks;       // own blocks
+  int32_t splits;
+  int32_t part;
+};
+struct PlanGroup {
+  int32_t start;        // first slot
+  int32_t blocks;       // of the prefix; -1: outside the table
+  int32_t leader;       // first slot whose table is read (INT_MAX: none)
+  int32_t row, rows;
+  int32_t splits;       // per chunk
+  int32_t part;
+  int32_t reserved;
+};
+__host__ __device__ constexpr size_t plan_lds(int B, int NG) {
+  return (size_t)B * sizeof(PlanSlot) + (size_t)(NG + 1) * sizeof(PlanGroup);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  PlanSlot* slots = reinterpret_cast<PlanSlot*>(lds);
+  PlanGroup* groups = reinterpret_cast<PlanGroup*>(lds + (size_t)a.B * sizeof(PlanSlot));
+  __shared__ int s_wave[kPlanThreads / 64];
+  __shared__ int s_best;
+  const int tid = threadIdx.x, lane = tid & 63;
+  PlanHeader* head = reinterpret_cast<PlanHeader*>(a.plan);
+  Row* rows = reinterpret_cast<Row*>(a.plan + rows_at());
+  Item* items = reinterpret_cast<Item*>(a.plan + items_at(a.B * a.T));
+
+  // group starts, kept in [0, B] and ascending whatever the array holds
+  for (int j = tid; j <= a.NG; j += kPlanThreads) {
+    groups[j].start = min(max(a.group_start[j], 0), a.B);
+    groups[j].leader = INT_MAX;
+    groups[j].blocks = j < a.NG ? a.prefix_blocks[j] : 0;
+    if (groups[j].blocks > a.MB) groups[j].blocks = -1;
+  }
+  __syncthreads();
+  if (tid == 0)
+    for (int j = 1; j <= a.NG; ++j) groups[j].start = max(groups[j].start, groups[j - 1].start);
+  __syncthreads();
+  const int first = groups[0].start, count = groups[a.NG].start;
+
+  // slots: who attends what; rows in slot order, those that become NaN last
+  int n_rows = 0, n_bad = 0;
+  for (int s0 = first; s0 < count; s0 += kPlanThreads) {
+    const int s = s0 + tid;
+    PlanSlot p{};
+    p.request = -1;
+    bool bad = false;
+    if (s < count) {
+      int lo = 0, hi = a.NG;          // the last group that starts at or before s and is not empty there
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (groups[mid].start <= s) lo = mid;
+        else hi = mid;
+      }
+      p.group = lo;
+      const int b = a.members[s];
+      if (b >= 0 && b < a.B && (a.flags == nullptr || a.flags[b] != 0)) {
+        p.tokens = a.n_tokens ? min(max(a.n_tokens[b], 0), a.T) : a.T;
+        const int n = a.seq_lens[b], pre = groups[lo].blocks;
+        p.request = b;
+        p.len = a.cached ? n : n - 1;
+        bad = n < 1 || n > a.max_len || pre < 0 || p.len / kBlock < pre ||
+              (a.cached && p.tokens > 0 && n > a.max_len - (p.tokens - 1));
+        p.blocks = bad ? 0 : (p.len + kBlock - 1) / kBlock - pre;
+        if (!bad && p.tokens > 0) atomicMin(&groups[lo].leader, s);
+      }
+    }
+    int total = 0;
+    const int at = block_scan(bad ? 0 : p.tokens, s_wave, total);
+    p.row = n_rows + at;
+    n_rows += total;
+    if (s < count) slots[s] = p;
+    // NaN rows fill the table from its end
+    const int bad_at = block_scan(bad ? p.tokens : 0, s_wave, total);
+    if (bad)
+      for (int t = 0; t < p.tokens; ++t) {
+        Row r{};
+        r.id = p.request * a.T + t;
+        rows[a.B * a.T - 1 - (n_bad + bad_at + t)] = r;
+      }
+    if (bad && s < count) slots[s].tokens = 0;
+    n_bad += total;
+  }
+  __syncthreads();
+  for (int j = tid; j < a.NG; j += kPlanThreads) {
+    const int s0 = groups[j].start, s1 = groups[j + 1].start;
+    groups[j].row = s0 < count ? slots[s0].row : n_rows;
+    groups[j].rows = (s1 < count ? slots[s1].row : n_rows) - groups[j].row;
+    if (groups[j].rows == 0) groups[j].blocks = 0;
+  }
+  __syncthreads();
+
+  // the cost of a split: each lane of the first wavefront tries one
+  if (tid < 64) {
+    float most = kLeastCost, sum = 0.f;
+    for (int j = 0; j < a.NG; ++j) {
+      const int cols = min(groups[j].rows * a.G, a.chunk_cols);
+      const float c = (float)groups[j].blocks * block_cost(cols);
+      most = fmaxf(most, c);
+      sum += c * (float)((groups[j].rows * a.G + a.chunk_cols - 1) / a.chunk_cols);
+    }
+    for (int s = first; s < count; ++s) {
+      const float c = slots[s].tokens > 0 ? (float)slots[s].blocks * block_cost(slots[s].tokens * a.G) : 0.f;
+      most = fmaxf(most, c);
+      sum += c;
+    }
+    const float t = lane == 63 ? most : kLeastCost * exp2f(log2f(most / kLeastCost) * (float)lane / 63.f);
+    int n = 0, pieces = 0;
+    for (int j = 0; j < a.NG; ++j) {
+      const int chunks = (groups[j].rows * a.G + a.chunk_cols - 1) / a.chunk_cols;
+      n += chunks * split_count(groups[j].blocks, block_cost(min(groups[j].rows * a.G, a.chunk_cols)), t);
+      pieces += groups[j].blocks > 0 ? chunks : 0;
+    }
+    for (int s = first; s < count; ++s) {
+      if (slots[s].tokens <= 0) continue;
+      n += split_count(slots[s].blocks, block_cost(slots[s].tokens * a.G), t);
+      pieces += slots[s].blocks > 0 ? 1 : 0;
+    }
+    float est = (float)a.units * n <= (float)kCus
+                    ? t + kItemCost
+                    : (float)a.units * (sum + (float)n * kItemCost) / (float)kCus + 0.5f * t;
+    if (n - pieces > a.extra_items) est = INFINITY;
+    float best = est;
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
+    const uint64_t who = __ballot(est == best);
+    const int at = who ? 63 - __builtin_clzll(who) : 63;
+    const float chosen = __shfl(t, at);
+    if (lane == 0) s_best = __float_as_int(chosen);
+  }
+  __syncthreads();
+  const float t = __int_as_float(s_best);
+
+  // items of the prefixes, then of the requests' own blocks; partial columns alike
+  int n_items = 0, n_part = 0;
+  for (int j0 = 0; j0 < a.NG; j0 += kPlanThreads) {
+    const int j = j0 + tid;
+    int splits = 0, chunks = 0, cols = 0;
+    if (j < a.NG) {
+      cols = groups[j].rows * a.G;
+      chunks = (cols + a.chunk_cols - 1) / a.chunk_cols;
+      splits = split_count(groups[j].blocks, block_cost(min(cols, a.chunk_cols)), t);
+      if (splits > 0) splits = (groups[j].blocks + split_length(groups[j].blocks, splits) - 1) / split_length(groups[j].blocks, splits);
+    }
+    int total = 0;
+    const int part = n_part + block_scan(cols * splits, s_wave, total);
+    n_part += total;
+    const int item = n_items + block_scan(chunks * splits, s_wave, total);
+    n_items += total;
+    if (j < a.NG) {
+      groups[j].splits = splits;
+      groups[j].part = part;
+      groups[j].reserved = item;
+    }
+  }
+  __syncthreads();
+  for (int j = 0; j < a.NG; ++j) {
+    const PlanGroup g = groups[j];
+    if (g.splits == 0) continue;
+    const int cols = g.rows * a.G, chunks = (cols + a.chunk_cols - 1) / a.chunk_cols;
+    const int length = split_length(g.blocks, g.splits);
+    for (int i = tid; i < chunks * g.splits; i += kPlanThreads) {
+      const int split = i / chunks, c = i - split * chunks;     // the chunks of a range next to each other
+      Item it;
+      it.row0 = g.row;
+      it.col0 = c * a.chunk_cols;
+      it.ncols = min(a.chunk_cols, cols - it.col0);
+      it.request = slots[g.leader].request;
+      it.blk_lo = split * length;
+      it.blk_hi = min(g.blocks, it.blk_lo + length);
+      it.limit = g.blocks * kBlock;
+      it.part = g.part + it.col0 * g.splits + split * it.ncols;
+      items[g.reserved + i] = it;
+    }
+  }
+  for (int s0 = first; s0 < count; s0 += kPlanThreads) {
+    const int s = s0 + tid;
+    PlanSlot p{};
+    if (s < count) p = slots[s];
+    const int cols = p.tokens * a.G;
+    int splits = cols > 0 ? split_count(p.blocks, block_cost(cols), t) : 0;
+    const int length = split_length(p.blocks, splits);
+    if (splits > 0) splits = (p.blocks + length - 1) / length;
+    int total = 0;
+    const int part = n_part + block_scan(cols * splits, s_wave, total);
+    n_part += total;
+    const int item = n_items + block_scan(splits, s_wave, total);
+    n_items += total;
+    if (cols <= 0) continue;
+    const PlanGroup g = groups[p.group];
+    for (int i = 0; i < splits; ++i) {
+      Item it;
+      it.row0 = p.row;
+      it.col0 = 0;
+      it.ncols = cols;
+      it.request = p.request;
+      it.blk_lo = g.blocks + i * length;
+      it.blk_hi = min(g.blocks + p.blocks, it.blk_lo + length);
+      it.limit = p.len;
+      it.part = part + i * cols;
+      items[item + i] = it;
+    }
+    for (int k = 0; k < p.tokens; ++k) {
+      Row r;
+      r.id = p.request * a.T + k;
+      r.len = p.len;
+      const int col = (p.row + k - g.row) * a.G, chunk = col / a.chunk_cols * a.chunk_cols;
+      r.pre_splits = g.splits;
+      r.pre_stride = min(a.chunk_cols, g.rows * a.G - chunk);
+      r.pre_part = g.part + chunk * g.splits + (col - chunk);
+      r.own_splits = splits;
+      r.own_stride = cols;
+      r.own_part = part + k * a.G;
+      rows[p.row + k] = r;
+    }
+  }
+  if (tid == 0) {
+    PlanHeader h{};
+    h.magic = kMagic;
+    h.batch = a.B;
+    h.tokens = a.T;
+    h.group = a.G;
+    h.max_blocks = a.MB;
+    h.cached = a.cached;
+    h.part_cols = a.part_cols;
+    h.n_items = n_part <= a.part_cols ? n_items : 0;
+    h.n_rows = n_rows;
+    h.n_bad = n_bad;
+    *head = h;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+
+struct PrefixArgs {
+  const uint16_t* q;
+  const uint16_t* k_cache;
+  const uint16_t* v_cache;
+  const int32_t* block_table;
+  const uint16_t* k_cur;
+  const uint16_t* v_cur;
+  const int32_t* plan;
+  float* out;
+  float* lse;
+  float* part_o;      // [units][part_cols][D]
+  float* part_ml;     // [units][part_cols][2]  (m in log2 units, l)
+  int64_t kv_layer_stride;
+  int64_t num_blocks;
+  int32_t L, B, T, Hq, Hkv, G, MB;
+  int32_t part_cols, max_items;
+  float scale_log2;
+};
+
+__device__ __forceinline__ bool plan_fits(const PrefixArgs& a, const PlanHeader& h) {
+  return h.magic == kMagic && h.batch == a.B && h.tokens == a.T && h.group == a.G && h.max_blocks == a.MB &&
+         h.cached == (a.k_cur == nullptr ? 1 : 0) && h.part_cols == a.part_cols;
+}
+
+__device__ __forceinline__ bf16x8 load16(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ u32x2 load8(const uint16_t* p) { return *reinterpret_cast<const u32x2*>(p); }
+__device__ __forceinline__ bf16x8 cat(u32x2 lo, u32x2 hi) {
+  u32x4 t = {lo.x, lo.y, hi.x, hi.y};
+  return __builtin_bit_cast(bf16x8, t);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+__device__ __forceinline__ u32x2 mask_pack(u32x2 v, bool m0, bool m1, bool m2, bool m3) {
+  const uint32_t w0 = (m0 ? 0x0000FFFFu : 0u) | (m1 ? 0xFFFF0000u : 0u);
+  const uint32_t w1 = (m2 ? 0x0000FFFFu : 0u) | (m3 ? 0xFFFF0000u : 0u);
+  return u32x2{v.x & w0, v.y & w1};
+}
+
+// One wavefront's blocks [lo, hi) against its column tiles.  Register layouts of
+// v_mfma_f32_16x16x32_bf16 and the cache layouts' fit with them are those of the
+// decode attention (attention.hip): a K block's 16-byte groups are A operands of
+// S^T, the scores come out as the A operand of P V, two V blocks are its B.
+template <int D, int N>
+struct WaveState {
+  f32x4 o[N][D / 16];
+  float m[N], l[N];
+};
+
+template <int D, int N>
+__device__ __forceinline__ void stream_blocks(const PrefixArgs& a, const uint16_t* kbase, const uint16_t* vbase,
+                                              const int32_t* table, int lo, int hi, int limit, int lane,
+                                              const bf16x8 (&qf)[N][D / 32], WaveState<D, N>& w, int& bad) {
+  constexpr int KK = D / 32, NT = D / 16;
+  const int h16 = lane & 15, j = lane >> 4;
+  const int64_t blk_stride = (int64_t)a.Hkv * kBlock * D;
+  int tbl = 0;
+  for (int v = lo; v < hi; v += 2) {
+    if (((v - lo) & 63) == 0) {
+      const int e = v + lane < hi ? table[v + lane] : 0;
+      const bool ok = e >= 0 && e < a.num_blocks;
+      bad |= ok ? 0 : 1;
+      tbl = ok ? e : 0;
+    }
+    const int i0 = (v - lo) & 63;
+    const bool has1 = v + 1 < hi;
+    const int64_t pb0 = __builtin_amdgcn_readlane(tbl, i0);
+    const int64_t pb1 = has1 ? __builtin_amdgcn_readlane(tbl, i0 + 1) : pb0;
+    const uint16_t* k0 = kbase + pb0 * blk_stride;
+    const uint16_t* k1 = kbase + pb1 * blk_stride;
+    const uint16_t* v0 = vbase + pb0 * blk_stride;
+    const uint16_t* v1 = vbase + pb1 * blk_stride;
+    bf16x8 ka[KK], kb[KK];
+    u32x2 va[NT], vb[NT];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      ka[kk] = load16(k0 + (kk * 64 + lane) * 8);
+      kb[kk] = load16(k1 + (kk * 64 + lane) * 8);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      va[n] = load8(v0 + (16 * n + h16) * kBlock + 4 * j);
+      vb[n] = load8(v1 + (16 * n + h16) * kBlock + 4 * j);
+    }
+    // positions past the limit, and the second block of an odd end
+    const int last = has1 ? limit : min(limit, (v + 1) * kBlock);
+    const bool whole = (v + 2) * kBlock <= last;
+    bool keep[8];
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        keep[i] = v * kBlock + 4 * j + i < last;
+        keep[4 + i] = (v + 1) * kBlock + 4 * j + i < last;
+      }
+      // unattended slots may hold anything (even NaN): zero them so 0 * V stays 0
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        va[n] = mask_pack(va[n], keep[0], keep[1], keep[2], keep[3]);
+        vb[n] = mask_pack(vb[n], keep[4], keep[5], keep[6], keep[7]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kk], qf[c][kk], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[kk], qf[c][kk], s1, 0, 0, 0);
+      }
+      float sc[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[i] = s0[i] * a.scale_log2;
+        sc[4 + i] = s1[i] * a.scale_log2;
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sc[i] = keep[i] ? sc[i] : -INFINITY;
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sc[i]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(w.m[c], mx);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = exp2_fast(w.m[c] - m_use);
+      w.m[c] = m_new;
+      float p[8], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_fast(sc[i] - m_use);
+        sum += p[i];
+      }
+      w.l[c] = w.l[c] * alpha + sum;
+      if (__any(alpha != 1.f)) {
+        float al[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * j + i);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w.o[c][n][i] *= al[i];
+      }
+      // P in two bf16 parts, so that the product keeps 16 bits of it
+      bf16x8 phi, plo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const __bf16 h = (__bf16)p[i];
+        phi[i] = h;
+        plo[i] = (__bf16)(p[i] - (float)h);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bf16x8 vf = cat(va[n], vb[n]);
+        w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(phi, vf, w.o[c][n], 0, 0, 0);
+        w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(plo, vf, w.o[c][n], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// LDS of an item: per wavefront m and l of its tiles, then one tile's O at a time.
+constexpr int lds_floats(int D) { return kWaves * kWaveTiles * kBlock * 2 + kWaves * kBlock * D; }
+
+// The item's wavefront grid: WC column positions (of N tiles each) by 8 / WC
+// position ranges.
+template <int D, int N>
+__device__ __forceinline__ void run_item(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int wc_shift,
+                                         float* smem) {
+  constexpr int KK = D / 32, NT = D / 16;
+  const int lane = threadIdx.x & 63;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int h16 = lane & 15, j = lane >> 4;
+  const int WC = 1 << wc_shift, WP = kWaves >> wc_shift;
+  const int wc = wave & (WC - 1), wp = wave >> wc_shift;
+  const int pairs = (it.blk_hi - it.blk_lo + 1) >> 1;
+  const int per = (pairs + WP - 1) / WP;
+  const int lo = min(it.blk_hi, it.blk_lo + 2 * per * wp);
+  const int hi = min(it.blk_hi, lo + 2 * per);
+
+  WaveState<D, N> w;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    w.m[c] = -INFINITY;
+    w.l[c] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) w.o[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int tile0 = wc * N;
+  if (lo < hi && tile0 * kBlock < it.ncols) {
+    bf16x8 qf[N][KK];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const int col = (tile0 + c) * kBlock + h16;
+      const bool in = col < it.ncols;
+      const int at = in ? it.col0 + col : it.col0;
+      const int row = at / a.G, h = at - row * a.G;
+      const uint16_t* q = a.q + (((int64_t)l * a.B * a.T + rows[it.row0 + row].id) * a.Hq + g * a.G + h) * D;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) qf[c][kk] = in ? load16(q + 32 * kk + 8 * j) : bf16x8{};
+    }
+    const int64_t base = (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * D;
+    int bad = 0;
+    stream_blocks<D, N>(a, a.k_cache + base, a.v_cache + base, a.block_table + (int64_t)it.request * a.MB, lo, hi, it.limit,
+                        lane, qf, w, bad);
+    const bool any_bad = __any(bad);
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      w.l[c] += __shfl_xor(w.l[c], 16);
+      w.l[c] += __shfl_xor(w.l[c], 32);
+      if (any_bad) w.m[c] = w.l[c] = __builtin_nanf("");   // a table entry out of range: these rows become NaN
+    }
+  }
+
+  // join the position ranges, one tile of every column position at a time
+  float* sm_m = smem;                                    // [waves][N][16]
+  float* sm_l = smem + kWaves * kWaveTiles * kBlock;
+  float* sm_o = smem + 2 * kWaves * kWaveTiles * kBlock; // [waves][16][D]
+  if (j == 0) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      sm_m[(wave * N + c) * kBlock + h16] = w.m[c];
+      sm_l[(wave * N + c) * kBlock + h16] = w.l[c];
+    }
+  }
+  const int64_t part0 = ((int64_t)(l * a.Hkv + g)) * a.part_cols + it.part;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    if (c > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* dst = sm_o + (wave * kBlock + 4 * j + i) * D + h16;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) dst[16 * n] = w.o[c][n][i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < WC * kBlock * D / 2; e += kThreads) {
+      const int d = e % (D / 2) * 2, col16 = e / (D / 2) % kBlock, q = e / (D / 2) / kBlock;
+      const int col = (q * N + c) * kBlock + col16;
+      if (col >= it.ncols) continue;
+      float M = -INFINITY;
+      for (int p = 0; p < WP; ++p) M = fmaxf(M, sm_m[((p * WC + q) * N + c) * kBlock + col16]);
+      const float Mu = M == -INFINITY ? 0.f : M;
+      float acc0 = 0.f, acc1 = 0.f, lam = 0.f;
+      for (int p = 0; p < WP; ++p) {
+        const int wv = p * WC + q;
+        const float s = exp2_fast(sm_m[(wv * N + c) * kBlock + col16] - Mu);
+        const float2 ow = *reinterpret_cast<const float2*>(sm_o + (wv * kBlock + col16) * D + d);
+        acc0 += s * ow.x;
+        acc1 += s * ow.y;
+        lam += s * sm_l[(wv * N + c) * kBlock + col16];
+      }
+      *reinterpret_cast<float2*>(a.part_o + (part0 + col) * D + d) = make_float2(acc0, acc1);
+      if (d == 0) *reinterpret_cast<float2*>(a.part_ml + (part0 + col) * 2) = make_float2(M, lam);
+    }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void prefix_split_kernel(PrefixArgs a) {
+  extern __shared__ float smem[];
+  const PlanHeader& h = *reinterpret_cast<const PlanHeader*>(a.plan);
+  const int units = a.L * a.Hkv;
+  const int i = blockIdx.x / units, u = blockIdx.x - i * units;
+  if (!plan_fits(a, h) || i >= min(h.n_items, a.max_items)) return;
+  const Row* rows = reinterpret_cast<const Row*>(a.plan + rows_at());
+  const Item it = reinterpret_cast<const Item*>(a.plan + items_at(a.B * a.T))[i];
+  const int l = u / a.Hkv, g = u - l * a.Hkv;
+  const int tiles = (it.ncols + kBlock - 1) / kBlock;
+  if (tiles == 1) run_item<D, 1>(a, it, rows, l, g, 0, smem);
+  else run_item<D, kWaveTiles>(a, it, rows, l, g, tiles <= 2 ? 0 : tiles <= 4 ? 1 : tiles <= 8 ? 2 : 3, smem);
+}
+
+// Running softmax state of a lane's output elements.
+template <int PD>
+struct Acc {
+  float m = -INFINITY, l = 0.f, o[PD] = {};
+  __device__ __forceinline__ void add(float pm, float pl, const float (&po)[PD]) {
+    const float M = fmaxf(m, pm);
+    const float Mu = M == -INFINITY ? 0.f : M;
+    const float r = exp2_fast(m - Mu), s = exp2_fast(pm - Mu);
+    l = l * r + s * pl;
+#pragma unroll
+    for (int e = 0; e < PD; ++e) o[e] = o[e] * r + s * po[e];
+    m = M;
+  }
+};
+
+// One wavefront per (layer, row, query head): the prefix's partials, the own
+// blocks' partials, then the current tokens up to the row's own.
+template <int D>
+__global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
+  constexpr int PD = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+  const int64_t per_layer = (int64_t)a.B * a.T * a.Hq;
+  const int l = (int)(wave / per_layer);
+  if (l >= a.L) return;
+  const int rest = (int)(wave - l * per_layer);
+  const int r = rest / a.Hq, head = rest - r * a.Hq;
+  const PlanHeader& h = *reinterpret_cast<const PlanHeader*>(a.plan);
+  const Row* rows = reinterpret_cast<const Row*>(a.plan + rows_at());
+  const int all = a.B * a.T;
+  int64_t id = r;
+  const bool fits = plan_fits(a, h);
+  bool nan = !fits;                         // a plan of other sizes, or none
+  if (fits) {
+    if (r < h.n_rows) id = rows[r].id;
+    else if (r >= all - h.n_bad) {
+      id = rows[r].id;
+      nan = true;
+    } else return;
+  }
+  float* out = a.out + (((int64_t)l * all + id) * a.Hq + head) * D + lane * PD;
+  float* lse = a.lse ? a.lse + ((int64_t)l * all + id) * a.Hq + head : nullptr;
+  if (nan) {
+#pragma unroll
+    for (int e = 0; e < PD; ++e) out[e] = __builtin_nanf("");
+    if (lse && lane == 0) *lse = __builtin_nanf("");
+    return;
+  }
+  const Row row = rows[r];
+  const int g = head / a.G, hh = head - g * a.G;
+  const int64_t part0 = (int64_t)(l * a.Hkv + g) * a.part_cols + hh;
+  Acc<PD> acc;
+  for (int k = 0; k < 2; ++k) {
+    const int64_t part = part0 + (k == 0 ? row.pre_part : row.own_part);
+    const int splits = k == 0 ? row.pre_splits : row.own_splits, stride = k == 0 ? row.pre_stride : row.own_stride;
+    for (int s = 0; s < splits; ++s) {
+      const int64_t c = part + (int64_t)s * stride;
+      float po[PD];
+#pragma unroll
+      for (int e = 0; e < PD; ++e) po[e] = a.part_o[c * D + lane * PD + e];
+      acc.add(a.part_ml[c * 2], a.part_ml[c * 2 + 1], po);
+    }
+  }
+  // the current tokens this row attends: candidates, or the cache's last positions
+  const int b = (int)(id / a.T), t = (int)(id - (int64_t)b * a.T);
+  const int more = a.k_cur ? t + 1 : t;
+  float q[PD];
+#pragma unroll
+  for (int e = 0; e < PD; ++e) q[e] = bf16_to_float(a.q[(((int64_t)l * all + id) * a.Hq + head) * D + lane * PD + e]);
+  bool bad = false;
+  for (int i = 0; i < more; ++i) {
+    float kd[PD], vd[PD];
+    if (a.k_cur) {
+      const int64_t at = ((((int64_t)l * a.B + b) * a.T + i) * a.Hkv + g) * D + lane * PD;
+#pragma unroll
+      for (int e = 0; e < PD; ++e) {
+        kd[e] = bf16_to_float(a.k_cur[at + e]);
+        vd[e] = bf16_to_float(a.v_cur[at + e]);
+      }
+    } else {
+      const int pos = row.len + i;          // below the table's end: the plan checked the length
+      const int blk = a.block_table[(int64_t)b * a.MB + pos / kBlock];
+      if (blk < 0 || blk >= a.num_blocks) {
+        bad = true;
+        continue;
+      }
+      const int64_t at = (int64_t)l * a.kv_layer_stride + ((int64_t)blk * a.Hkv + g) * kBlock * D;
+#pragma unroll
+      for (int e = 0; e < PD; ++e) {
+        const int d = lane * PD + e;
+        kd[e] = bf16_to_float(a.k_cache[at + ((d / 8) * kBlock + pos % kBlock) * 8 + d % 8]);
+        vd[e] = bf16_to_float(a.v_cache[at + d * kBlock + pos % kBlock]);
+      }
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int e = 0; e < PD; ++e) dot += q[e] * kd[e];
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
+    dot *= a.scale_log2;
+    acc.add(dot, 1.f, vd);
+  }
+  if (bad) acc.l = __builtin_nanf("");
+#pragma unroll
+  for (int e = 0; e < PD; ++e) out[e] = acc.o[e] / acc.l;
+  if (lse && lane == 0) *lse = (acc.m + __log2f(acc.l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+
+// Sizes that host and plan agree on.  Items beyond one per piece fill the CUs
+// twice; each of them has at most kMaxCols partial columns.
+struct Sizes {
+  int group, chunk_cols, extra_items, part_cols, max_items;
+  size_t plan_bytes, off_ml, ws_bytes;
+};
+
+oda_status sizes_of(const oda_attn_shape* s, const oda_prefix_groups* p, Sizes* z) {
+  if (s == nullptr) return oda::fail(ODA_ERR_NULL, "shape is NULL");
+  if (p == nullptr) return oda::fail(ODA_ERR_NULL, "groups is NULL");
+  size_t unused = 0;
+  const oda_status st = oda_attn_workspace_size(s, 0, 0, &unused);   // the shape's own checks
+  if (st != ODA_OK) return st;
+  if (s->split_blocks != 0) return oda::fail(ODA_ERR_SHAPE, "split_blocks must be 0 (the plan chooses)");
+  if (p->tokens < 1 || p->tokens > kMaxTokens) return oda::fail(ODA_ERR_SHAPE, "tokens %d not in 1..%d", p->tokens, kMaxTokens);
+  if (p->num_groups < 1 || p->num_groups > kMaxBatch)
+    return oda::fail(ODA_ERR_SHAPE, "num_groups %d not in 1..%d", p->num_groups, kMaxBatch);
+  if (s->batch > kMaxBatch) return oda::fail(ODA_ERR_UNSUPPORTED, "batch %d above %d", s->batch, kMaxBatch);
+  const int64_t units = (int64_t)s->num_layers * s->num_kv_heads;
+  z->group = s->num_q_heads / s->num_kv_heads;
+  z->chunk_cols = kMaxCols / z->group * z->group;
+  const int64_t cols = (int64_t)s->batch * p->tokens * z->group;
+  z->extra_items = (int)oda::ceil_div(2 * kCus, units);
+  z->part_cols = (int)(2 * cols + (int64_t)z->extra_items * kMaxCols);
+  z->max_items = (int)(s->batch + std::min<int64_t>(p->num_groups, s->batch) + cols / z->chunk_cols + z->extra_items);
+  z->plan_bytes = (size_t)oda::round_up(
+      (items_at(s->batch * p->tokens) + (int64_t)z->max_items * (int64_t)(sizeof(Item) / 4)) * 4, 256);
+  z->off_ml = (size_t)oda::round_up(units * z->part_cols * s->head_dim * 4, 256);
+  z->ws_bytes = z->off_ml + (size_t)oda::round_up(units * z->part_cols * 8, 256);
+  return ODA_OK;
+}
+
+oda_status check_buffer(const char* name, const void* p, size_t bytes, size_t need) {
+  if (p == nullptr) return oda::fail(ODA_ERR_WORKSPACE, "%s is NULL (%zu bytes needed)", name, need);
+  if (bytes < need) return oda::fail(ODA_ERR_WORKSPACE, "%s has %zu bytes, %zu needed", name, bytes, need);
+  if (!oda::aligned(p, 256)) return oda::fail(ODA_ERR_WORKSPACE, "%s must be 256-byte aligned", name);
+  return ODA_OK;
+}
+
+oda_status launch_status() {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return oda::fail(ODA_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return oda::ok();
+}
+
+// Raise a kernel's dynamic-LDS limit once per device (the attribute belongs to
+// the device's copy of the kernel; host threads that race set the same value).
+// A failure shows in the launch that needs the limit.
+void raise_lds_limit(const void* kernel, std::atomic<uint64_t>* done, int bytes) {
+  int dev = -1;
+  (void)hipGetDevice(&dev);
+  const uint64_t bit = (dev >= 0 && dev < 64) ? (1ull << dev) : 0ull;
+  if (bit != 0 && (done->load(std::memory_order_acquire) & bit) != 0) return;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
+    done->fetch_or(bit, std::memory_order_acq_rel);
+}
+
+template <int D>
+oda_status launch_attention(const PrefixArgs& a, hipStream_t stream) {
+  const int64_t items = (int64_t)a.max_items * a.L * a.Hkv;
+  const int64_t merges = oda::ceil_div((int64_t)a.L * a.B * a.T * a.Hq, 4);
+  if (items > INT_MAX || merges > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "grid too large");
+  const int lds = lds_floats(D) * 4;
+  static std::atomic<uint64_t> raised{0};
+  raise_lds_limit(reinterpret_cast<const void*>(prefix_split_kernel<D>), &raised, lds);
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(prefix_split_kernel<D>, dim3((unsigned)items), dim3(kThreads), lds, stream, a);
+  hipLaunchKernelGGL(prefix_merge_kernel<D>, dim3((unsigned)merges), dim3(256), 0, stream, a);
+  return launch_status();
+}
+
+}  // namespace
+
+extern "C" oda_status oda_prefix_plan_size(const oda_attn_shape* shape, const oda_prefix_groups* groups, size_t* bytes) {
+  Sizes z;
+  const oda_status st = sizes_of(shape, groups, &z);
+  if (st != ODA_OK) return st;
+  if (bytes == nullptr) return oda::fail(ODA_ERR_NULL, "bytes is NULL");
+  *bytes = z.plan_bytes;
+  return oda::ok();
+}
+
+extern "C" oda_status oda_prefix_workspace_size(const oda_attn_shape* shape, const oda_prefix_groups* groups,
+                                               size_t* bytes) {
+  Sizes z;
+  const oda_status st = sizes_of(shape, groups, &z);
+  if (st != ODA_OK) return st;
+  if (bytes == nullptr) return oda::fail(ODA_ERR_NULL, "bytes is NULL");
+  *bytes = z.ws_bytes;
+  return oda::ok();
+}
+
+extern "C" oda_status oda_prefix_plan(const oda_attn_shape* shape, const oda_attn_inputs* in,
+                                     const oda_prefix_groups* groups, void* plan, size_t plan_bytes, hipStream_t stream) {
+  Sizes z;
+  oda_status st = sizes_of(shape, groups, &z);
+  if (st != ODA_OK) return st;
+  if (in == nullptr) return oda::fail(ODA_ERR_NULL, "inputs is NULL");
+  if (!in->seq_lens || !groups->group_start || !groups->members || !groups->prefix_blocks)
+    return oda::fail(ODA_ERR_NULL, "seq_lens, group_start, members and prefix_blocks are required");
+  if ((in->k_cur == nullptr) != (in->v_cur == nullptr))
+    return oda::fail(ODA_ERR_NULL, "k_cur and v_cur must both be NULL or both be set");
+  st = check_buffer("plan", plan, plan_bytes, z.plan_bytes);
+  if (st != ODA_OK) return st;
+  PlanArgs a;
+  a.seq_lens = in->seq_lens;
+  a.group_start = groups->group_start;
+  a.members = groups->members;
+  a.prefix_blocks = groups->prefix_blocks;
+  a.n_tokens = groups->n_tokens;
+  a.flags = groups->flags;
+  a.plan = static_cast<int32_t*>(plan);
+  a.B = shape->batch;
+  a.NG = groups->num_groups;
+  a.T = groups->tokens;
+  a.G = z.group;
+  a.MB = shape->max_blocks_per_seq;
+  a.max_len = shape->max_seq_len;
+  a.cached = in->k_cur == nullptr ? 1 : 0;
+  a.units = shape->num_layers * shape->num_kv_heads;
+  a.extra_items = z.extra_items;
+  a.chunk_cols = z.chunk_cols;
+  a.part_cols = z.part_cols;
+  const int lds = (int)plan_lds(a.B, a.NG);
+  static std::atomic<uint64_t> raised{0};
+  raise_lds_limit(reinterpret_cast<const void*>(prefix_plan_kernel), &raised, (int)plan_lds(kMaxBatch, kMaxBatch));
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(prefix_plan_kernel, dim3(1), dim3(kPlanThreads), lds, stream, a);
+  return launch_status();
+}
+
+extern "C" oda_status oda_prefix_decode_attn(const oda_attn_shape* shape, const oda_attn_inputs* in,
+                                            const oda_prefix_groups* groups, const void* plan, size_t plan_bytes,
+                                            float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream) {
+  Sizes z;
+  oda_status st = sizes_of(shape, groups, &z);
+  if (st != ODA_OK) return st;
+  if (in == nullptr) return oda::fail(ODA_ERR_NULL, "inputs is NULL");
+  if (!in->q || !in->k_cache || !in->v_cache || !in->block_table || !out)
+    return oda::fail(ODA_ERR_NULL, "q, k_cache, v_cache, block_table and out are required");
+  if ((in->k_cur == nullptr) != (in->v_cur == nullptr))
+    return oda::fail(ODA_ERR_NULL, "k_cur and v_cur must both be NULL or both be set");
+  if (!oda::aligned(in->q, 16) || !oda::aligned(in->k_cache, 16) || !oda::aligned(in->v_cache, 16) ||
+      !oda::aligned(out, 16) || (in->k_cur && (!oda::aligned(in->k_cur, 16) || !oda::aligned(in->v_cur, 16))))
+    return oda::fail(ODA_ERR_SHAPE, "q, caches, k_cur, v_cur and out must be 16-byte aligned");
+  if (!(in->scale > 0.f) || !std::isfinite(in->scale)) return oda::fail(ODA_ERR_SHAPE, "scale must be finite and > 0");
+  st = check_buffer("plan", plan, plan_bytes, z.plan_bytes);
+  if (st != ODA_OK) return st;
+  st = check_buffer("workspace", workspace, workspace_bytes, z.ws_bytes);
+  if (st != ODA_OK) return st;
+  PrefixArgs a;
+  a.q = in->q;
+  a.k_cache = in->k_cache;
+  a.v_cache = in->v_cache;
+  a.block_table = in->block_table;
+  a.k_cur = in->k_cur;
+  a.v_cur = in->v_cur;
+  a.plan = static_cast<const int32_t*>(plan);
+  a.out = out;
+  a.lse = lse;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + z.off_ml);
+  a.kv_layer_stride = shape->layer_stride_kv != 0
+                          ? shape->layer_stride_kv
+                          : shape->num_blocks * shape->num_kv_heads * kBlock * shape->head_dim;
+  a.num_blocks = shape->num_blocks;
+  a.L = shape->num_layers;
+  a.B = shape->batch;
+  a.T = groups->tokens;
+  a.Hq = shape->num_q_heads;
+  a.Hkv = shape->num_kv_heads;
+  a.G = z.group;
+  a.MB = shape->max_blocks_per_seq;
+  a.part_cols = z.part_cols;
+  a.max_items = z.max_items;
+  a.scale_log2 = in->scale * kLog2e;
+  return shape->head_dim == 128 ? launch_attention<128>(a, stream) : launch_attention<64>(a, stream);
+}

@@ -91,3 +91,55 @@ def test_commit_drafts_refusals(L, kw, status):
     assert status_of(L, lambda: L.commit_drafts(shape, a["T"], a["k"], a["v"], a["table"], a["seq"], a["kc"], a["vc"], None,
                                                 a["advance"], a["rows"], a["ws"], a["k_ring"], a["v_ring"], a["n_sink"],
                                                 a["window"], a["wb"], stream=0)) == status
+
+
+def _prefix_shape(L, **kw):
+    base = dict(num_layers=2, batch=3, num_q_heads=8, num_kv_heads=2, head_dim=128, max_blocks_per_seq=4, max_seq_len=64,
+                num_blocks=20)
+    base.update(kw)
+    return L.Shape(**base)
+
+
+def _prefix_groups(L, NG=2, T=4, start=0x1000, members=0x2000, blocks=0x3000):
+    return L.prefix_groups(NG, T, start, members, blocks)
+
+
+def test_prefix_sizes(L):
+    s, g = _prefix_shape(L), _prefix_groups(L)
+    plan, ws = L.prefix_plan_size(s, g), L.prefix_workspace_size(s, g)
+    assert plan % 256 == 0 and ws % 256 == 0
+    assert L.prefix_plan_size(_prefix_shape(L, batch=300), g) > plan
+    assert L.prefix_workspace_size(_prefix_shape(L, batch=300), g) > ws
+    for kw, gw, status in [(dict(batch=2049), {}, -3), (dict(head_dim=96), {}, -3), (dict(batch=0), {}, -2),
+                           (dict(split_blocks=2), {}, -2), (dict(num_q_heads=34), {}, -3), ({}, dict(T=0), -2),
+                           ({}, dict(T=17), -2), ({}, dict(NG=0), -2), ({}, dict(NG=2049), -2)]:
+        assert status_of(L, lambda: L.prefix_plan_size(_prefix_shape(L, **kw), _prefix_groups(L, **gw))) == status
+        assert status_of(L, lambda: L.prefix_workspace_size(_prefix_shape(L, **kw), _prefix_groups(L, **gw))) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(seq=None), -1), (dict(start=None), -1), (dict(members=None), -1), (dict(blocks=None), -1), (dict(kc=0x8000), -1),
+    (dict(plan=None), -4), (dict(short=1), -4), (dict(plan=0x200040), -4)])
+def test_prefix_plan_refusals(L, kw, status):
+    a = dict(seq=0x5000, start=0x1000, members=0x2000, blocks=0x3000, kc=None, plan=0x200000, short=0)
+    a.update(kw)
+    s, g = _prefix_shape(L), _prefix_groups(L, start=a["start"], members=a["members"], blocks=a["blocks"])
+    inp = L.inputs(None, None, None, None, a["seq"], 0.1, a["kc"], None)
+    n = L.prefix_plan_size(s, g) - a["short"]
+    assert status_of(L, lambda: L.prefix_plan(s, inp, g, a["plan"], n, stream=0)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), -1), (dict(k=None), -1), (dict(table=None), -1), (dict(out=None), -1), (dict(kc=0x8000), -1),
+    (dict(q=0x4008), -2), (dict(kc=0x8008, vc=0x9000), -2), (dict(scale=0.0), -2), (dict(scale=float("nan")), -2),
+    (dict(out=0xa004), -2), (dict(plan=None), -4), (dict(short_plan=1), -4), (dict(ws=None), -4), (dict(short=1), -4),
+    (dict(ws=0x300010), -4)])
+def test_prefix_attention_refusals(L, kw, status):
+    a = dict(q=0x4000, k=0x5000, v=0x6000, table=0x7000, kc=None, vc=None, scale=0.1, out=0xa000, plan=0x200000,
+             ws=0x300000, short=0, short_plan=0)
+    a.update(kw)
+    s, g = _prefix_shape(L), _prefix_groups(L)
+    inp = L.inputs(a["q"], a["k"], a["v"], a["table"], None, a["scale"], a["kc"], a["vc"])
+    pn, wn = L.prefix_plan_size(s, g) - a["short_plan"], L.prefix_workspace_size(s, g) - a["short"]
+    assert status_of(L, lambda: L.prefix_decode_attn(s, inp, g, a["plan"], a["out"], None, a["ws"], pn, wn,
+                                                     stream=0)) == status
