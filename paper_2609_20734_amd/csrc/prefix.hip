@@ -23,6 +23,7 @@
 #include <atomic>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "oda.h"
 #include "oda_internal.h"
@@ -401,198 +402,169 @@ __device__ __forceinline__ bool plan_fits(const PrefixArgs& a, const PlanHeader&
 
 __device__ __forceinline__ bf16x8 load16(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
 __device__ __forceinline__ u32x2 load8(const uint16_t* p) { return *reinterpret_cast<const u32x2*>(p); }
+// blocks of one request's own: read once per call
+__device__ __forceinline__ bf16x8 stream16(const uint16_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p));
+}
+__device__ __forceinline__ u32x2 stream8(const uint16_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+}
 __device__ __forceinline__ bf16x8 cat(u32x2 lo, u32x2 hi) {
   u32x4 t = {lo.x, lo.y, hi.x, hi.y};
   return __builtin_bit_cast(bf16x8, t);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
-__device__ __forceinline__ u32x2 mask_pack(u32x2 v, bool m0, bool m1, bool m2, bool m3) {
-  const uint32_t w0 = (m0 ? 0x0000FFFFu : 0u) | (m1 ? 0xFFFF0000u : 0u);
-  const uint32_t w1 = (m2 ? 0x0000FFFFu : 0u) | (m3 ? 0xFFFF0000u : 0u);
-  return u32x2{v.x & w0, v.y & w1};
-}
+// Register layouts of v_mfma_f32_16x16x32_bf16 and the cache layouts' fit with
+// them are those of the decode attention (attention.hip): a K block's 16-byte
+// groups are A operands of S^T, the scores come out as the A operand of P V, two
+// V blocks are its B.
 
-// One wavefront's blocks [lo, hi) against its column tiles.  Register layouts of
-// v_mfma_f32_16x16x32_bf16 and the cache layouts' fit with them are those of the
-// decode attention (attention.hip): a K block's 16-byte groups are A operands of
-// S^T, the scores come out as the A operand of P V, two V blocks are its B.
+// A wavefront's share of N column tiles: O = P V (rows: columns 4j..4j+3 of the
+// tile, 16 n + h16 the dimension), the reference of column h16's weights (a score
+// in log2 units, -infinity: none yet) and this lane's part of their sum.
 template <int D, int N>
 struct WaveState {
   f32x4 o[N][D / 16];
   float m[N], l[N];
-};
-
-template <int D, int N>
-__device__ __forceinline__ void stream_blocks(const PrefixArgs& a, const uint16_t* kbase, const uint16_t* vbase,
-                                              const int32_t* table, int lo, int hi, int limit, int lane,
-                                              const bf16x8 (&qf)[N][D / 32], WaveState<D, N>& w, int& bad) {
-  constexpr int KK = D / 32, NT = D / 16;
-  const int h16 = lane & 15, j = lane >> 4;
-  const int64_t blk_stride = (int64_t)a.Hkv * kBlock * D;
-  int tbl = 0;
-  for (int v = lo; v < hi; v += 2) {
-    if (((v - lo) & 63) == 0) {
-      const int e = v + lane < hi ? table[v + lane] : 0;
-      const bool ok = e >= 0 && e < a.num_blocks;
-      bad |= ok ? 0 : 1;
-      tbl = ok ? e : 0;
-    }
-    const int i0 = (v - lo) & 63;
-    const bool has1 = v + 1 < hi;
-    const int64_t pb0 = __builtin_amdgcn_readlane(tbl, i0);
-    const int64_t pb1 = has1 ? __builtin_amdgcn_readlane(tbl, i0 + 1) : pb0;
-    const uint16_t* k0 = kbase + pb0 * blk_stride;
-    const uint16_t* k1 = kbase + pb1 * blk_stride;
-    const uint16_t* v0 = vbase + pb0 * blk_stride;
-    const uint16_t* v1 = vbase + pb1 * blk_stride;
-    bf16x8 ka[KK], kb[KK];
-    u32x2 va[NT], vb[NT];
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      ka[kk] = load16(k0 + (kk * 64 + lane) * 8);
-      kb[kk] = load16(k1 + (kk * 64 + lane) * 8);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      va[n] = load8(v0 + (16 * n + h16) * kBlock + 4 * j);
-      vb[n] = load8(v1 + (16 * n + h16) * kBlock + 4 * j);
-    }
-    // positions past the limit, and the second block of an odd end
-    const int last = has1 ? limit : min(limit, (v + 1) * kBlock);
-    const bool whole = (v + 2) * kBlock <= last;
-    bool keep[8];
-    if (!whole) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        keep[i] = v * kBlock + 4 * j + i < last;
-        keep[4 + i] = (v + 1) * kBlock + 4 * j + i < last;
-      }
-      // unattended slots may hold anything (even NaN): zero them so 0 * V stays 0
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        va[n] = mask_pack(va[n], keep[0], keep[1], keep[2], keep[3]);
-        vb[n] = mask_pack(vb[n], keep[4], keep[5], keep[6], keep[7]);
-      }
-    }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+      m[c] = -INFINITY;
+      l[c] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kk], qf[c][kk], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[kk], qf[c][kk], s1, 0, 0, 0);
-      }
-      float sc[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[i] = s0[i] * a.scale_log2;
-        sc[4 + i] = s1[i] * a.scale_log2;
-      }
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sc[i] = keep[i] ? sc[i] : -INFINITY;
-      }
-      float mx = sc[0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sc[i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(w.m[c], mx);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = exp2_fast(w.m[c] - m_use);
-      w.m[c] = m_new;
-      float p[8], sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = exp2_fast(sc[i] - m_use);
-        sum += p[i];
-      }
-      w.l[c] = w.l[c] * alpha + sum;
-      if (__any(alpha != 1.f)) {
-        float al[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * j + i);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w.o[c][n][i] *= al[i];
-      }
-      // P in two bf16 parts, so that the product keeps 16 bits of it
-      bf16x8 phi, plo;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const __bf16 h = (__bf16)p[i];
-        phi[i] = h;
-        plo[i] = (__bf16)(p[i] - (float)h);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const bf16x8 vf = cat(va[n], vb[n]);
-        w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(phi, vf, w.o[c][n], 0, 0, 0);
-        w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(plo, vf, w.o[c][n], 0, 0, 0);
-      }
+      for (int n = 0; n < D / 16; ++n) o[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+  }
+};
+
+// The largest over the four lanes that share a column (h16 + 16 j).
+__device__ __forceinline__ float column_max(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Two floats to bf16, and what the rounding leaves of them.
+__device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+  x -= __uint_as_float(w << 16);
+  y -= __uint_as_float(w & 0xffff0000u);
+  return w;
+}
+
+// Scores of 32 positions of column h16 (this lane: 4j.. of either block) into the
+// online softmax; p comes back as kParts bf16 parts.  Two parts keep 16 bits of
+// each weight (rms error 2.4e-6 of a sum of random values), three all of them.
+//
+// Weights are taken against the column's reference, which need not be the largest
+// score so far: fp32 and bf16 hold weights up to 2^kHeadroom as well as those
+// below 1, and the reference's own position keeps the sum at 1 or more.  So the
+// largest score is looked for, and sums are rescaled, only where a weight passes
+// the headroom or a column has no reference yet (its weights come out infinite or
+// NaN): a third fewer vector operations per score than with the largest score of
+// every step.
+constexpr float kHeadroom = 1.0995116e12f;   // 2^40
+template <int D, int kParts>
+__device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, float scale, f32x4 (&o)[D / 16], float& m,
+                                             float& l, bf16x8 (&part)[kParts]) {
+  float p[8], sum;
+  auto weights = [&](float ref) {
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = exp2_fast(fmaf(i < 4 ? s0[i] : s1[i - 4], scale, -ref));
+      sum += p[i];
+    }
+  };
+  weights(m);
+  if (__any(!(sum <= kHeadroom))) {
+    float mx = s0[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, i < 4 ? s0[i] : s1[i - 4]);
+    const float m_new = fmaxf(m, column_max(mx) * scale);
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = exp2_fast(m - ref);
+    m = m_new;
+    l *= alpha;
+    const int j = (threadIdx.x & 63) >> 4;
+    float al[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) al[i] = __shfl(alpha, 4 * j + i);
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][i] *= al[i];
+    weights(ref);
+  }
+  l += sum;
+#pragma unroll
+  for (int q = 0; q < kParts; ++q) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = round_pair(p[2 * e], p[2 * e + 1]);
+    part[q] = __builtin_bit_cast(bf16x8, w);
   }
 }
 
-// LDS of an item: per wavefront m and l of its tiles, then one tile's O at a time.
-constexpr int lds_floats(int D) { return kWaves * kWaveTiles * kBlock * 2 + kWaves * kBlock * D; }
+// The last pair of an item may end early: positions from the limit on are not
+// attended, nor is the second block of an odd end.  Attended positions of the
+// pair whose first block is v:
+__device__ __forceinline__ int pair_positions(int v, bool has1, int limit) {
+  return (has1 ? limit : min(limit, (v + 1) * kBlock)) - v * kBlock;
+}
+// room: attended positions from the scores' first on.
+__device__ __forceinline__ void mask_scores(int room, f32x4& s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = i < room ? s[i] : -INFINITY;
+}
+// Unattended slots may hold anything (even NaN): zeroed so that 0 * V stays 0.
+__device__ __forceinline__ u32x2 mask_values(int room, u32x2 v) {
+  const uint32_t w0 = (room > 0 ? 0x0000FFFFu : 0u) | (room > 1 ? 0xFFFF0000u : 0u);
+  const uint32_t w1 = (room > 2 ? 0x0000FFFFu : 0u) | (room > 3 ? 0xFFFF0000u : 0u);
+  return u32x2{v.x & w0, v.y & w1};
+}
 
-// The item's wavefront grid: WC column positions (of N tiles each) by 8 / WC
-// position ranges.
+// The queries of a wavefront's column tiles as B operands.
 template <int D, int N>
-__device__ __forceinline__ void run_item(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int wc_shift,
-                                         float* smem) {
-  constexpr int KK = D / 32, NT = D / 16;
-  const int lane = threadIdx.x & 63;
-  const int wave = uniform(threadIdx.x >> 6);
-  const int h16 = lane & 15, j = lane >> 4;
-  const int WC = 1 << wc_shift, WP = kWaves >> wc_shift;
-  const int wc = wave & (WC - 1), wp = wave >> wc_shift;
-  const int pairs = (it.blk_hi - it.blk_lo + 1) >> 1;
-  const int per = (pairs + WP - 1) / WP;
-  const int lo = min(it.blk_hi, it.blk_lo + 2 * per * wp);
-  const int hi = min(it.blk_hi, lo + 2 * per);
-
-  WaveState<D, N> w;
+__device__ __forceinline__ void load_queries(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int tile0,
+                                             bf16x8 (&qf)[N][D / 32]) {
+  const int lane = threadIdx.x & 63, h16 = lane & 15, j = lane >> 4;
 #pragma unroll
   for (int c = 0; c < N; ++c) {
-    w.m[c] = -INFINITY;
-    w.l[c] = 0.f;
+    const int col = (tile0 + c) * kBlock + h16;
+    const bool in = col < it.ncols;
+    const int at = in ? it.col0 + col : it.col0;
+    const int row = at / a.G, h = at - row * a.G;
+    const uint16_t* q = a.q + (((int64_t)l * a.B * a.T + rows[it.row0 + row].id) * a.Hq + g * a.G + h) * D;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) w.o[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kk = 0; kk < D / 32; ++kk) qf[c][kk] = in ? load16(q + 32 * kk + 8 * j) : bf16x8{};
   }
-  const int tile0 = wc * N;
-  if (lo < hi && tile0 * kBlock < it.ncols) {
-    bf16x8 qf[N][KK];
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const int col = (tile0 + c) * kBlock + h16;
-      const bool in = col < it.ncols;
-      const int at = in ? it.col0 + col : it.col0;
-      const int row = at / a.G, h = at - row * a.G;
-      const uint16_t* q = a.q + (((int64_t)l * a.B * a.T + rows[it.row0 + row].id) * a.Hq + g * a.G + h) * D;
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[c][kk] = in ? load16(q + 32 * kk + 8 * j) : bf16x8{};
-    }
-    const int64_t base = (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * D;
-    int bad = 0;
-    stream_blocks<D, N>(a, a.k_cache + base, a.v_cache + base, a.block_table + (int64_t)it.request * a.MB, lo, hi, it.limit,
-                        lane, qf, w, bad);
-    const bool any_bad = __any(bad);
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      w.l[c] += __shfl_xor(w.l[c], 16);
-      w.l[c] += __shfl_xor(w.l[c], 32);
-      if (any_bad) w.m[c] = w.l[c] = __builtin_nanf("");   // a table entry out of range: these rows become NaN
-    }
-  }
+}
 
-  // join the position ranges, one tile of every column position at a time
-  float* sm_m = smem;                                    // [waves][N][16]
-  float* sm_l = smem + kWaves * kWaveTiles * kBlock;
-  float* sm_o = smem + 2 * kWaves * kWaveTiles * kBlock; // [waves][16][D]
+// LDS: the staged blocks of wide items (two stages), or one O tile per wavefront
+// where position ranges are joined; then m and l per wavefront and column.
+constexpr int kStagePairs = 4;
+__host__ __device__ constexpr int block_bytes(int D) { return kBlock * D * 2; }      // of K, of V
+__host__ __device__ constexpr int stage_bytes(int D) { return 2 * kStagePairs * 2 * block_bytes(D); }
+__host__ __device__ constexpr int lds_bytes(int D) { return 2 * stage_bytes(D) + 2 * kWaves * kWaveTiles * kBlock * 4 + 16; }
+static_assert(2 * 2 * kStagePairs * 2 * kBlock * 2 >= kWaves * kBlock * 4, "a tile of O per wavefront fits the stages");
+static_assert(2 * kStagePairs == kWaves, "a wavefront stages one block of K and one of V");
+
+// Joins the position ranges (WP of them; wavefront = range * WC + column position)
+// of N tiles per column position and writes the partials.
+template <int D, int N>
+__device__ __forceinline__ void join(const PrefixArgs& a, const Item& it, int l, int g, int wc_shift, WaveState<D, N>& w,
+                                     char* smem) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int h16 = lane & 15, j = lane >> 4;
+  const int WC = 1 << wc_shift, WP = kWaves >> wc_shift;
+  float* sm_o = reinterpret_cast<float*>(smem);                          // [waves][16][D]
+  float* sm_m = reinterpret_cast<float*>(smem + 2 * stage_bytes(D));     // [waves][N][16]
+  float* sm_l = sm_m + kWaves * kWaveTiles * kBlock;
   if (j == 0) {
 #pragma unroll
     for (int c = 0; c < N; ++c) {
@@ -608,7 +580,7 @@ __device__ __forceinline__ void run_item(const PrefixArgs& a, const Item& it, co
     for (int i = 0; i < 4; ++i) {
       float* dst = sm_o + (wave * kBlock + 4 * j + i) * D + h16;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) dst[16 * n] = w.o[c][n][i];
+      for (int n = 0; n < D / 16; ++n) dst[16 * n] = w.o[c][n][i];
     }
     __syncthreads();
     for (int e = threadIdx.x; e < WC * kBlock * D / 2; e += kThreads) {
@@ -633,10 +605,258 @@ __device__ __forceinline__ void run_item(const PrefixArgs& a, const Item& it, co
   }
 }
 
+// The sums of a column's four lanes; NaN where a table entry was out of range.
+template <int D, int N>
+__device__ __forceinline__ void finish(WaveState<D, N>& w, bool bad) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    w.l[c] += __shfl_xor(w.l[c], 16);
+    w.l[c] += __shfl_xor(w.l[c], 32);
+    if (bad) w.m[c] = w.l[c] = __builtin_nanf("");
+  }
+}
+
+// Narrow items (one or two column tiles): the wavefronts take contiguous position
+// ranges, K and V go straight to registers.
+template <int D, int N>
+__device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, char* smem) {
+  constexpr int KK = D / 32, NT = D / 16, kParts = 3;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int h16 = lane & 15, j = lane >> 4;
+  const int pairs = (it.blk_hi - it.blk_lo + 1) >> 1;
+  const int per = (pairs + kWaves - 1) / kWaves;
+  const int lo = min(it.blk_hi, it.blk_lo + 2 * per * wave);
+  const int hi = min(it.blk_hi, lo + 2 * per);
+  WaveState<D, N> w;
+  w.clear();
+  if (lo < hi) {
+    const int64_t base = (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * D;
+    const uint16_t* kbase = a.k_cache + base + lane * 8;
+    const uint16_t* vbase = a.v_cache + base + h16 * kBlock + 4 * j;
+    const int32_t* table = a.block_table + (int64_t)it.request * a.MB;
+    const int64_t blk_stride = (int64_t)a.Hkv * kBlock * D;
+    bf16x8 qf[N][KK];
+    load_queries<D, N>(a, it, rows, l, g, 0, qf);
+    int tbl = 0, bad = 0;
+    auto pair = [&](int v, auto masked) {
+      constexpr bool kMasked = decltype(masked)::value;
+      const int i0 = (v - lo) & 63;
+      if (i0 == 0) {
+        const int e = v + lane < hi ? table[v + lane] : 0;
+        const bool ok = e >= 0 && e < a.num_blocks;
+        bad |= ok ? 0 : 1;
+        tbl = ok ? e : 0;
+      }
+      const bool has1 = !kMasked || v + 1 < hi;
+      const int64_t pb0 = (int64_t)__builtin_amdgcn_readlane(tbl, i0) * blk_stride;
+      const int64_t pb1 = has1 ? (int64_t)__builtin_amdgcn_readlane(tbl, i0 + 1) * blk_stride : pb0;
+      bf16x8 ka[KK], kb[KK];
+      u32x2 va[NT], vb[NT];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        ka[kk] = stream16(kbase + pb0 + kk * 512);
+        kb[kk] = stream16(kbase + pb1 + kk * 512);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        va[n] = stream8(vbase + pb0 + n * kBlock * kBlock);
+        vb[n] = stream8(vbase + pb1 + n * kBlock * kBlock);
+      }
+      const int room = kMasked ? pair_positions(v, has1, it.limit) - 4 * j : 0;
+      if (kMasked) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          va[n] = mask_values(room, va[n]);
+          vb[n] = mask_values(room - kBlock, vb[n]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kk], qf[c][kk], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[kk], qf[c][kk], s1, 0, 0, 0);
+        }
+        if (kMasked) {
+          mask_scores(room, s0);
+          mask_scores(room - kBlock, s1);
+        }
+        bf16x8 part[kParts];
+        softmax_tile<D, kParts>(s0, s1, a.scale_log2, w.o[c], w.m[c], w.l[c], part);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const bf16x8 vf = cat(va[n], vb[n]);
+#pragma unroll
+          for (int q = 0; q < kParts; ++q)
+            w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[q], vf, w.o[c][n], 0, 0, 0);
+        }
+      }
+    };
+    int v = lo;
+    for (; v + 2 <= hi && (v + 2) * kBlock <= it.limit; v += 2) pair(v, std::false_type{});
+    if (v < hi) pair(v, std::true_type{});
+    finish<D, N>(w, __any(bad));
+  }
+  join<D, N>(a, it, l, g, 0, w, smem);
+}
+
+// Wide items: K and V are staged through LDS once for all column tiles, eight
+// blocks a stage (wavefront i brings block i while the stage before it is used),
+// with the positions of K ordered so that operand reads are free of bank
+// conflicts.  Up to four tiles: two position ranges, which share a stage's pairs alternately;
+// more: every wavefront goes through all pairs with its N tiles.
+template <int D, int N>
+__device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int wc_shift,
+                                         char* smem) {
+  constexpr int KK = D / 32, NT = D / 16, kParts = N == 1 ? 3 : 2;
+  constexpr int kLoads = block_bytes(D) / 1024;      // 16-byte loads of a block per lane
+  constexpr int kElems = kBlock * D;                 // of a block
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int h16 = lane & 15, j = lane >> 4;
+  const int WP = kWaves >> wc_shift;
+  const int wc = wave & ((1 << wc_shift) - 1), wp = wave >> wc_shift;
+  int& s_bad = *reinterpret_cast<int*>(smem + lds_bytes(D) - 16);
+  if (threadIdx.x == 0) s_bad = 0;
+  const bool active = wc * N * kBlock < it.ncols;
+  WaveState<D, N> w;
+  w.clear();
+  bf16x8 qf[N][KK];
+  load_queries<D, N>(a, it, rows, l, g, wc * N, qf);
+
+  const int64_t base = (int64_t)l * a.kv_layer_stride + (int64_t)g * kElems;
+  // staged slot lane % 16 of a 16-position row of K holds position (bits 0, 1, 3, 2 of the slot)
+  const int k_lane = ((lane & 48) | (lane & 3) | ((lane & 4) << 1) | ((lane & 8) >> 1)) * 8;
+  const int32_t* table = a.block_table + (int64_t)it.request * a.MB + it.blk_lo + wave;
+  const int64_t blk_stride = (int64_t)a.Hkv * kElems;
+  const int blocks = it.blk_hi - it.blk_lo;
+  const int stages = (blocks + kWaves - 1) / kWaves;
+  int tbl = 0, bad = 0;
+  bf16x8 kr[kLoads], vr[kLoads];
+  // a stage's block of this wavefront; past the end the cache's first (masked, and zeroed where V is used)
+  auto fetch = [&](int st) {
+    if ((st & 63) == 0) {
+      const int e = (st + lane) * kWaves + wave < blocks ? table[(st + lane) * kWaves] : 0;
+      const bool ok = e >= 0 && e < a.num_blocks;
+      bad |= ok ? 0 : 1;
+      tbl = ok ? e : 0;
+    }
+    const int64_t pb = (int64_t)__builtin_amdgcn_readlane(tbl, st & 63) * blk_stride + base;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      kr[i] = load16(a.k_cache + pb + k_lane + i * 512);
+      vr[i] = load16(a.v_cache + pb + lane * 8 + i * 512);
+    }
+  };
+  uint16_t* lds = reinterpret_cast<uint16_t*>(smem);
+  auto put = [&](int st) {      // stage: K blocks, then V blocks
+    uint16_t* dst = lds + (st & 1) * (stage_bytes(D) / 2) + wave * kElems + lane * 8;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      *reinterpret_cast<bf16x8*>(dst + i * 512) = kr[i];
+      *reinterpret_cast<bf16x8*>(dst + kWaves * kElems + i * 512) = vr[i];
+    }
+  };
+  // One pair of staged blocks against the N tiles.  Row 4a + i of the first score
+  // tile is position 8a + i of the pair's 32, of the second 8a + 4 + i, so that lane
+  // j's scores are eight neighbours and V comes in one 16-byte read; the staged
+  // slots put the first tile's rows of a block in front of the second's.
+  const int k_at = (h16 >> 3) * kElems + (j * kBlock + (h16 & 7)) * 8;
+  const int v_at = (kWaves + (j >> 1)) * kElems + h16 * kBlock + 8 * (j & 1);
+  auto pair = [&](const uint16_t* k0, const uint16_t* v0, int room, auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;
+    f32x4 s0[N], s1[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) s0[c] = s1[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const bf16x8 ka = load16(k0 + kk * 512), kb = load16(k0 + kk * 512 + 8 * 8);
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        s0[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[c][kk], s0[c], 0, 0, 0);
+        s1[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qf[c][kk], s1[c], 0, 0, 0);
+      }
+    }
+    bf16x8 part[N][kParts];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      if (kMasked) {
+        mask_scores(room, s0[c]);
+        mask_scores(room - 4, s1[c]);
+      }
+      softmax_tile<D, kParts>(s0[c], s1[c], a.scale_log2, w.o[c], w.m[c], w.l[c], part[c]);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      bf16x8 vf = load16(v0 + n * kBlock * kBlock);
+      if (kMasked) {
+        const u32x4 q = __builtin_bit_cast(u32x4, vf);
+        vf = cat(mask_values(room, u32x2{q.x, q.y}), mask_values(room - 4, u32x2{q.z, q.w}));
+      }
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int q = 0; q < kParts; ++q)
+          w.o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[c][q], vf, w.o[c][n], 0, 0, 0);
+    }
+  };
+  fetch(0);
+  put(0);
+  if (stages > 1) fetch(1);
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    if (active) {
+      const uint16_t* stage = lds + (st & 1) * (stage_bytes(D) / 2);
+      for (int pr = wp; pr < kStagePairs; pr += WP) {
+        const int v = it.blk_lo + st * kWaves + 2 * pr;
+        if (v >= it.blk_hi) break;
+        if (v + 2 > it.blk_hi || (v + 2) * kBlock > it.limit) break;   // the last pair, below
+        pair(stage + k_at + 2 * pr * kElems, stage + v_at + 2 * pr * kElems, 0, std::false_type{});
+      }
+    }
+    // the other buffer was last read before the barrier that ended the stage before
+    if (st + 1 < stages) {
+      put(st + 1);
+      if (st + 2 < stages) fetch(st + 2);
+    }
+    __syncthreads();
+  }
+  // a last pair that ends early, still staged: its range's wavefronts
+  const int v_last = it.blk_lo + (blocks - 1) / 2 * 2, pr_last = (blocks - 1) / 2 % kStagePairs;
+  if (active && (pr_last & (WP - 1)) == wp && (v_last + 2 > it.blk_hi || (v_last + 2) * kBlock > it.limit)) {
+    const uint16_t* stage = lds + ((stages - 1) & 1) * (stage_bytes(D) / 2);
+    pair(stage + k_at + 2 * pr_last * kElems, stage + v_at + 2 * pr_last * kElems,
+         pair_positions(v_last, v_last + 1 < it.blk_hi, it.limit) - 8 * j, std::true_type{});
+  }
+  if (bad) s_bad = 1;
+  __syncthreads();
+  finish<D, N>(w, s_bad != 0);
+  if (wc_shift != 3) {
+    join<D, N>(a, it, l, g, wc_shift, w, smem);
+    return;
+  }
+  // one position range: the partials straight from the registers
+  const int64_t part0 = ((int64_t)(l * a.Hkv + g)) * a.part_cols + it.part;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    const int col0 = (wc * N + c) * kBlock;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (col0 + 4 * j + i >= it.ncols) continue;
+      float* dst = a.part_o + (part0 + col0 + 4 * j + i) * D + h16;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) dst[16 * n] = w.o[c][n][i];
+    }
+    if (j == 0 && col0 + h16 < it.ncols)
+      *reinterpret_cast<float2*>(a.part_ml + (part0 + col0 + h16) * 2) =
+          make_float2(w.m[c], w.l[c]);
+  }
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void prefix_split_kernel(PrefixArgs a) {
-  extern __shared__ float smem[];
+  extern __shared__ __attribute__((aligned(16))) char smem[];
   const PlanHeader& h = *reinterpret_cast<const PlanHeader*>(a.plan);
   const int units = a.L * a.Hkv;
   const int i = blockIdx.x / units, u = blockIdx.x - i * units;
@@ -645,27 +865,28 @@ void prefix_split_kernel(PrefixArgs a) {
   const Item it = reinterpret_cast<const Item*>(a.plan + items_at(a.B * a.T))[i];
   const int l = u / a.Hkv, g = u - l * a.Hkv;
   const int tiles = (it.ncols + kBlock - 1) / kBlock;
-  if (tiles == 1) run_item<D, 1>(a, it, rows, l, g, 0, smem);
-  else run_item<D, kWaveTiles>(a, it, rows, l, g, tiles <= 2 ? 0 : tiles <= 4 ? 1 : tiles <= 8 ? 2 : 3, smem);
+  if (tiles == 1) run_narrow<D, 1>(a, it, rows, l, g, smem);
+  else if (tiles == 2) run_narrow<D, 2>(a, it, rows, l, g, smem);
+  else if (tiles <= kWaves) run_wide<D, 1>(a, it, rows, l, g, tiles <= 4 ? 2 : 3, smem);
+  else run_wide<D, 2>(a, it, rows, l, g, 3, smem);
 }
 
-// Running softmax state of a lane's output elements.
-template <int PD>
-struct Acc {
-  float m = -INFINITY, l = 0.f, o[PD] = {};
-  __device__ __forceinline__ void add(float pm, float pl, const float (&po)[PD]) {
-    const float M = fmaxf(m, pm);
-    const float Mu = M == -INFINITY ? 0.f : M;
-    const float r = exp2_fast(m - Mu), s = exp2_fast(pm - Mu);
-    l = l * r + s * pl;
+__device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
-    for (int e = 0; e < PD; ++e) o[e] = o[e] * r + s * po[e];
-    m = M;
-  }
-};
+  for (int s = 32; s >= 1; s >>= 1) x += __shfl_xor(x, s);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
+  return x;
+}
 
 // One wavefront per (layer, row, query head): the prefix's partials, the own
-// blocks' partials, then the current tokens up to the row's own.
+// blocks' partials, then the current tokens up to the row's own.  The weights of
+// up to 64 partials are formed side by side, one per lane, and the partials read
+// kMergeLoads at a time.
+constexpr int kMergeLoads = 8;
 template <int D>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
   constexpr int PD = D / 64;
@@ -700,24 +921,60 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
   const Row row = rows[r];
   const int g = head / a.G, hh = head - g * a.G;
   const int64_t part0 = (int64_t)(l * a.Hkv + g) * a.part_cols + hh;
-  Acc<PD> acc;
-  for (int k = 0; k < 2; ++k) {
-    const int64_t part = part0 + (k == 0 ? row.pre_part : row.own_part);
-    const int splits = k == 0 ? row.pre_splits : row.own_splits, stride = k == 0 ? row.pre_stride : row.own_stride;
-    for (int s = 0; s < splits; ++s) {
-      const int64_t c = part + (int64_t)s * stride;
-      float po[PD];
-#pragma unroll
-      for (int e = 0; e < PD; ++e) po[e] = a.part_o[c * D + lane * PD + e];
-      acc.add(a.part_ml[c * 2], a.part_ml[c * 2 + 1], po);
-    }
-  }
-  // the current tokens this row attends: candidates, or the cache's last positions
   const int b = (int)(id / a.T), t = (int)(id - (int64_t)b * a.T);
-  const int more = a.k_cur ? t + 1 : t;
   float q[PD];
 #pragma unroll
   for (int e = 0; e < PD; ++e) q[e] = bf16_to_float(a.q[(((int64_t)l * all + id) * a.Hq + head) * D + lane * PD + e]);
+
+  float M = -INFINITY, sum = 0.f, o[PD] = {};
+  // weights against a new largest logit
+  auto rescale = [&](float m) {
+    const float top = fmaxf(M, m);
+    const float s = M == -INFINITY ? 0.f : exp2_fast(M - top);
+    sum *= s;
+#pragma unroll
+    for (int e = 0; e < PD; ++e) o[e] *= s;
+    M = top;
+  };
+  const int splits = row.pre_splits + row.own_splits;
+  auto column = [&](int s) {
+    return part0 + (s < row.pre_splits ? row.pre_part + (int64_t)s * row.pre_stride
+                                       : row.own_part + (int64_t)(s - row.pre_splits) * row.own_stride);
+  };
+  for (int s0 = 0; s0 < splits; s0 += 64) {
+    const int n = min(64, splits - s0);
+    float m = -INFINITY, part = 0.f;
+    if (lane < n) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + column(s0 + lane) * 2);
+      m = ml.x;
+      part = ml.y;
+    }
+    float po[kMergeLoads][PD];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < kMergeLoads; ++k) {
+        const float* p = a.part_o + column(s0 + min(k0 + k, n - 1)) * D + lane * PD;
+#pragma unroll
+        for (int e = 0; e < PD; ++e) po[k][e] = p[e];
+      }
+    };
+    load(0);
+    rescale(wave_max(m));
+    const float w = exp2_fast(m - (M == -INFINITY ? 0.f : M));    // NaN of a bad entry stays
+    sum += wave_sum(lane < n ? w * part : 0.f);
+    for (int k0 = 0; k0 < n; k0 += kMergeLoads) {
+      if (k0 > 0) load(k0);
+#pragma unroll
+      for (int k = 0; k < kMergeLoads; ++k) {
+        const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), (k0 + k) & 63));
+        if (k0 + k < n)
+#pragma unroll
+          for (int e = 0; e < PD; ++e) o[e] += wk * po[k][e];
+      }
+    }
+  }
+  // the current tokens this row attends: candidates, or the cache's last positions
+  const int more = a.k_cur ? t + 1 : t;
   bool bad = false;
   for (int i = 0; i < more; ++i) {
     float kd[PD], vd[PD];
@@ -746,15 +1003,17 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
     float dot = 0.f;
 #pragma unroll
     for (int e = 0; e < PD; ++e) dot += q[e] * kd[e];
+    dot = wave_sum(dot) * a.scale_log2;
+    rescale(dot);
+    const float w = exp2_fast(dot - (M == -INFINITY ? 0.f : M));
+    sum += w;
 #pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
-    dot *= a.scale_log2;
-    acc.add(dot, 1.f, vd);
+    for (int e = 0; e < PD; ++e) o[e] += w * vd[e];
   }
-  if (bad) acc.l = __builtin_nanf("");
+  if (bad) sum = __builtin_nanf("");
 #pragma unroll
-  for (int e = 0; e < PD; ++e) out[e] = acc.o[e] / acc.l;
-  if (lse && lane == 0) *lse = (acc.m + __log2f(acc.l)) * kLn2;
+  for (int e = 0; e < PD; ++e) out[e] = o[e] / sum;
+  if (lse && lane == 0) *lse = (M + __log2f(sum)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------
@@ -823,7 +1082,7 @@ oda_status launch_attention(const PrefixArgs& a, hipStream_t stream) {
   const int64_t items = (int64_t)a.max_items * a.L * a.Hkv;
   const int64_t merges = oda::ceil_div((int64_t)a.L * a.B * a.T * a.Hq, 4);
   if (items > INT_MAX || merges > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "grid too large");
-  const int lds = lds_floats(D) * 4;
+  const int lds = lds_bytes(D);
   static std::atomic<uint64_t> raised{0};
   raise_lds_limit(reinterpret_cast<const void*>(prefix_split_kernel<D>), &raised, lds);
   (void)hipGetLastError();
