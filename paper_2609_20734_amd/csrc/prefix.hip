@@ -99,210 +99,253 @@ struct PlanArgs {
 // which one CU's share of HBM delivers it: a tile's products and softmax take
 // about an eighth of that, so up to eight tiles are free.
 constexpr float kBlockCost = 8.f;
-constexpr float kItemCost = 80.f;       // start-up, the join and the partial's share of the merge
+constexpr float kItemCost = 160.f;      // start-up, the join and the partial's share of the merge
 constexpr float kLeastCost = 16 * kBlockCost;   // shortest split: two blocks per wavefront
 
-__device__ __forceinline__ float block_cost(int cols) { return fmaxf(kBlockCost, (float)((cols + kBlock - 1) / kBlock)); }
-
-// Splits of a piece of `blocks` blocks for items of cost t, and their length.
-__device__ __forceinline__ int split_count(int blocks, float cost, float t) {
-  return blocks <= 0 ? 0 : max(1, (int)ceilf((float)blocks * cost / t));
-}
-__device__ __forceinline__ int split_length(int blocks, int splits) {
-  return splits <= 0 ? 2 : ((blocks + splits - 1) / splits + 1) & ~1;
-}
-
-// Exclusive sums of x over the workgroup's threads, and the total.
-__device__ __forceinline__ int block_scan(int x, int* s_wave, int& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int v = x;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int y = __shfl_up(v, s);
-    if (lane >= s) v += y;
-  }
-  __syncthreads();
-  if (lane == 63) s_wave[wave] = v;
-  __syncthreads();
-  int base = 0;
-  total = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) base += s_wave[w];
-    total += s_wave[w];
-  }
-  return base + v - x;
-}
-
+// What the plan holds in LDS per slot (place in `members`), per group and per
+// piece of work (the groups' prefixes, then the slots' own blocks).
 struct PlanSlot {
   int32_t request;      // -1: not attended
   int32_t tokens;       // rows (0: none)
   int32_t len;          // positions common to the request's rows
   int32_t row;          // first row
   int32_t group;
-  int32_t blocks;       // own blocks
-  int32_t splits;
-  int32_t part;
 };
 struct PlanGroup {
   int32_t start;        // first slot
   int32_t blocks;       // of the prefix; -1: outside the table
-  int32_t leader;       // first slot whose table is read (INT_MAX: none)
+  int32_t leader;       // first slot with rows, whose table is read (INT_MAX: none)
   int32_t row, rows;
-  int32_t splits;       // per chunk
-  int32_t part;
-  int32_t reserved;
+  int32_t chunks;       // items side by side that hold its columns
 };
+struct PlanPiece {
+  float cost;           // of one chunk of columns over all blocks (0: no work)
+  int32_t splits, item, part;
+};
+static_assert(kMaxBatch * (sizeof(PlanSlot) + sizeof(PlanGroup) + 2 * sizeof(PlanPiece)) < 158 * 1024, "the plan fits LDS");
 __host__ __device__ constexpr size_t plan_lds(int B, int NG) {
-  return (size_t)B * sizeof(PlanSlot) + (size_t)(NG + 1) * sizeof(PlanGroup);
+  return (size_t)B * sizeof(PlanSlot) + (size_t)(NG + 1) * sizeof(PlanGroup) + (size_t)(B + NG) * sizeof(PlanPiece);
 }
 
+__device__ __forceinline__ float piece_cost(int blocks, int cols) {
+  return blocks <= 0 ? 0.f : (float)blocks * fmaxf(kBlockCost, (float)((cols + kBlock - 1) / kBlock));
+}
+// Splits of a piece where an item may cost 1 / inv.
+__device__ __forceinline__ int split_count(float cost, float inv) { return cost > 0.f ? max(1, (int)ceilf(cost * inv)) : 0; }
+// Blocks per split: even, as blocks are taken in pairs.
+__device__ __forceinline__ int split_length(int blocks, int splits) { return ((blocks + splits - 1) / splits + 1) & ~1; }
+
+// Exclusive sums of (x, y) over the workgroup's threads, and the totals.
+__device__ __forceinline__ int2 block_scan(int2 x, int2* s_wave, int2& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int2 v = x;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int a = __shfl_up(v.x, s), b = __shfl_up(v.y, s);
+    if (lane >= s) {
+      v.x += a;
+      v.y += b;
+    }
+  }
+  __syncthreads();       // the sums of the call before have been read
+  if (lane == 63) s_wave[wave] = v;
+  __syncthreads();
+  int2 base = make_int2(0, 0);
+  total = make_int2(0, 0);
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    const int2 t = s_wave[w];
+    if (w < wave) {
+      base.x += t.x;
+      base.y += t.y;
+    }
+    total.x += t.x;
+    total.y += t.y;
+  }
+  return make_int2(base.x + v.x - x.x, base.y + v.y - x.y);
+}
+
+// One workgroup.  Bound by latency: the arrays are asked for together, then the
+// phases go through LDS.
 __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   PlanSlot* slots = reinterpret_cast<PlanSlot*>(lds);
-  PlanGroup* groups = reinterpret_cast<PlanGroup*>(lds + (size_t)a.B * sizeof(PlanSlot));
-  __shared__ int s_wave[kPlanThreads / 64];
-  __shared__ int s_best;
-  const int tid = threadIdx.x, lane = tid & 63;
+  PlanGroup* groups = reinterpret_cast<PlanGroup*>(slots + a.B);
+  PlanPiece* pieces = reinterpret_cast<PlanPiece*>(groups + a.NG + 1);
+  __shared__ int2 s_wave[kPlanThreads / 64];
+  __shared__ float s_sum[kPlanThreads / 64], s_most[kPlanThreads / 64];
+  __shared__ int s_count[kPlanThreads / 64][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   PlanHeader* head = reinterpret_cast<PlanHeader*>(a.plan);
   Row* rows = reinterpret_cast<Row*>(a.plan + rows_at());
   Item* items = reinterpret_cast<Item*>(a.plan + items_at(a.B * a.T));
 
+  // the first round of members comes with the group arrays
+  int member = tid < a.B ? a.members[tid] : -1;
   // group starts, kept in [0, B] and ascending whatever the array holds
-  for (int j = tid; j <= a.NG; j += kPlanThreads) {
-    groups[j].start = min(max(a.group_start[j], 0), a.B);
-    groups[j].leader = INT_MAX;
-    groups[j].blocks = j < a.NG ? a.prefix_blocks[j] : 0;
-    if (groups[j].blocks > a.MB) groups[j].blocks = -1;
+  int carry = 0;
+  for (int j0 = 0; j0 <= a.NG; j0 += 64) {
+    const int j = j0 + lane;
+    int start = j <= a.NG ? min(max(a.group_start[j], 0), a.B) : 0;
+    const int blocks = j < a.NG ? a.prefix_blocks[j] : 0;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int y = __shfl_up(start, s);
+      if (lane >= s) start = max(start, y);
+    }
+    start = max(start, carry);
+    carry = __shfl(start, 63);
+    if (wave == 0 && j <= a.NG) {
+      groups[j].start = start;
+      groups[j].leader = INT_MAX;
+      groups[j].blocks = blocks <= a.MB ? blocks : -1;
+    }
   }
-  __syncthreads();
-  if (tid == 0)
-    for (int j = 1; j <= a.NG; ++j) groups[j].start = max(groups[j].start, groups[j - 1].start);
   __syncthreads();
   const int first = groups[0].start, count = groups[a.NG].start;
 
-  // slots: who attends what; rows in slot order, those that become NaN last
+  // slots: who attends what; rows in slot order, those that become NaN from the
+  // table's end
   int n_rows = 0, n_bad = 0;
-  for (int s0 = first; s0 < count; s0 += kPlanThreads) {
+  for (int s0 = 0; s0 < count; s0 += kPlanThreads) {
     const int s = s0 + tid;
     PlanSlot p{};
     p.request = -1;
     bool bad = false;
     if (s < count) {
-      int lo = 0, hi = a.NG;          // the last group that starts at or before s and is not empty there
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (groups[mid].start <= s) lo = mid;
-        else hi = mid;
-      }
-      p.group = lo;
-      const int b = a.members[s];
-      if (b >= 0 && b < a.B && (a.flags == nullptr || a.flags[b] != 0)) {
-        p.tokens = a.n_tokens ? min(max(a.n_tokens[b], 0), a.T) : a.T;
-        const int n = a.seq_lens[b], pre = groups[lo].blocks;
+      const int b = s0 == 0 ? member : a.members[s];
+      if (s >= first && b >= 0 && b < a.B) {
+        const int n = a.seq_lens[b], tokens = a.n_tokens ? a.n_tokens[b] : a.T, flag = a.flags ? a.flags[b] : 1;
+        int lo = 0, hi = a.NG;        // the last group that starts at or before s
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (groups[mid].start <= s) lo = mid;
+          else hi = mid;
+        }
+        const int pre = groups[lo].blocks;
+        p.group = lo;
         p.request = b;
+        p.tokens = flag != 0 ? min(max(tokens, 0), a.T) : 0;
         p.len = a.cached ? n : n - 1;
-        bad = n < 1 || n > a.max_len || pre < 0 || p.len / kBlock < pre ||
-              (a.cached && p.tokens > 0 && n > a.max_len - (p.tokens - 1));
-        p.blocks = bad ? 0 : (p.len + kBlock - 1) / kBlock - pre;
+        bad = p.tokens > 0 && (n < 1 || n > a.max_len || pre < 0 || p.len / kBlock < pre ||
+                               (a.cached && n > a.max_len - (p.tokens - 1)));
         if (!bad && p.tokens > 0) atomicMin(&groups[lo].leader, s);
       }
     }
-    int total = 0;
-    const int at = block_scan(bad ? 0 : p.tokens, s_wave, total);
-    p.row = n_rows + at;
-    n_rows += total;
-    if (s < count) slots[s] = p;
-    // NaN rows fill the table from its end
-    const int bad_at = block_scan(bad ? p.tokens : 0, s_wave, total);
-    if (bad)
+    int2 total;
+    const int2 at = block_scan(bad ? make_int2(0, p.tokens) : make_int2(p.tokens, 0), s_wave, total);
+    if (bad) {
       for (int t = 0; t < p.tokens; ++t) {
         Row r{};
         r.id = p.request * a.T + t;
-        rows[a.B * a.T - 1 - (n_bad + bad_at + t)] = r;
+        rows[a.B * a.T - 1 - (n_bad + at.y + t)] = r;
       }
-    if (bad && s < count) slots[s].tokens = 0;
-    n_bad += total;
-  }
-  __syncthreads();
-  for (int j = tid; j < a.NG; j += kPlanThreads) {
-    const int s0 = groups[j].start, s1 = groups[j + 1].start;
-    groups[j].row = s0 < count ? slots[s0].row : n_rows;
-    groups[j].rows = (s1 < count ? slots[s1].row : n_rows) - groups[j].row;
-    if (groups[j].rows == 0) groups[j].blocks = 0;
+      p.tokens = 0;
+    }
+    p.row = n_rows + at.x;
+    n_rows += total.x;
+    n_bad += total.y;
+    if (s < count) slots[s] = p;
   }
   __syncthreads();
 
-  // the cost of a split: each lane of the first wavefront tries one
-  if (tid < 64) {
-    float most = kLeastCost, sum = 0.f;
-    for (int j = 0; j < a.NG; ++j) {
-      const int cols = min(groups[j].rows * a.G, a.chunk_cols);
-      const float c = (float)groups[j].blocks * block_cost(cols);
-      most = fmaxf(most, c);
-      sum += c * (float)((groups[j].rows * a.G + a.chunk_cols - 1) / a.chunk_cols);
+  // pieces and their costs
+  const auto own_blocks = [&](const PlanSlot& p) { return (p.len + kBlock - 1) / kBlock - groups[p.group].blocks; };
+  float sum = 0.f, most = kLeastCost;
+  const int n_pieces = a.NG + count;
+  for (int i = tid; i < n_pieces; i += kPlanThreads) {
+    PlanPiece p{};
+    int chunks = 1;
+    if (i < a.NG) {
+      const int s0 = groups[i].start, s1 = groups[i + 1].start;
+      const int row = s0 < count ? slots[s0].row : n_rows;
+      const int n = (s1 < count ? slots[s1].row : n_rows) - row;
+      groups[i].row = row;
+      groups[i].rows = n;
+      groups[i].chunks = chunks = (n * a.G + a.chunk_cols - 1) / a.chunk_cols;
+      p.cost = n > 0 ? piece_cost(groups[i].blocks, min(n * a.G, a.chunk_cols)) : 0.f;
+    } else if (slots[i - a.NG].tokens > 0) {
+      p.cost = piece_cost(own_blocks(slots[i - a.NG]), slots[i - a.NG].tokens * a.G);
     }
-    for (int s = first; s < count; ++s) {
-      const float c = slots[s].tokens > 0 ? (float)slots[s].blocks * block_cost(slots[s].tokens * a.G) : 0.f;
-      most = fmaxf(most, c);
-      sum += c;
-    }
-    const float t = lane == 63 ? most : kLeastCost * exp2f(log2f(most / kLeastCost) * (float)lane / 63.f);
-    int n = 0, pieces = 0;
-    for (int j = 0; j < a.NG; ++j) {
-      const int chunks = (groups[j].rows * a.G + a.chunk_cols - 1) / a.chunk_cols;
-      n += chunks * split_count(groups[j].blocks, block_cost(min(groups[j].rows * a.G, a.chunk_cols)), t);
-      pieces += groups[j].blocks > 0 ? chunks : 0;
-    }
-    for (int s = first; s < count; ++s) {
-      if (slots[s].tokens <= 0) continue;
-      n += split_count(slots[s].blocks, block_cost(slots[s].tokens * a.G), t);
-      pieces += slots[s].blocks > 0 ? 1 : 0;
-    }
-    float est = (float)a.units * n <= (float)kCus
-                    ? t + kItemCost
-                    : (float)a.units * (sum + (float)n * kItemCost) / (float)kCus + 0.5f * t;
-    if (n - pieces > a.extra_items) est = INFINITY;
-    float best = est;
+    most = fmaxf(most, p.cost);
+    sum += p.cost * (float)chunks;
+    pieces[i] = p;
+  }
 #pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
-    const uint64_t who = __ballot(est == best);
-    const int at = who ? 63 - __builtin_clzll(who) : 63;
-    const float chosen = __shfl(t, at);
-    if (lane == 0) s_best = __float_as_int(chosen);
+  for (int s = 32; s >= 1; s >>= 1) {
+    sum += __shfl_xor(sum, s);
+    most = fmaxf(most, __shfl_xor(most, s));
+  }
+  if (lane == 0) {
+    s_sum[wave] = sum;
+    s_most[wave] = most;
   }
   __syncthreads();
-  const float t = __int_as_float(s_best);
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    sum += s_sum[w];
+    most = fmaxf(most, s_most[w]);
+  }
 
-  // items of the prefixes, then of the requests' own blocks; partial columns alike
+  // what an item may cost: every lane tries one value; the last, with a margin for
+  // rounding, splits nothing
+  const float t = lane == 63 ? most : kLeastCost * __builtin_amdgcn_exp2f(__log2f(most / kLeastCost) * (float)lane * (1.f / 63.f));
+  const float inv = 0.999f / t;
+  int n = 0;
+#pragma unroll 4
+  for (int i = wave; i < n_pieces; i += kPlanThreads / 64) {
+    n += split_count(pieces[i].cost, inv) * (i < a.NG ? groups[i].chunks : 1);
+  }
+  s_count[wave][lane] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) n += s_count[w][lane];
+  const int least = __shfl(n, 63);
+  float est = (float)a.units * n <= (float)kCus
+                  ? t + kItemCost
+                  : (float)a.units * (sum + (float)n * kItemCost) * (1.f / (float)kCus) + 0.5f * t;
+  if (n - least > a.extra_items) est = INFINITY;
+  float best = est;
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
+  const uint64_t who = __ballot(est == best);
+  const float inv_best = __shfl(inv, who ? 63 - __builtin_clzll(who) : 63);
+
+  // splits, items and partial columns
   int n_items = 0, n_part = 0;
-  for (int j0 = 0; j0 < a.NG; j0 += kPlanThreads) {
-    const int j = j0 + tid;
-    int splits = 0, chunks = 0, cols = 0;
-    if (j < a.NG) {
-      cols = groups[j].rows * a.G;
-      chunks = (cols + a.chunk_cols - 1) / a.chunk_cols;
-      splits = split_count(groups[j].blocks, block_cost(min(cols, a.chunk_cols)), t);
-      if (splits > 0) splits = (groups[j].blocks + split_length(groups[j].blocks, splits) - 1) / split_length(groups[j].blocks, splits);
+  for (int i0 = 0; i0 < n_pieces; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    int splits = 0, cols = 0, chunks = 0;
+    if (i < n_pieces) {
+      chunks = i < a.NG ? groups[i].chunks : 1;
+      splits = split_count(pieces[i].cost, inv_best);
+      cols = (i < a.NG ? groups[i].rows : slots[i - a.NG].tokens) * a.G;
+      if (splits > 0) {
+        const int blocks = i < a.NG ? groups[i].blocks : own_blocks(slots[i - a.NG]);
+        const int length = split_length(blocks, splits);
+        splits = (blocks + length - 1) / length;
+      }
     }
-    int total = 0;
-    const int part = n_part + block_scan(cols * splits, s_wave, total);
-    n_part += total;
-    const int item = n_items + block_scan(chunks * splits, s_wave, total);
-    n_items += total;
-    if (j < a.NG) {
-      groups[j].splits = splits;
-      groups[j].part = part;
-      groups[j].reserved = item;
+    int2 total;
+    const int2 at = block_scan(make_int2(chunks * splits, cols * splits), s_wave, total);
+    if (i < n_pieces) {
+      pieces[i].splits = splits;
+      pieces[i].item = n_items + at.x;
+      pieces[i].part = n_part + at.y;
     }
+    n_items += total.x;
+    n_part += total.y;
   }
   __syncthreads();
   for (int j = 0; j < a.NG; ++j) {
+    const PlanPiece p = pieces[j];
+    if (p.splits == 0) continue;
     const PlanGroup g = groups[j];
-    if (g.splits == 0) continue;
-    const int cols = g.rows * a.G, chunks = (cols + a.chunk_cols - 1) / a.chunk_cols;
-    const int length = split_length(g.blocks, g.splits);
-    for (int i = tid; i < chunks * g.splits; i += kPlanThreads) {
-      const int split = i / chunks, c = i - split * chunks;     // the chunks of a range next to each other
+    const int cols = g.rows * a.G, length = split_length(g.blocks, p.splits);
+    for (int i = tid; i < g.chunks * p.splits; i += kPlanThreads) {
+      const int split = i / g.chunks, c = i - split * g.chunks;     // the chunks of a range next to each other
       Item it;
       it.row0 = g.row;
       it.col0 = c * a.chunk_cols;
@@ -311,48 +354,40 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
       it.blk_lo = split * length;
       it.blk_hi = min(g.blocks, it.blk_lo + length);
       it.limit = g.blocks * kBlock;
-      it.part = g.part + it.col0 * g.splits + split * it.ncols;
-      items[g.reserved + i] = it;
+      it.part = p.part + it.col0 * p.splits + split * it.ncols;
+      items[p.item + i] = it;
     }
   }
-  for (int s0 = first; s0 < count; s0 += kPlanThreads) {
-    const int s = s0 + tid;
-    PlanSlot p{};
-    if (s < count) p = slots[s];
-    const int cols = p.tokens * a.G;
-    int splits = cols > 0 ? split_count(p.blocks, block_cost(cols), t) : 0;
-    const int length = split_length(p.blocks, splits);
-    if (splits > 0) splits = (p.blocks + length - 1) / length;
-    int total = 0;
-    const int part = n_part + block_scan(cols * splits, s_wave, total);
-    n_part += total;
-    const int item = n_items + block_scan(splits, s_wave, total);
-    n_items += total;
-    if (cols <= 0) continue;
+  for (int s = first + tid; s < count; s += kPlanThreads) {
+    const PlanSlot p = slots[s];
+    if (p.tokens <= 0) continue;
     const PlanGroup g = groups[p.group];
-    for (int i = 0; i < splits; ++i) {
+    const PlanPiece pre = pieces[p.group], own = pieces[a.NG + s];
+    const int cols = p.tokens * a.G;
+    const int blocks = own_blocks(p), length = own.splits > 0 ? split_length(blocks, own.splits) : 0;
+    for (int i = 0; i < own.splits; ++i) {
       Item it;
       it.row0 = p.row;
       it.col0 = 0;
       it.ncols = cols;
       it.request = p.request;
       it.blk_lo = g.blocks + i * length;
-      it.blk_hi = min(g.blocks + p.blocks, it.blk_lo + length);
+      it.blk_hi = min(g.blocks + blocks, it.blk_lo + length);
       it.limit = p.len;
-      it.part = part + i * cols;
-      items[item + i] = it;
+      it.part = own.part + i * cols;
+      items[own.item + i] = it;
     }
     for (int k = 0; k < p.tokens; ++k) {
       Row r;
       r.id = p.request * a.T + k;
       r.len = p.len;
       const int col = (p.row + k - g.row) * a.G, chunk = col / a.chunk_cols * a.chunk_cols;
-      r.pre_splits = g.splits;
+      r.pre_splits = pre.splits;
       r.pre_stride = min(a.chunk_cols, g.rows * a.G - chunk);
-      r.pre_part = g.part + chunk * g.splits + (col - chunk);
-      r.own_splits = splits;
+      r.pre_part = pre.part + chunk * pre.splits + (col - chunk);
+      r.own_splits = own.splits;
       r.own_stride = cols;
-      r.own_part = part + k * a.G;
+      r.own_part = own.part + k * a.G;
       rows[p.row + k] = r;
     }
   }
