@@ -18,6 +18,7 @@ constexpr int kBlock = 16;
 constexpr int kThreads = 256;
 constexpr int kTargetGroups = 256;   // workgroups the launch aims for (one per CU)
 constexpr int kMaxTokens = 64;       // candidates per request of one commit
+constexpr int kDraftGroups = 4096;   // workgroups a commit of several tokens aims for
 
 struct CommitArgs {
   uint16_t* k_cache;
@@ -113,7 +114,8 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 // n - 2 + count.  Work split and ticket as in commit_kernel.  K: one 16-byte
 // store per (unit, 8 dims, token), the tokens of a block next to each other;
 // V: a thread walks the tokens of one dim, whose slots are neighbours in the
-// block's [D][16] row.
+// block's [D][16] row.  Bound by partly written lines (a token is 2 of a V row's
+// 32 bytes), so the launch has as many wavefronts as the chip holds.
 struct CommitDraftsArgs {
   uint16_t* k_cache;
   uint16_t* v_cache;
@@ -169,24 +171,45 @@ __global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArg
     const int e = i / count, t = i - e * count;
     const int u = u0 + e / groups, d8 = e % groups;
     const int l = u / a.Hkv, g = u - l * a.Hkv;
+    const u32x4 k8 = *reinterpret_cast<const u32x4*>(a.k_cand + ((((int64_t)l * a.B + b) * a.T + t) * a.Hkv + g) * a.D + d8 * 8);
     const Slot s = slot_of(a, b, pos0 + t, last);
     if (s.blk < 0) continue;
-    const u32x4 k8 = *reinterpret_cast<const u32x4*>(a.k_cand + ((((int64_t)l * a.B + b) * a.T + t) * a.Hkv + g) * a.D + d8 * 8);
     const int64_t in = ((int64_t)d8 * kBlock + s.at) * 8;
     *reinterpret_cast<u32x4*>(a.k_cache + (int64_t)l * a.kv_layer_stride + (s.blk * a.Hkv + g) * kBlock * a.D + in) = k8;
     if (s.ring >= 0)
       *reinterpret_cast<u32x4*>(a.k_ring + ((((int64_t)l * a.B + b) * nr + s.ring) * a.Hkv + g) * kBlock * a.D + in) = k8;
   }
+  // (the tokens' values of a dim are loaded four at a time, stored two at a time
+  // where they share a word)
+  const int64_t v_step = (int64_t)a.Hkv * a.D;
   for (int i = threadIdx.x; i < nu * a.D; i += kThreads) {
     const int u = u0 + i / a.D, d = i % a.D;
     const int l = u / a.Hkv, g = u - l * a.Hkv;
-    for (int t = 0; t < count; ++t) {
-      const Slot s = slot_of(a, b, pos0 + t, last);
-      if (s.blk < 0) continue;
-      const uint16_t v1 = a.v_cand[((((int64_t)l * a.B + b) * a.T + t) * a.Hkv + g) * a.D + d];
-      const int64_t in = (int64_t)d * kBlock + s.at;
-      a.v_cache[(int64_t)l * a.kv_layer_stride + (s.blk * a.Hkv + g) * kBlock * a.D + in] = v1;
-      if (s.ring >= 0) a.v_ring[((((int64_t)l * a.B + b) * nr + s.ring) * a.Hkv + g) * kBlock * a.D + in] = v1;
+    const uint16_t* src = a.v_cand + (((int64_t)l * a.B + b) * a.T * a.Hkv + g) * a.D + d;
+    uint16_t* cache = a.v_cache + (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * a.D + d * kBlock;
+    uint16_t* ring = a.v_ring + ((int64_t)l * a.B + b) * nr * a.Hkv * kBlock * a.D + (int64_t)g * kBlock * a.D + d * kBlock;
+    for (int t0 = 0; t0 < count; t0 += 4) {
+      uint16_t v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = src[min(t0 + k, count - 1) * v_step];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int t = t0 + k;
+        if (t >= count) break;
+        const Slot s = slot_of(a, b, pos0 + t, last);
+        const bool second = k > 0 && (s.at & 1) != 0;      // already stored with the token before
+        if (s.blk < 0 || second) continue;
+        const bool two = k < 3 && (s.at & 1) == 0 && t + 1 < count;   // (neighbours of one block)
+        const uint32_t w = (uint32_t)v[k] | (uint32_t)v[k < 3 ? k + 1 : k] << 16;
+        uint16_t* p = cache + s.blk * v_step * kBlock + s.at;
+        if (two) *reinterpret_cast<uint32_t*>(p) = w;
+        else *p = v[k];
+        if (s.ring >= 0) {
+          uint16_t* r = ring + s.ring * v_step * kBlock + s.at;
+          if (two) *reinterpret_cast<uint32_t*>(r) = w;
+          else *r = v[k];
+        }
+      }
     }
   }
   if (a.tickets == nullptr) return;
@@ -373,7 +396,7 @@ extern "C" oda_status oda_commit_drafts(const oda_attn_shape* shape, int32_t tok
   a.ring_sb = rg.sink_blocks;
   a.ring_rb = rg.ring_blocks;
   const int64_t units = (int64_t)a.L * a.Hkv;
-  const int64_t want = std::min<int64_t>(units, oda::ceil_div(kTargetGroups, a.B));
+  const int64_t want = std::min<int64_t>(units, oda::ceil_div(kDraftGroups, a.B));
   a.units_per_chunk = (int)oda::ceil_div(units, want);
   a.chunks = (int)oda::ceil_div(units, a.units_per_chunk);
   const int64_t groups = (int64_t)a.B * a.chunks;
