@@ -16,9 +16,7 @@
 // Weights and sums are fp64: the next token has to be the one whose interval
 // holds u_K, and a vocabulary of 150,000 tokens has so many borders that fp32
 // sums (2^-24 of the whole per border) would put about one draw in a hundred on
-// the other side of one.  The exponential costs 20 fp64 operations a logit,
-// 13 us of the chip's fp64 rate for 160 rows of 151,936 logits, beside 20 us of
-// reading them.
+// the other side of one.  The exponential costs 18 fp64 operations a logit.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -36,6 +34,7 @@ constexpr int kPer = 16;                     // logits a thread holds at a time
 constexpr int kTile = kThreads * kPer;
 constexpr int kMaxSplits = 64;               // splits of a row: one per lane where they are joined
 constexpr int kMaxDrafts = 63;
+constexpr double kLog2e = 1.4426950408889634074;
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // rows start anywhere
 
@@ -80,39 +79,46 @@ __device__ __forceinline__ double temperature_of(const VerifyArgs& a, int b) {
   return a.temperature ? (double)a.temperature[b] : 1.0;
 }
 
-// exp(x) for x <= 0, by 2^k e^r with |r| <= ln(2) / 2 and the Taylor series to
-// r^13 (the next term is below 2^-57); 0 from -708 on, where results would be
-// subnormal, and for NaN.
-__device__ __forceinline__ double exp_neg(double x) {
-  const double k = rint(x * 1.4426950408889634074);
-  double r = fma(k, -0.69314718055994528623, x);        // ln(2) in two parts
-  r = fma(k, -2.3190468138462995584e-17, r);
-  double p = 1.0 / 6227020800.0;
-  p = fma(p, r, 1.0 / 479001600.0);
-  p = fma(p, r, 1.0 / 39916800.0);
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return x > -708.0 ? ldexp(p, (int)k) : 0.0;
+// 2^y for y <= 0 (NaN: 0), by 2^k 2^f with |f| <= 1/2 and the Taylor series of
+// e^(f ln 2) to the eleventh power (the next term is below 2^-47 of the value).
+// Below 2^-1022 it runs out into subnormals and 0.
+__device__ __forceinline__ double exp2_neg(double y) {
+  y = fmax(y, -1100.0);
+  const double k = rint(y), f = y - k;
+  constexpr double c = 0.69314718055994530942;
+  constexpr double c2 = c * c, c3 = c2 * c, c4 = c2 * c2, c5 = c4 * c, c6 = c4 * c2, c7 = c4 * c3, c8 = c4 * c4, c9 = c8 * c,
+                   c10 = c8 * c2, c11 = c8 * c3;
+  double p = c11 / 39916800.0;
+  p = fma(p, f, c10 / 3628800.0);
+  p = fma(p, f, c9 / 362880.0);
+  p = fma(p, f, c8 / 40320.0);
+  p = fma(p, f, c7 / 5040.0);
+  p = fma(p, f, c6 / 720.0);
+  p = fma(p, f, c5 / 120.0);
+  p = fma(p, f, c4 / 24.0);
+  p = fma(p, f, c3 / 6.0);
+  p = fma(p, f, c2 / 2.0);
+  p = fma(p, f, c);
+  p = fma(p, f, 1.0);
+  return ldexp(p, (int)k);
 }
 
-// Weight of logit z in a row whose largest is `top` (above -infinity): 1 at the
-// largest itself, an infinite one too.
-__device__ __forceinline__ double weight(float z, float top, double inv_t) {
-  return z == top ? 1.0 : exp_neg(((double)z - (double)top) * inv_t);
+// Weights of a row's logits against `top`, its largest (above -infinity): slope =
+// log2(e) / temperature.  (The difference first: a logit may be the type's lowest
+// value, whose product is off by more than the whole range.)  Where the largest is
+// +infinity it alone weighs.
+struct Weights {
+  double slope, top;
+};
+__device__ __forceinline__ Weights weights_against(float top, double slope) { return Weights{slope, (double)top}; }
+__device__ __forceinline__ double weight(const Weights& w, float z) {
+  if (w.top == (double)INFINITY) return z == INFINITY ? 1.0 : 0.0;
+  return exp2_neg(((double)z - w.top) * w.slope);
 }
 // The same for a split's or thread's largest logit against a row's, 0 where it
 // holds nothing.
-__device__ __forceinline__ double rescale(float m, float top, double inv_t) {
-  return m == -INFINITY ? 0.0 : weight(m, top, inv_t);
+__device__ __forceinline__ double rescale(float m, float top, double slope) {
+  return m == -INFINITY ? 0.0 : m == top ? 1.0 : exp2_neg(((double)m - (double)top) * slope);
 }
 
 // kPer logits of a split from v on, -infinity past its end.
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
   if (!selected_request(a, blockIdx.z, b) || i > drafts_of(a, b)) return;
   const double t = temperature_of(a, b);
   const bool greedy = !(t > 0.0);
-  const double inv_t = greedy ? 0.0 : 1.0 / t;
+  const double slope = greedy ? 0.0 : kLog2e / t;
   const float* row = a.logits + ((int64_t)b * (a.K + 1) + i) * a.V;
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -178,9 +184,10 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
         for (int e = kPer - 1; e >= 0; --e)
           if (z[e] == m) first = v0 + ((e / 4) * kThreads + tid) * 4 + e % 4;
     } else {
-      if (m > top) sum *= rescale(top, m, inv_t);
+      if (m > top) sum *= rescale(top, m, slope);
+      const Weights w = weights_against(m, slope);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) sum += weight(z[e], m, inv_t);
+      for (int e = 0; e < kPer; ++e) sum += weight(w, z[e]);
     }
     top = m;
   }
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
     const int f = wave_min(top == all && all != -INFINITY ? first : INT_MAX);
     if (lane == 0) s_first[wave] = f;
   } else {
-    const double s = wave_sum(all == -INFINITY ? 0.0 : sum * rescale(top, all, inv_t));
+    const double s = wave_sum(all == -INFINITY ? 0.0 : sum * rescale(top, all, slope));
     if (lane == 0) s_sum[wave] = s;
   }
   __syncthreads();
@@ -218,7 +225,7 @@ struct RowStat {
   double part;      // of this lane's split
   int first;        // greedy: the first index of the largest
 };
-__device__ __forceinline__ RowStat join_row(const VerifyArgs& a, int b, int i, int lane, bool greedy, double inv_t) {
+__device__ __forceinline__ RowStat join_row(const VerifyArgs& a, int b, int i, int lane, bool greedy, double slope) {
   SplitStat s;
   s.top = -INFINITY;
   s.sum = 0.0;
@@ -226,7 +233,7 @@ __device__ __forceinline__ RowStat join_row(const VerifyArgs& a, int b, int i, i
   if (lane < a.splits) s = a.stats[((int64_t)b * (a.K + 1) + i) * a.splits + lane];
   RowStat r;
   r.top = wave_max(s.top);
-  r.part = r.top == -INFINITY || greedy ? 0.0 : s.sum * rescale(s.top, r.top, inv_t);
+  r.part = r.top == -INFINITY || greedy ? 0.0 : s.sum * rescale(s.top, r.top, slope);
   r.sum = wave_sum(r.part);
   r.first = greedy ? wave_min(s.top == r.top ? s.first : INT_MAX) : INT_MAX;
   return r;
@@ -238,14 +245,14 @@ struct Draw {
   const float* q;       // the draft's probabilities, or NULL
   int skip;             // a draft that was not drawn: its own weight is 0 (-1: none)
   bool residual;
-  float top;
-  double inv_t, scale;  // scale: 1 / the row's sum
+  Weights w;
+  double scale;         // 1 / the row's sum
 };
-__device__ __forceinline__ double draw_weight(const Draw& d, float z, int v) {
-  double w = weight(z, d.top, d.inv_t);
+__device__ __forceinline__ double draw_weight(const Draw& d, float z, float q, int v) {
+  double w = weight(d.w, z);
   if (!d.residual) return w;
   w *= d.scale;
-  if (d.q != nullptr) return fmax(w - (double)fmaxf(d.q[v], 0.f), 0.0);
+  if (d.q != nullptr) return fmax(w - (double)fmaxf(q, 0.f), 0.0);
   return v == d.skip ? 0.0 : w;
 }
 
@@ -259,45 +266,77 @@ __device__ __forceinline__ double wave_scan(double x, int lane) {
   return x;
 }
 
+// The weights of kPer neighbouring tokens from v on (0 past the end).
+__device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (&w)[kPer]) {
+  float z[kPer], q[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; e += 4) {
+    if (v + e + 4 <= end) {
+      const f32x4u t = *reinterpret_cast<const f32x4u*>(d.row + v + e);
+      z[e] = t[0], z[e + 1] = t[1], z[e + 2] = t[2], z[e + 3] = t[3];
+    } else {
+#pragma unroll
+      for (int k = e; k < e + 4; ++k) z[k] = v + k < end ? d.row[v + k] : -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) q[e] = 0.f;
+  if (d.residual && d.q != nullptr) {
+#pragma unroll
+    for (int e = 0; e < kPer; e += 4) {
+      if (v + e + 4 <= end) {
+        const f32x4u t = *reinterpret_cast<const f32x4u*>(d.q + v + e);
+        q[e] = t[0], q[e + 1] = t[1], q[e + 2] = t[2], q[e + 3] = t[3];
+      } else {
+#pragma unroll
+        for (int k = e; k < e + 4; ++k) q[k] = v + k < end ? d.q[v + k] : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) w[e] = draw_weight(d, z[e], q[e], v + e);
+}
+
 // The first token of the split whose cumulative weight, with `below` in front of
 // the split, exceeds `goal`; else its last token with a weight (INT_MAX: none).
-// Threads take contiguous runs, so their sums are in the tokens' order.
+// Threads take kPer neighbours each, so their sums are in the tokens' order.
 __device__ __forceinline__ int find_token(const Draw& d, int begin, int end, double below, double goal, double* s_scan,
                                           int* s_hit) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int run = (end - begin + kThreads - 1) / kThreads;
-  const int v0 = min(end, begin + tid * run), v1 = min(end, v0 + run);
-  double sum = 0.0;
-  int last = -1;
-  for (int v = v0; v < v1; ++v) {
-    const double w = draw_weight(d, d.row[v], v);
-    sum += w;
-    if (w > 0.0) last = v;
-  }
-  const double upto = wave_scan(sum, lane);
-  if (lane == 63) s_scan[wave] = upto;
   if (tid == 0) {
     s_hit[0] = INT_MAX;
     s_hit[1] = -1;
   }
-  __syncthreads();
-  double base = below;
-  for (int w = 0; w < wave; ++w) base += s_scan[w];
-  if (last >= 0) {
-    atomicMax(&s_hit[1], last);
-    if (base + upto > goal) {
-      double c = base + (upto - sum);
-      int hit = INT_MAX;
-      for (int v = v0; v < v1; ++v) {
-        const double w = draw_weight(d, d.row[v], v);
-        c += w;
-        if (w > 0.0 && c > goal) {
-          hit = v;
-          break;
+  for (int v0 = begin; v0 < end; v0 += kTile) {
+    const int v = v0 + tid * kPer;
+    double w[kPer], sum = 0.0;
+    draw_run(d, v, end, w);
+    int last = -1;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      sum += w[e];
+      if (w[e] > 0.0) last = v + e;
+    }
+    const double upto = wave_scan(sum, lane);
+    __syncthreads();          // the tile before has been summed up; s_hit is set
+    if (lane == 63) s_scan[wave] = upto;
+    __syncthreads();
+    double base = below;
+    for (int k = 0; k < wave; ++k) base += s_scan[k];
+    for (int k = 0; k < kThreads / 64; ++k) below += s_scan[k];
+    if (last >= 0) {
+      atomicMax(&s_hit[1], last);
+      if (base + upto > goal) {
+        double c = base + (upto - sum);
+        int hit = INT_MAX;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          c += w[e];
+          if (hit == INT_MAX && w[e] > 0.0 && c > goal) hit = v + e;
         }
+        // a thread whose sum passes the goal only by rounding takes its last
+        atomicMin(&s_hit[0], hit == INT_MAX ? last : hit);
       }
-      // a thread whose own sum passes the goal only by rounding takes its last
-      atomicMin(&s_hit[0], hit == INT_MAX ? last : hit);
     }
   }
   __syncthreads();
@@ -331,23 +370,23 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const double t = temperature_of(a, b);
   const bool greedy = !(t > 0.0);
-  const double inv_t = greedy ? 0.0 : 1.0 / t;
+  const double slope = greedy ? 0.0 : kLog2e / t;
   const int n = drafts_of(a, b);
   const float* u = a.uniform + (int64_t)b * (a.K + 1);
 
   // every row's splits joined, every draft decided (by each workgroup alike)
   for (int i = wave; i <= n; i += kWaves) {
-    const RowStat r = join_row(a, b, i, lane, greedy, inv_t);
+    // the draft's own logit and probability come beside the splits
+    const int x = i < n ? uniform(a.draft_tokens[(int64_t)b * a.K + i]) : -1;
+    const bool known = x >= 0 && x < a.V;
+    const float z = known ? a.logits[((int64_t)b * (a.K + 1) + i) * a.V + x] : 0.f;
+    const float qx = known && a.draft_probs ? a.draft_probs[((int64_t)b * a.K + i) * a.V + x] : 1.f;
+    const RowStat r = join_row(a, b, i, lane, greedy, slope);
     if (lane != 0) continue;
     int ok = 0;
-    if (i < n) {
-      const int x = a.draft_tokens[(int64_t)b * a.K + i];
-      if (x >= 0 && x < a.V && r.top != -INFINITY) {
-        const double q = a.draft_probs ? (double)fmaxf(a.draft_probs[((int64_t)b * a.K + i) * a.V + x], 0.f) : 1.0;
-        const float z = a.logits[((int64_t)b * (a.K + 1) + i) * a.V + x];
-        const double p = greedy ? (x == r.first ? 1.0 : 0.0) : weight(z, r.top, inv_t) / r.sum;
-        ok = (double)u[i] * q < p ? 1 : 0;
-      }
+    if (known && r.top != -INFINITY) {
+      const double p = greedy ? (x == r.first ? 1.0 : 0.0) : weight(weights_against(r.top, slope), z) / r.sum;
+      ok = (double)u[i] * (double)fmaxf(qx, 0.f) < p ? 1 : 0;
     }
     s_ok[i] = ok;
     s_top[i] = r.top;
@@ -364,8 +403,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   d.residual = refused && !greedy;
   d.q = d.residual && a.draft_probs ? a.draft_probs + ((int64_t)b * a.K + j) * a.V : nullptr;
   d.skip = d.residual && !a.draft_probs ? a.draft_tokens[(int64_t)b * a.K + j] : -1;
-  d.top = top;
-  d.inv_t = inv_t;
+  d.w = weights_against(top, slope);
   d.scale = 1.0 / s_sum[j];
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
 
@@ -373,13 +411,10 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   if (summed) {
     double sum = 0.0;
     for (int v0 = begin; v0 < end; v0 += kTile) {
-      float z[kPer];
-      load_tile(d.row, v0, end, tid, z);
+      double w[kPer];
+      draw_run(d, v0 + tid * kPer, end, w);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const int v = v0 + ((e / 4) * kThreads + tid) * 4 + e % 4;
-        if (v < end) sum += draw_weight(d, z[e], v);
-      }
+      for (int e = 0; e < kPer; ++e) sum += w[e];
     }
     sum = wave_sum(sum);
     if (lane == 0) s_scan[wave] = sum;
@@ -415,7 +450,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         all = wave_sum(part);
         from_p = !(all > 0.0);
       }
-      if (from_p) part = join_row(a, b, j, lane, false, inv_t).part;
+      if (from_p) part = join_row(a, b, j, lane, false, slope).part;
       const double upto = wave_scan(part, lane);
       const double goal = (double)u[a.K] * __shfl(upto, 63);
       const uint64_t past = __ballot(upto > goal && part > 0.0);
