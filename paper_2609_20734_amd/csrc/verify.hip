@@ -29,8 +29,8 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPer = 16;                     // logits a thread holds at a time
+constexpr int kThreads = 512;
+constexpr int kPer = 8;                      // logits a thread holds at a time
 constexpr int kTile = kThreads * kPer;
 constexpr int kMaxSplits = 64;               // splits of a row: one per lane where they are joined
 constexpr int kMaxDrafts = 63;
@@ -111,9 +111,11 @@ struct Weights {
   double slope, top;
 };
 __device__ __forceinline__ Weights weights_against(float top, double slope) { return Weights{slope, (double)top}; }
-__device__ __forceinline__ double weight(const Weights& w, float z) {
-  if (w.top == (double)INFINITY) return z == INFINITY ? 1.0 : 0.0;
+__device__ __forceinline__ double finite_weight(const Weights& w, float z) {
   return exp2_neg(((double)z - w.top) * w.slope);
+}
+__device__ __forceinline__ double weight(const Weights& w, float z) {
+  return w.top == (double)INFINITY ? (z == INFINITY ? 1.0 : 0.0) : finite_weight(w, z);
 }
 // The same for a split's or thread's largest logit against a row's, 0 where it
 // holds nothing.
@@ -185,9 +187,14 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
           if (z[e] == m) first = v0 + ((e / 4) * kThreads + tid) * 4 + e % 4;
     } else {
       if (m > top) sum *= rescale(top, m, slope);
-      const Weights w = weights_against(m, slope);
+      if (m == INFINITY) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) sum += weight(w, z[e]);
+        for (int e = 0; e < kPer; ++e) sum += z[e] == INFINITY ? 1.0 : 0.0;
+      } else {
+        const Weights w = weights_against(m, slope);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum += finite_weight(w, z[e]);
+      }
     }
     top = m;
   }
@@ -248,13 +255,6 @@ struct Draw {
   Weights w;
   double scale;         // 1 / the row's sum
 };
-__device__ __forceinline__ double draw_weight(const Draw& d, float z, float q, int v) {
-  double w = weight(d.w, z);
-  if (!d.residual) return w;
-  w *= d.scale;
-  if (d.q != nullptr) return fmax(w - (double)fmaxf(q, 0.f), 0.0);
-  return v == d.skip ? 0.0 : w;
-}
 
 // Inclusive sums over the lanes.
 __device__ __forceinline__ double wave_scan(double x, int lane) {
@@ -293,8 +293,21 @@ __device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (
       }
     }
   }
+  if (d.w.top == (double)INFINITY) {
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) w[e] = draw_weight(d, z[e], q[e], v + e);
+    for (int e = 0; e < kPer; ++e) w[e] = z[e] == INFINITY ? 1.0 : 0.0;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) w[e] = finite_weight(d.w, z[e]);
+  }
+  if (d.residual) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      w[e] *= d.scale;
+      if (d.q != nullptr) w[e] = fmax(w[e] - (double)fmaxf(q[e], 0.f), 0.0);
+      else w[e] = v + e == d.skip ? 0.0 : w[e];
+    }
+  }
 }
 
 // The first token of the split whose cumulative weight, with `below` in front of
