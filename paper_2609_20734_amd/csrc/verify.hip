@@ -22,6 +22,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 
 #include "oda.h"
@@ -34,6 +35,8 @@ constexpr int kPer = 8;                      // logits a thread holds at a time
 constexpr int kTile = kThreads * kPer;
 constexpr int kMaxSplits = 64;               // splits of a row: one per lane where they are joined
 constexpr int kMaxDrafts = 63;
+constexpr int kStatGroups = 2048;            // workgroups the launches aim for
+constexpr int kDrawGroups = 768;
 constexpr double kLog2e = 1.4426950408889634074;
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // rows start anywhere
@@ -58,9 +61,11 @@ struct VerifyArgs {
   const int32_t* work_list;
   const int32_t* n_work;
   SplitStat* stats;       // [B][K + 1][splits]
-  double* sums;           // [B][splits]: weights of the row that the next token is drawn from
+  double* sums;           // [B][kMaxSplits]: weights of the row that the next token is drawn from
   uint32_t* tickets;      // [B], zero between calls
-  int32_t B, K, V, splits, chunk;
+  int32_t B, K, V;
+  int32_t splits, chunk;            // of a row in the first launch
+  int32_t draw_splits, draw_chunk;  // of a refused row in the second
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -75,44 +80,45 @@ __device__ __forceinline__ bool selected_request(const VerifyArgs& a, int slot, 
 __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int b) {
   return a.n_drafts ? min(max(a.n_drafts[b], 0), a.K) : a.K;
 }
-__device__ __forceinline__ double temperature_of(const VerifyArgs& a, int b) {
-  return a.temperature ? (double)a.temperature[b] : 1.0;
+// log2(e) / temperature, 0 for greedy.  Temperatures count as at most 2^100 and at
+// least 2^-100, where logits a step of fp32 apart no longer or fully differ.
+__device__ __forceinline__ double slope_of(const VerifyArgs& a, int b) {
+  const float t = a.temperature ? a.temperature[b] : 1.f;
+  return t > 0.f ? kLog2e / (double)fminf(fmaxf(t, 0x1p-100f), 0x1p100f) : 0.0;
 }
 
-// 2^y for y <= 0 (NaN: 0), by 2^k 2^f with |f| <= 1/2 and the Taylor series of
-// e^(f ln 2) to the eleventh power (the next term is below 2^-47 of the value).
-// Below 2^-1022 it runs out into subnormals and 0.
+// 2^y for y in [-1000, 0], by 2^k 2^f with |f| <= 1/2: the polynomial through 2^f
+// at the nine Chebyshev nodes of the interval is off by 1.1e-12 of the value at
+// most (a draw sees borders moved by that share of the whole).  k comes out of the
+// low bits of y + 1.5 2^52.
 __device__ __forceinline__ double exp2_neg(double y) {
-  y = fmax(y, -1100.0);
-  const double k = rint(y), f = y - k;
-  constexpr double c = 0.69314718055994530942;
-  constexpr double c2 = c * c, c3 = c2 * c, c4 = c2 * c2, c5 = c4 * c, c6 = c4 * c2, c7 = c4 * c3, c8 = c4 * c4, c9 = c8 * c,
-                   c10 = c8 * c2, c11 = c8 * c3;
-  double p = c11 / 39916800.0;
-  p = fma(p, f, c10 / 3628800.0);
-  p = fma(p, f, c9 / 362880.0);
-  p = fma(p, f, c8 / 40320.0);
-  p = fma(p, f, c7 / 5040.0);
-  p = fma(p, f, c6 / 720.0);
-  p = fma(p, f, c5 / 120.0);
-  p = fma(p, f, c4 / 24.0);
-  p = fma(p, f, c3 / 6.0);
-  p = fma(p, f, c2 / 2.0);
-  p = fma(p, f, c);
+  constexpr double kShift = 6755399441055744.0;
+  const double t = y + kShift;
+  const double f = y - (t - kShift);
+  double p = 1.3255224878668817e-06;
+  p = fma(p, f, 1.5310079402249296e-05);
+  p = fma(p, f, 0.00015403455852453838);
+  p = fma(p, f, 0.0013333450568000645);
+  p = fma(p, f, 0.009618129159402558);
+  p = fma(p, f, 0.05550410941205933);
+  p = fma(p, f, 0.2402265069581299);
+  p = fma(p, f, 0.6931471805459335);
   p = fma(p, f, 1.0);
-  return ldexp(p, (int)k);
+  return ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
 }
 
 // Weights of a row's logits against `top`, its largest (above -infinity): slope =
 // log2(e) / temperature.  (The difference first: a logit may be the type's lowest
-// value, whose product is off by more than the whole range.)  Where the largest is
-// +infinity it alone weighs.
+// value, whose product is off by more than the whole range.)  Weights below 2^-1000
+// are 0, and so is NaN's.  Where the largest is +infinity it alone weighs.
 struct Weights {
   double slope, top;
 };
 __device__ __forceinline__ Weights weights_against(float top, double slope) { return Weights{slope, (double)top}; }
 __device__ __forceinline__ double finite_weight(const Weights& w, float z) {
-  return exp2_neg(((double)z - w.top) * w.slope);
+  const double y = ((double)z - w.top) * w.slope;
+  const double e = exp2_neg(y);
+  return y >= -1000.0 ? e : 0.0;
 }
 __device__ __forceinline__ double weight(const Weights& w, float z) {
   return w.top == (double)INFINITY ? (z == INFINITY ? 1.0 : 0.0) : finite_weight(w, z);
@@ -120,7 +126,7 @@ __device__ __forceinline__ double weight(const Weights& w, float z) {
 // The same for a split's or thread's largest logit against a row's, 0 where it
 // holds nothing.
 __device__ __forceinline__ double rescale(float m, float top, double slope) {
-  return m == -INFINITY ? 0.0 : m == top ? 1.0 : exp2_neg(((double)m - (double)top) * slope);
+  return m == top && m != -INFINITY ? 1.0 : weight(weights_against(top, slope), m);
 }
 
 // kPer logits of a split from v on, -infinity past its end.
@@ -139,15 +145,45 @@ __device__ __forceinline__ void load_tile(const float* row, int v0, int end, int
   }
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) x += __shfl_xor(x, s);
+// Reductions over the wavefront in six DPP steps (row shifts by 1, 2, 4, 8, then
+// each row's last lane into the next row, then the lower half's into the upper):
+// inclusive scans, whose last lane holds the whole.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double shifted(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, kCtrl, kRows, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), kCtrl, kRows, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_scan(double x) {
+  x += shifted<0x111, 0xf>(x);
+  x += shifted<0x112, 0xf>(x);
+  x += shifted<0x114, 0xf>(x);
+  x += shifted<0x118, 0xf>(x);
+  x += shifted<0x142, 0xa>(x);
+  x += shifted<0x143, 0xc>(x);
   return x;
 }
+__device__ __forceinline__ double lane_value(double x, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_value(wave_scan(x), 63); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float shifted_max(float x) {
+  const int none = __builtin_bit_cast(int, -INFINITY);
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(none, __builtin_bit_cast(int, x), kCtrl, kRows, 0xf, false)));
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
-  return x;
+  x = shifted_max<0x111, 0xf>(x);
+  x = shifted_max<0x112, 0xf>(x);
+  x = shifted_max<0x114, 0xf>(x);
+  x = shifted_max<0x118, 0xf>(x);
+  x = shifted_max<0x142, 0xa>(x);
+  x = shifted_max<0x143, 0xc>(x);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 __device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
@@ -163,9 +199,8 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
   const int split = blockIdx.x, i = blockIdx.y;
   int b;
   if (!selected_request(a, blockIdx.z, b) || i > drafts_of(a, b)) return;
-  const double t = temperature_of(a, b);
-  const bool greedy = !(t > 0.0);
-  const double slope = greedy ? 0.0 : kLog2e / t;
+  const double slope = slope_of(a, b);
+  const bool greedy = slope == 0.0;
   const float* row = a.logits + ((int64_t)b * (a.K + 1) + i) * a.V;
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -173,9 +208,13 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
   float top = -INFINITY;
   double sum = 0.0;
   int first = INT_MAX;
+  float next[kPer];
+  load_tile(row, begin, end, tid, next);
   for (int v0 = begin; v0 < end; v0 += kTile) {
     float z[kPer];
-    load_tile(row, v0, end, tid, z);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) z[e] = next[e];
+    if (v0 + kTile < end) load_tile(row, v0 + kTile, end, tid, next);
     float m = top;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) m = fmaxf(m, z[e]);     // passes NaN over
@@ -256,21 +295,12 @@ struct Draw {
   double scale;         // 1 / the row's sum
 };
 
-// Inclusive sums over the lanes.
-__device__ __forceinline__ double wave_scan(double x, int lane) {
+// The weights of N neighbouring tokens from v on (0 past the end).
+template <int N>
+__device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (&w)[N]) {
+  float z[N], q[N];
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const double y = __shfl_up(x, s);
-    if (lane >= s) x += y;
-  }
-  return x;
-}
-
-// The weights of kPer neighbouring tokens from v on (0 past the end).
-__device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (&w)[kPer]) {
-  float z[kPer], q[kPer];
-#pragma unroll
-  for (int e = 0; e < kPer; e += 4) {
+  for (int e = 0; e < N; e += 4) {
     if (v + e + 4 <= end) {
       const f32x4u t = *reinterpret_cast<const f32x4u*>(d.row + v + e);
       z[e] = t[0], z[e + 1] = t[1], z[e + 2] = t[2], z[e + 3] = t[3];
@@ -280,10 +310,10 @@ __device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (
     }
   }
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) q[e] = 0.f;
+  for (int e = 0; e < N; ++e) q[e] = 0.f;
   if (d.residual && d.q != nullptr) {
 #pragma unroll
-    for (int e = 0; e < kPer; e += 4) {
+    for (int e = 0; e < N; e += 4) {
       if (v + e + 4 <= end) {
         const f32x4u t = *reinterpret_cast<const f32x4u*>(d.q + v + e);
         q[e] = t[0], q[e + 1] = t[1], q[e + 2] = t[2], q[e + 3] = t[3];
@@ -295,14 +325,14 @@ __device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (
   }
   if (d.w.top == (double)INFINITY) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) w[e] = z[e] == INFINITY ? 1.0 : 0.0;
+    for (int e = 0; e < N; ++e) w[e] = z[e] == INFINITY ? 1.0 : 0.0;
   } else {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) w[e] = finite_weight(d.w, z[e]);
+    for (int e = 0; e < N; ++e) w[e] = finite_weight(d.w, z[e]);
   }
   if (d.residual) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
+    for (int e = 0; e < N; ++e) {
       w[e] *= d.scale;
       if (d.q != nullptr) w[e] = fmax(w[e] - (double)fmaxf(q[e], 0.f), 0.0);
       else w[e] = v + e == d.skip ? 0.0 : w[e];
@@ -311,49 +341,66 @@ __device__ __forceinline__ void draw_run(const Draw& d, int v, int end, double (
 }
 
 // The first token of the split whose cumulative weight, with `below` in front of
-// the split, exceeds `goal`; else its last token with a weight (INT_MAX: none).
-// Threads take kPer neighbours each, so their sums are in the tokens' order.
-__device__ __forceinline__ int find_token(const Draw& d, int begin, int end, double below, double goal, double* s_scan,
-                                          int* s_hit) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid == 0) {
-    s_hit[0] = INT_MAX;
-    s_hit[1] = -1;
-  }
-  for (int v0 = begin; v0 < end; v0 += kTile) {
-    const int v = v0 + tid * kPer;
-    double w[kPer], sum = 0.0;
+// the split, exceeds `goal`; else its last token with a weight (-1: none).  Threads
+// take kFind neighbours each, so their sums are in the tokens' order.
+constexpr int kFind = 16;
+struct FindScratch {
+  double sum[kThreads / 64];
+  int hit[kThreads / 64], last[kThreads / 64];
+};
+__device__ __forceinline__ int find_token(const Draw& d, int begin, int end, double below, double goal, FindScratch& sm) {
+  constexpr int kWaves = kThreads / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  int last_token = -1;
+  for (int v0 = begin; v0 < end; v0 += kThreads * kFind) {
+    const int v = v0 + tid * kFind;
+    double w[kFind], sum = 0.0;
     draw_run(d, v, end, w);
     int last = -1;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
+    for (int e = 0; e < kFind; ++e) {
       sum += w[e];
       if (w[e] > 0.0) last = v + e;
     }
-    const double upto = wave_scan(sum, lane);
-    __syncthreads();          // the tile before has been summed up; s_hit is set
-    if (lane == 63) s_scan[wave] = upto;
+    const double upto = wave_scan(sum);
+    __syncthreads();          // the round before has been read
+    if (lane == 63) sm.sum[wave] = upto;
     __syncthreads();
-    double base = below;
-    for (int k = 0; k < wave; ++k) base += s_scan[k];
-    for (int k = 0; k < kThreads / 64; ++k) below += s_scan[k];
-    if (last >= 0) {
-      atomicMax(&s_hit[1], last);
-      if (base + upto > goal) {
-        double c = base + (upto - sum);
-        int hit = INT_MAX;
+    double base = below, all = below;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          c += w[e];
-          if (hit == INT_MAX && w[e] > 0.0 && c > goal) hit = v + e;
-        }
-        // a thread whose sum passes the goal only by rounding takes its last
-        atomicMin(&s_hit[0], hit == INT_MAX ? last : hit);
-      }
+    for (int k = 0; k < kWaves; ++k) {
+      const double x = sm.sum[k];
+      if (k < wave) base += x;
+      all += x;
     }
+    below = all;
+    // the first lane whose sum passes the goal looks where (by rounding alone: its last)
+    const uint64_t past = __ballot(last >= 0 && base + upto > goal), some = __ballot(last >= 0);
+    int hit = -1;
+    if (past != 0 && lane == __builtin_ctzll(past)) {
+      double c = base + (upto - sum);
+#pragma unroll
+      for (int e = 0; e < kFind; ++e) {
+        c += w[e];
+        if (hit < 0 && w[e] > 0.0 && c > goal) hit = v + e;
+      }
+      if (hit < 0) hit = last;
+    }
+    const int wave_hit = past ? __builtin_amdgcn_readlane(hit, __builtin_ctzll(past)) : -1;
+    const int wave_last = some ? __builtin_amdgcn_readlane(last, 63 - __builtin_clzll(some)) : -1;
+    if (lane == 0) {
+      sm.hit[wave] = wave_hit;
+      sm.last[wave] = wave_last;
+    }
+    __syncthreads();
+    int found = -1;
+#pragma unroll
+    for (int k = kWaves - 1; k >= 0; --k) found = sm.hit[k] >= 0 ? sm.hit[k] : found;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) last_token = max(last_token, sm.last[k]);
+    if (found >= 0) return found;
   }
-  __syncthreads();
-  return s_hit[0] != INT_MAX ? s_hit[0] : s_hit[1] >= 0 ? s_hit[1] : INT_MAX;
+  return last_token;
 }
 
 // Split sums pass between workgroups of different XCDs: write-through stores
@@ -367,7 +414,7 @@ __device__ __forceinline__ double published(const double* p) {
                                                       __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// Launch 2: one workgroup per (split, request).
+// Launch 2: one workgroup per (split of a refused row, request).
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   constexpr int kWaves = kThreads / 64;
   __shared__ double s_sum[kMaxDrafts + 1];
@@ -375,15 +422,15 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   __shared__ int s_first[kMaxDrafts + 1];
   __shared__ int s_ok[kMaxDrafts + 1];
   __shared__ double s_scan[kWaves];
-  __shared__ int s_hit[2], s_split, s_last;
+  __shared__ FindScratch s_find;
+  __shared__ int s_from_p, s_split, s_last;
   __shared__ double s_below, s_goal;
   const int split = blockIdx.x;
   int b;
   if (!selected_request(a, blockIdx.y, b)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const double t = temperature_of(a, b);
-  const bool greedy = !(t > 0.0);
-  const double slope = greedy ? 0.0 : kLog2e / t;
+  const double slope = slope_of(a, b);
+  const bool greedy = slope == 0.0;
   const int n = drafts_of(a, b);
   const float* u = a.uniform + (int64_t)b * (a.K + 1);
 
@@ -418,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   d.skip = d.residual && !a.draft_probs ? a.draft_tokens[(int64_t)b * a.K + j] : -1;
   d.w = weights_against(top, slope);
   d.scale = 1.0 / s_sum[j];
-  const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
+  const int begin = min(a.V, split * a.draw_chunk), end = min(a.V, begin + a.draw_chunk);
 
   const bool summed = d.residual && top != -INFINITY;   // this call sums the weights itself
   if (summed) {
@@ -435,14 +482,14 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     if (tid == 0) {
       double all = 0.0;
       for (int w = 0; w < kWaves; ++w) all += s_scan[w];
-      publish(a.sums + (int64_t)b * a.splits + split, all);
+      publish(a.sums + (int64_t)b * kMaxSplits + split, all);
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (tid == 0) {
       const uint32_t k =
-          __builtin_amdgcn_atomic_inc32(a.tickets + b, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent");
-      s_last = k == (uint32_t)(a.splits - 1) ? 1 : 0;
+          __builtin_amdgcn_atomic_inc32(a.tickets + b, (uint32_t)(a.draw_splits - 1), __ATOMIC_RELAXED, "agent");
+      s_last = k == (uint32_t)(a.draw_splits - 1) ? 1 : 0;
     }
     __syncthreads();
     if (!s_last) return;
@@ -459,13 +506,13 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
       double part = 0.0, all = 0.0;
       bool from_p = !summed;
       if (summed) {
-        if (lane < a.splits) part = published(a.sums + (int64_t)b * a.splits + lane);
+        if (lane < a.draw_splits) part = published(a.sums + (int64_t)b * kMaxSplits + lane);
         all = wave_sum(part);
         from_p = !(all > 0.0);
       }
       if (from_p) part = join_row(a, b, j, lane, false, slope).part;
-      const double upto = wave_scan(part, lane);
-      const double goal = (double)u[a.K] * __shfl(upto, 63);
+      const double upto = wave_scan(part);
+      const double goal = (double)u[a.K] * lane_value(upto, 63);
       const uint64_t past = __ballot(upto > goal && part > 0.0);
       const uint64_t some = __ballot(part > 0.0);
       const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
@@ -473,16 +520,15 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         s_split = at;
         s_below = upto - part;
         s_goal = past ? goal : INFINITY;
-        s_hit[0] = from_p ? 1 : 0;
+        s_from_p = from_p ? 1 : 0;
       }
     }
     __syncthreads();
-    if (s_hit[0]) d.residual = false;
-    const int at = s_split;
-    const double below = s_below, goal = s_goal;
-    __syncthreads();
-    const int v = find_token(d, min(a.V, at * a.chunk), min(a.V, (at + 1) * a.chunk), below, goal, s_scan, s_hit);
-    token = v == INT_MAX ? -1 : v;
+    if (s_from_p) d.residual = false;
+    // (a residual's splits are this launch's, p's the first one's)
+    const int chunk = d.residual ? a.draw_chunk : a.chunk;
+    const int from = s_split * chunk;
+    token = find_token(d, min(a.V, from), min(a.V, from + chunk), s_below, s_goal, s_find);
   }
   int32_t* out = a.tokens + (int64_t)b * (a.K + 1);
   for (int i = tid; i <= a.K; i += kThreads)
@@ -491,21 +537,25 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
 }
 
 struct Layout {
-  int splits, chunk;
+  int splits, chunk, draw_splits, draw_chunk;
   size_t off_sums, off_stats, bytes;
 };
 
-// Splits of a row: enough that the rows' splits cover the chip a few times over,
-// of at least 2,048 logits, whole groups of four, at most kMaxSplits.
+// Splits of a row into at most kMaxSplits: about `groups` workgroups over `rows`
+// rows, of at least 2,048 logits; a split past one tile takes whole tiles.
+void split_row(int64_t vocab, int64_t rows, int64_t groups, int* splits, int* chunk) {
+  const int64_t most = std::min<int64_t>(kMaxSplits, oda::ceil_div(vocab, 2048));
+  const int64_t n = std::min(most, std::max<int64_t>(1, oda::ceil_div(groups, rows)));
+  const int64_t c = oda::ceil_div(vocab, n);
+  *chunk = (int)oda::round_up(c, c > kTile ? kTile : 4);
+  *splits = (int)oda::ceil_div(vocab, *chunk);
+}
+
 Layout layout(int64_t batch, int64_t vocab, int64_t max_drafts) {
   Layout l;
   const int64_t rows = batch * (max_drafts + 1);
-  const int64_t want = std::max<int64_t>(1, oda::ceil_div(2048, rows));
-  const int64_t most = std::min<int64_t>(kMaxSplits, oda::ceil_div(vocab, 2048));
-  const int64_t least = std::min<int64_t>(most, oda::ceil_div(vocab, kTile));
-  const int64_t n = std::min(most, std::max(want, least));
-  l.chunk = (int)std::min<int64_t>(INT_MAX / 2, oda::round_up(oda::ceil_div(vocab, n), 4));
-  l.splits = (int)oda::ceil_div(vocab, l.chunk);
+  split_row(vocab, rows, kStatGroups, &l.splits, &l.chunk);
+  split_row(vocab, batch, kDrawGroups, &l.draw_splits, &l.draw_chunk);
   l.off_sums = (size_t)oda::round_up(batch * 4, 256);                     // tickets first
   l.off_stats = l.off_sums + (size_t)oda::round_up(batch * kMaxSplits * 8, 256);
   l.bytes = l.off_stats + (size_t)oda::round_up(rows * kMaxSplits * (int64_t)sizeof(SplitStat), 256);
@@ -566,10 +616,12 @@ extern "C" oda_status oda_verify_drafts(const oda_verify_desc* desc, int32_t bat
   a.V = desc->vocab;
   a.splits = l.splits;
   a.chunk = l.chunk;
+  a.draw_splits = l.draw_splits;
+  a.draw_chunk = l.draw_chunk;
   (void)hipGetLastError();
   hipLaunchKernelGGL(verify_stats_kernel, dim3((unsigned)l.splits, (unsigned)(a.K + 1), (unsigned)batch),
                      dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)l.splits, (unsigned)batch), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)l.draw_splits, (unsigned)batch), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return oda::fail(ODA_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
   return oda::ok();
