@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(LoraShrinkArgs p) {
 #pragma unroll
   for (int j = 0; j < R; ++j) acc[j] = 0.f;
   const int nchunks = (p.K + 511) / 512;
-#pragma unroll 4
+#pragma unroll 2
   for (int c = 0; c < nchunks; ++c) {
     const int k0 = c * 512 + 8 * lane;
     const bool in = k0 < p.K;
@@ -449,6 +449,7 @@ void dense_mfma_kernel(Args p) {
   constexpr int kPer = (kOut + kThreads - 1) / kThreads;
   int out_b[kPer];
   float res[kPer];
+  [[maybe_unused]] int adapter[kPer];
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
     const int e = threadIdx.x + q * kThreads;
@@ -463,6 +464,7 @@ void dense_mfma_kernel(Args p) {
         if (!kSwiGLU && p.residual) res[q] = p.residual[(int64_t)b * p.N + row];
       }
     }
+    if constexpr (kLora) adapter[q] = out_b[q] >= 0 ? adapter_of(p.ids, p.num, out_b[q]) : -1;
   }
 
   f32x4 acc[S], low[S];
@@ -573,6 +575,29 @@ void dense_mfma_kernel(Args p) {
     for (int u = 0; u < U; ++u) step(u);
   }
 
+  // the adapters' terms of this thread's outputs, while other wavefronts still
+  // multiply
+  constexpr int kLoraRows = kSwiGLU ? 2 : 1;
+  [[maybe_unused]] float low_rank[kPer][kLoraRows];
+  if constexpr (kLora) {
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int e = threadIdx.x + q * kThreads;
+#pragma unroll
+      for (int r = 0; r < kLoraRows; ++r) {
+        float d = adapter[q] == -2 ? __builtin_nanf("") : 0.f;
+        if (adapter[q] >= 0) {
+          const int row = row0 + (e / (kEdge * kEdge)) * kEdge + e % kEdge + (r ? p.N : 0);
+          const uint16_t* lb = p.lora_b + (int64_t)adapter[q] * p.adapter_stride + (int64_t)row * p.rank;
+          const float* lt = lora_t(p, out_b[q], row);
+#pragma unroll 4
+          for (int i = 0; i < p.rank; i += 8) d += lora_dot8(lb + i, lt + i);
+        }
+        low_rank[q][r] = d;
+      }
+    }
+  }
+
   // add the wavefronts' tiles in order
   if (kNorm) {
 #pragma unroll
@@ -611,22 +636,8 @@ void dense_mfma_kernel(Args p) {
       }
     }
     if constexpr (kLora) {
-      const int id = adapter_of(p.ids, p.num, out_b[q]);
-      if (id == -2) {
-        v = __builtin_nanf("");
-      } else if (id >= 0) {
-        const int r = row0 + tile * kEdge + row;
-        const uint16_t* lb = p.lora_b + (int64_t)id * p.adapter_stride + (int64_t)r * p.rank;
-        const float* lt = lora_t(p, out_b[q], r);
-        float d = 0.f, d2 = 0.f;
-        const float* lt2 = kSwiGLU ? lora_t(p, out_b[q], p.N + r) : nullptr;
-        for (int i = 0; i < p.rank; i += 8) {
-          d += lora_dot8(lb + i, lt + i);
-          if (kSwiGLU) d2 += lora_dot8(lb + (int64_t)p.N * p.rank + i, lt2 + i);
-        }
-        v += d;
-        v2 += d2;
-      }
+      v += low_rank[q][0];
+      if (kSwiGLU) v2 += low_rank[q][kLoraRows - 1];
     }
     const float inv = kNorm ? rsqrtf(sq / (float)p.K + p.eps) : 1.f;
     const float out = kSwiGLU ? silu(v * inv) * (v2 * inv) : v * inv + res[q];
@@ -950,6 +961,7 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
 
 namespace {
 
+constexpr int kShrinkWaves = 2048;
 constexpr int kMaxRank = 128;   // rank / 8 lanes of a wavefront hold a row of the second factor
 
 oda_status check_lora(const oda_lora_desc* lora, int64_t* rows) {
@@ -1024,8 +1036,15 @@ extern "C" oda_status oda_dense_lora_bf16(const oda_dense_desc* desc, const oda_
   }
   if (batch > 65535) return oda::fail(ODA_ERR_SHAPE, "batch %d above 65535", batch);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(lora_shrink_kernel<1>, dim3((unsigned)oda::ceil_div(t_rows, kWaves), (unsigned)batch), dim3(256), 0,
-                     stream, sh);
+  // the most rows per wavefront (each reads the request's input) that leave
+  // kShrinkWaves wavefronts: 64 rows of 6,144 for 160 requests 16 us with one row
+  // each, 10 with four
+  const auto leaves = [&](int rows) { return (int64_t)batch * t_rows / rows >= kShrinkWaves; };
+  const auto grid = [&](int rows) { return dim3((unsigned)oda::ceil_div(t_rows / rows, kWaves), (unsigned)batch); };
+  if (leaves(8)) hipLaunchKernelGGL(lora_shrink_kernel<8>, grid(8), dim3(256), 0, stream, sh);
+  else if (leaves(4)) hipLaunchKernelGGL(lora_shrink_kernel<4>, grid(4), dim3(256), 0, stream, sh);
+  else if (leaves(2)) hipLaunchKernelGGL(lora_shrink_kernel<2>, grid(2), dim3(256), 0, stream, sh);
+  else hipLaunchKernelGGL(lora_shrink_kernel<1>, grid(1), dim3(256), 0, stream, sh);
   return launch_dense(a, swiglu, stream);
 }
 
