@@ -18,7 +18,9 @@ Per step (Alg. 1 with the commit of App. A.5):
                 candidates of every layer
 
 Native Full (always Full, no gate) and standalone Local (no gate, no retry)
-use the same pieces.  Stages are lists of pre-marshalled calls, so they can be
+use the same pieces.  DraftDecoder composes the step of many tenants with drafted
+tokens: shared-prefix attention, adapters beside the dense layers, verification
+and the commit of what was accepted.  Stages are lists of pre-marshalled calls, so they can be
 launched eagerly or captured as HIP graphs.
 """
 from __future__ import annotations
@@ -202,6 +204,131 @@ class Decoder:
     def local_stages(self):
         """Standalone Local: every layer over S^L, no gate, no retry."""
         return self._input() + self._forward(self.h, self.k_loc, self.v_loc, "local", False), [], self._output()
+
+
+class DraftDecoder:
+    """Decode steps of many tenants with drafted tokens: one forward of each
+    request's current token and its drafts (Full attention in every layer), the
+    drafts verified, the accepted tokens committed, the next token drawn.
+
+    Row b * T + t of the buffers is token t of request b.  Before a step, `tokens`
+    [B][T] holds the last committed choice's successor (the current token) and the
+    drafts, `drafts` [B][T - 1] the drafts again, `n_drafts` / `n_tokens` [B] how
+    many of each are in use (set_drafts writes the four), `uniform` [B][T] the random
+    numbers.  After it, `accepted` [B] and `answer` [B][T] (accepted drafts, next
+    token, -1) are oda_verify_drafts' outputs, and caches, lengths and row_lens are
+    ready for the next step.
+
+    groups: (group_start, members, prefix_blocks), int32 device tensors: requests
+    whose prompts share their first blocks; adapters: {"w_qkv" | "w_o" | "w_gu" |
+    "w_down": [LoraDesc per layer]}, any of them, chosen per request by adapter_ids
+    [B] (-1: none); temperature: fp32 [B] or None; draft_probs: True to verify
+    against `probs` [B][T - 1][V] (written before each step), else drafts count as
+    given."""
+
+    def __init__(self, shape: DecoderShape, weights: dict, batch: int, tokens: int, k_cache, v_cache, block_table,
+                 seq_lens, max_blocks_per_seq: int, max_seq_len: int, num_blocks: int, groups, adapters: dict | None = None,
+                 adapter_ids=None, temperature=None, draft_probs: bool = False):
+        import torch
+        s, B, T = shape, batch, tokens
+        dev = k_cache.device
+        self.shape, self.B, self.T, self.w = s, B, T, weights
+        self.k_cache, self.v_cache, self.table, self.seq_lens = k_cache, v_cache, block_table, seq_lens
+        self.temperature = temperature
+        f32 = dict(dtype=torch.float32, device=dev)
+        bf = dict(dtype=torch.bfloat16, device=dev)
+        i32 = dict(dtype=torch.int32, device=dev)
+        L, d, Hq, Hkv, D, rows = s.num_layers, s.d_model, s.num_q_heads, s.num_kv_heads, s.head_dim, B * T
+        self.tokens = torch.zeros(B, T, **i32)
+        self.drafts = torch.zeros(B, max(1, T - 1), **i32)
+        self.n_tokens = torch.full((B,), T, **i32)
+        self.n_drafts = torch.full((B,), T - 1, **i32)
+        self.uniform = torch.zeros(B, T, **f32)
+        self.probs = torch.zeros(B, T - 1, s.vocab, **f32) if draft_probs and T > 1 else None
+        self.accepted = torch.zeros(B, **i32)
+        self.answer = torch.zeros(B, T, **i32)
+        self.row_lens = (seq_lens[:, None] + torch.arange(T, **i32)).to(torch.int32).contiguous()
+        self.h = torch.zeros(rows, d, **f32)
+        self.state = torch.zeros(rows, d, **f32)       # final-normalised
+        self.qkv = torch.zeros(rows, s.qkv_dim, **f32)
+        self.q = torch.zeros(B, T, Hq, D, **bf)
+        self.attn = torch.zeros(rows, Hq * D, **f32)
+        self.mlp = torch.zeros(rows, s.d_ffn, **f32)
+        self.logits = torch.zeros(B, T, s.vocab, **f32)
+        self.k_cand = torch.zeros(L, B, T, Hkv, D, **bf)
+        self.v_cand = torch.zeros(L, B, T, Hkv, D, **bf)
+        self.scale = 1.0 / math.sqrt(D)
+        self.adapters = adapters or {}
+        self.row_adapters = None if adapter_ids is None else \
+            adapter_ids.to(torch.int32).repeat_interleave(T).contiguous()
+        if self.adapters and self.row_adapters is None:
+            raise ValueError("adapters need adapter_ids")
+        start, members, prefix = groups
+        self.attn_shape = P.Shape(1, B, Hq, Hkv, D, max_blocks_per_seq, max_seq_len, num_blocks)
+        self.commit_shape = P.Shape(L, B, Hq, Hkv, D, max_blocks_per_seq, max_seq_len, num_blocks)
+        self.groups = P.prefix_groups(prefix.numel(), T, start, members, prefix, self.n_tokens)
+
+        def zeros(n):
+            return torch.zeros(max(256, n), dtype=torch.uint8, device=dev)
+
+        self.plan = zeros(P.prefix_plan_size(self.attn_shape, self.groups))
+        self.ws_attn = zeros(P.prefix_workspace_size(self.attn_shape, self.groups))
+        self.ws_lora = zeros(max([P.lora_workspace_size(a[0], rows) for a in self.adapters.values()], default=0))
+        self.ws_verify = zeros(P.verify_workspace_size(B, s.vocab, T - 1))
+        self.ws_commit = zeros(P.commit_workspace_size(self.commit_shape))
+        w = weights
+        self.desc = dict(
+            w_qkv=[P.dense_desc(d, s.qkv_dim, P.DENSE_PLAIN, w["w_qkv"][l], w["attn_norm"][l], s.rms_eps) for l in range(L)],
+            w_o=[P.dense_desc(Hq * D, d, P.DENSE_PLAIN, w["w_o"][l]) for l in range(L)],
+            w_gu=[P.dense_desc(d, s.d_ffn, P.DENSE_SWIGLU, w["w_gu"][l], w["mlp_norm"][l], s.rms_eps) for l in range(L)],
+            w_down=[P.dense_desc(s.d_ffn, d, P.DENSE_PLAIN, w["w_down"][l]) for l in range(L)])
+        self.d_vocab = P.dense_desc(d, s.vocab, P.DENSE_PLAIN, w["embed"])
+
+    def set_drafts(self, current, drafts, n_drafts) -> None:
+        """The next step's current tokens [B], drafts [B][T - 1] and their counts [B]."""
+        self.tokens[:, 0].copy_(current)
+        if self.T > 1:
+            self.tokens[:, 1:].copy_(drafts)
+            self.drafts.copy_(drafts)
+        self.n_drafts.copy_(n_drafts)
+        self.n_tokens.copy_(n_drafts + 1)
+
+    def _dense(self, name: str, l: int, x, residual, y):
+        rows = self.B * self.T
+        if name in self.adapters:
+            return P.prepare_dense_lora(self.desc[name][l], self.adapters[name][l], rows, x, residual, y, self.row_adapters,
+                                        self.ws_lora)
+        return P.prepare_dense(self.desc[name][l], rows, x, residual, y)
+
+    def stages(self):
+        """(forward, verification, commit) of one step, as prepared calls."""
+        s, B, T = self.shape, self.B, self.T
+        rows = B * T
+
+        def inputs(l):
+            return P.inputs(self.q, self.k_cache[l], self.v_cache[l], self.table, self.seq_lens, self.scale, self.k_cand[l],
+                            self.v_cand[l])
+
+        forward = [P.prepare_embed(self.w["embed"], s.vocab, s.d_model, rows, self.tokens, self.h),
+                   P.prepare_prefix_plan(self.attn_shape, inputs(0), self.groups, self.plan)]
+        for l in range(s.num_layers):
+            forward += [
+                self._dense("w_qkv", l, self.h, None, self.qkv),
+                P.prepare_qk_norm_rope(rows, s.num_q_heads, s.num_kv_heads, s.head_dim, self.qkv, self.w["q_norm"][l],
+                                       self.w["k_norm"][l], s.rms_eps, s.rope_theta, self.row_lens, self.q, self.k_cand[l],
+                                       self.v_cand[l]),
+                P.prepare_prefix_decode_attn(self.attn_shape, inputs(l), self.groups, self.plan, self.attn, None,
+                                             self.ws_attn),
+                self._dense("w_o", l, self.attn, self.h, self.h),
+                self._dense("w_gu", l, self.h, None, self.mlp),
+                self._dense("w_down", l, self.mlp, self.h, self.h)]
+        forward += [P.prepare_rms_norm_rows(rows, s.d_model, self.h, self.w["final_norm"], s.rms_eps, self.state),
+                    P.prepare_dense(self.d_vocab, rows, self.state, None, self.logits)]
+        verify = P.verify_desc(s.vocab, T - 1, self.logits, self.drafts if T > 1 else None, self.uniform, self.probs,
+                               self.n_drafts, self.temperature)
+        return (forward, [P.prepare_verify_drafts(verify, B, self.accepted, self.answer, self.ws_verify)],
+                [P.prepare_commit_drafts(self.commit_shape, T, self.k_cache, self.v_cache, self.table, self.seq_lens,
+                                         self.k_cand, self.v_cand, self.accepted, True, self.row_lens, self.ws_commit)])
 
 
 def run(calls) -> None:
