@@ -108,7 +108,8 @@ __device__ __forceinline__ float lora_dot8(const uint16_t* b8, const float* t8) 
 }
 
 // t[b][r] = scale[a] * sum_k A[a][r][k] gain[k] x[b][k] for the rank rows r of all
-// parts, a = the request's adapter.  One wavefront per R rows of one request.
+// parts, a = the request's adapter.  One workgroup per R rows of one request, whose
+// wavefronts take every fourth chunk of 512 elements.
 struct LoraShrinkArgs {
   const uint16_t* a;         // [num][rows][K], rows = parts * rank
   const float* scale;
@@ -123,10 +124,11 @@ struct LoraShrinkArgs {
 
 template <int R>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(LoraShrinkArgs p) {
+  __shared__ float sums[kWaves][R];
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
-  const int row0 = (blockIdx.x * kWaves + wave) * R;   // rows is a multiple of R
-  if (row0 >= p.rows || (int)blockIdx.y >= selected_count(p.n_work, p.B)) return;
+  const int row0 = blockIdx.x * R;               // rows is a multiple of R
+  if ((int)blockIdx.y >= selected_count(p.n_work, p.B)) return;
   const int b = selected_request(p.work_list, blockIdx.y);
   if (b < 0 || b >= p.B) return;
   const int id = uniform(adapter_of(p.ids, p.num, b));
@@ -136,9 +138,8 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(LoraShrinkArgs p) {
   float acc[R];
 #pragma unroll
   for (int j = 0; j < R; ++j) acc[j] = 0.f;
-  const int nchunks = (p.K + 511) / 512;
 #pragma unroll 2
-  for (int c = 0; c < nchunks; ++c) {
+  for (int c = wave; c * 512 < p.K; c += kWaves) {
     const int k0 = c * 512 + 8 * lane;
     const bool in = k0 < p.K;
     const int k = in ? k0 : 0;
@@ -159,13 +160,18 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(LoraShrinkArgs p) {
 #pragma unroll
       for (int j = 0; j < R; ++j) acc[j] += ((e & 1) ? bf16_hi(w[j][e >> 1]) : bf16_lo(w[j][e >> 1])) * xv[e];
   }
-  float v = 0.f;
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const float sum = wave_sum(acc[j]);
-    if (lane == j) v = sum;
+    if (lane == j) sums[wave][j] = sum;
   }
-  if (lane < R) p.t[(int64_t)b * p.rows + row0 + lane] = v * p.scale[id];
+  __syncthreads();
+  if (threadIdx.x < R) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) v += sums[i][threadIdx.x];
+    p.t[(int64_t)b * p.rows + row0 + threadIdx.x] = v * p.scale[id];
+  }
 }
 
 // One request per grid row, one wavefront per group of R output rows.  Lanes take 8
@@ -345,7 +351,7 @@ __device__ __forceinline__ void split_bf16x3(const float (&x)[8], bf16x8 (&p)[3]
   }
 }
 
-// y = W x' for up to 16 selected requests per workgroup on
+// y = W x' for up to 16 T selected requests per workgroup on
 // v_mfma_f32_16x16x32_bf16, W's rows as the A operand (lane h, j: row h,
 // elements 8j..8j+7 of a 32-element step) and the requests as columns.  The
 // fp32 inputs enter as three bf16 pieces each (split_bf16x3), so every product
@@ -367,11 +373,13 @@ __device__ __forceinline__ void split_bf16x3(const float (&x)[8], bf16x8 (&p)[3]
 // the reduction for small ones.  Two chunks of weights in flight, 16
 // wavefronts, and chunks of 128 were all slower.
 //   P       row tiles of the workgroup (SwiGLU: gate and up tiles each)
+//   T       tiles of sixteen requests; two, with four row tiles, halve what a
+//           launch of many workgroups reads from L2 and splits into pieces
 //   kHalf   tiles of eight rows, for at most eight requests at a time: tile
 //           rows and columns 8..15 hold the same rows and requests over the
 //           second half of K (the two off-diagonal quadrants are not used), so
 //           that a layer of few rows still fills the chip
-template <bool kSwiGLU, bool kNorm, int P, bool kHalf, class Args>
+template <bool kSwiGLU, bool kNorm, int P, int T, bool kHalf, class Args>
 __global__ __launch_bounds__(kMfmaWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void dense_mfma_kernel(Args p) {
   constexpr bool kLora = std::is_same<Args, DenseLoraArgs>::value;
@@ -380,19 +388,19 @@ void dense_mfma_kernel(Args p) {
   constexpr int U = kChunk / 32;                      // steps per chunk
   constexpr int kLanes = kChunk / 4;                  // lanes that read one input row of a chunk
   constexpr int kRowsAt = 64 / kLanes;                // input rows per load
-  constexpr int kPairs = kMfmaRows / kRowsAt;         // loads that read a chunk of the sixteen input rows
+  constexpr int kPairs = T * kMfmaRows / kRowsAt;     // loads that read a chunk of the input rows
   constexpr int kPitch = kChunk + 4;                  // floats per staged input row: rows on different banks
   constexpr int kWLanes = kChunk / 8;                 // lanes that read one weight row of a chunk
   constexpr int kWLoads = kMfmaRows * kWLanes / 64;   // loads that read a chunk of one tile
   constexpr int kWPitch = kChunk + 8;
   __shared__ union {
     struct {
-      float x[kMfmaWaves][kMfmaRows][kPitch];
+      float x[kMfmaWaves][T * kMfmaRows][kPitch];
       uint16_t w[kMfmaWaves][S][kMfmaRows][kWPitch];
     };
-    f32x4 acc[kMfmaWaves][S][64];
+    f32x4 acc[kMfmaWaves][T][S][64];
   } sm;
-  __shared__ float sm_ss[kMfmaWaves][kMfmaRows];
+  __shared__ float sm_ss[kMfmaWaves][T * kMfmaRows];
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const int h = lane & 15, j = lane >> 4;
@@ -400,11 +408,11 @@ void dense_mfma_kernel(Args p) {
   // the batch tiles of a row group run next to each other on one XCD
   // (workgroup i runs on XCD i mod 8), so its weights come from HBM once
   const int groups = (p.N + P * kEdge - 1) / (P * kEdge);
-  const int span = 8 * ((p.B + kEdge - 1) / kEdge);
+  const int span = 8 * ((p.B + T * kEdge - 1) / (T * kEdge));
   const int rg = (int)(blockIdx.x / span) * 8 + (int)(blockIdx.x % 8);
-  const int s0 = (int)(blockIdx.x % span) / 8 * kEdge;
+  const int s0 = (int)(blockIdx.x % span) / 8 * (T * kEdge);
   if (rg >= groups || s0 >= count) return;
-  const int nb = min(kEdge, count - s0);
+  const int nb = min(T * kEdge, count - s0);
   const int row0 = rg * P * kEdge;
 
   // K in 32-element steps, a contiguous stretch per wavefront; kHalf: tile
@@ -417,7 +425,7 @@ void dense_mfma_kernel(Args p) {
   const int chunks = (n + U - 1) / U;
   // end of this wavefront's stretch within either half (kHalf: loads of tile
   // rows and columns 8..15 take the second)
-  static_assert(!kHalf || (kMfmaRows / kRowsAt == 4 && kWLoads == 2), "a load stays within one half");
+  static_assert(!kHalf || (kPairs == 4 && kWLoads == 2), "a load stays within one half");
   const int stop0 = min(khalf, (step0 + n) * 32), stop1 = min(p.K - khalf, (step0 + n) * 32);
 
   // input row 4m + lane / 16 of load m: its request's row (columns past the
@@ -427,7 +435,7 @@ void dense_mfma_kernel(Args p) {
 #pragma unroll
   for (int m = 0; m < kPairs; ++m) {
     const int v = kRowsAt * m + lane / kLanes;
-    const int b = selected_request(p.work_list, s0 + min(v & (kEdge - 1), nb - 1));
+    const int b = selected_request(p.work_list, s0 + min(kHalf ? v & (kEdge - 1) : v, nb - 1));
     xrow[m] = p.x + (int64_t)(b >= 0 && b < p.B ? b : 0) * p.K + (kHalf && m >= kPairs / 2 ? khalf : 0);
   }
   // tile row kMfmaRows / kWLoads * i + lane / kWLanes of weight load i, as an
@@ -443,34 +451,41 @@ void dense_mfma_kernel(Args p) {
     for (int s = 0; s < P; ++s)
       woff[s][i] = (uint32_t)max(0, min(v & (kEdge - 1), p.N - 1 - (row0 + s * kEdge))) * (uint32_t)p.K;
   }
-  // the epilogue's outputs of this thread; their residuals are read now
-  constexpr int kOut = P * kEdge * kEdge;
+  // the epilogue's outputs of this thread and their residuals, read now where
+  // the registers allow it
+  constexpr int kOut = P * T * kEdge * kEdge;
   constexpr int kThreads = kMfmaWaves * 64;
   constexpr int kPer = (kOut + kThreads - 1) / kThreads;
+  constexpr bool kEarly = T == 1 || !kLora;
   int out_b[kPer];
   float res[kPer];
   [[maybe_unused]] int adapter[kPer];
+  auto outputs = [&] {
 #pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    const int e = threadIdx.x + q * kThreads;
-    const int row = row0 + (e / (kEdge * kEdge)) * kEdge + e % kEdge;
-    const int slot = e / kEdge % kEdge;
-    out_b[q] = -1;
-    res[q] = 0.f;
-    if (e < kOut && row < p.N && slot < nb) {
-      const int b = selected_request(p.work_list, s0 + slot);
-      if (b >= 0 && b < p.B) {
-        out_b[q] = b;
-        if (!kSwiGLU && p.residual) res[q] = p.residual[(int64_t)b * p.N + row];
+    for (int q = 0; q < kPer; ++q) {
+      const int e = threadIdx.x + q * kThreads;
+      const int row = row0 + (e / (T * kEdge * kEdge)) * kEdge + e % kEdge;
+      const int slot = e / kEdge % (T * kEdge);
+      out_b[q] = -1;
+      res[q] = 0.f;
+      if (e < kOut && row < p.N && slot < nb) {
+        const int b = selected_request(p.work_list, s0 + slot);
+        if (b >= 0 && b < p.B) {
+          out_b[q] = b;
+          if (!kSwiGLU && p.residual) res[q] = p.residual[(int64_t)b * p.N + row];
+        }
       }
+      if constexpr (kLora) adapter[q] = out_b[q] >= 0 ? adapter_of(p.ids, p.num, out_b[q]) : -1;
     }
-    if constexpr (kLora) adapter[q] = out_b[q] >= 0 ? adapter_of(p.ids, p.num, out_b[q]) : -1;
-  }
+  };
+  if (kEarly) outputs();
 
-  f32x4 acc[S], low[S];
+  f32x4 acc[T][S], low[T][S];
   float ss[kPairs];
 #pragma unroll
-  for (int s = 0; s < S; ++s) acc[s] = low[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int s = 0; s < S; ++s) acc[t][s] = low[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int m = 0; m < kPairs; ++m) ss[m] = 0.f;
   u32x4 w[S][kWLoads];
@@ -503,7 +518,7 @@ void dense_mfma_kernel(Args p) {
       for (int s = 0; s < S; ++s) w[s][i] = *reinterpret_cast<const u32x4*>(wbase[s] + (woff[s % P][i] + at));
     }
   };
-  float (&stage)[kMfmaRows][kPitch] = sm.x[wave];
+  float (&stage)[T * kMfmaRows][kPitch] = sm.x[wave];
   // Only a stretch's last chunk can reach past its end (kHalf: the second
   // half's, which is no longer than the first): there inputs, gains and weights
   // are zeroed, all of them, since 0 times an infinity would be NaN.
@@ -537,22 +552,27 @@ void dense_mfma_kernel(Args p) {
     }
   };
   auto step = [&](int u) {
-    float xv[8];
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(&stage[h][32 * u + 8 * j]);
-    const f32x4 hi = *reinterpret_cast<const f32x4*>(&stage[h][32 * u + 8 * j + 4]);
+    bf16x8 ws[S];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      xv[e] = lo[e];
-      xv[4 + e] = hi[e];
-    }
-    bf16x8 px[3];
-    split_bf16x3(xv, px);
+    for (int s = 0; s < S; ++s) ws[s] = *reinterpret_cast<const bf16x8*>(&sm.w[wave][s][h][32 * u + 8 * j]);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const bf16x8 ws = *reinterpret_cast<const bf16x8*>(&sm.w[wave][s][h][32 * u + 8 * j]);
-      acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[0], acc[s], 0, 0, 0);
-      low[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[2], low[s], 0, 0, 0);
-      low[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[1], low[s], 0, 0, 0);
+    for (int t = 0; t < T; ++t) {
+      float xv[8];
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(&stage[kMfmaRows * t + h][32 * u + 8 * j]);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(&stage[kMfmaRows * t + h][32 * u + 8 * j + 4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        xv[e] = lo[e];
+        xv[4 + e] = hi[e];
+      }
+      bf16x8 px[3];
+      split_bf16x3(xv, px);
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        acc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[0], acc[t][s], 0, 0, 0);
+        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[2], low[t][s], 0, 0, 0);
+        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[1], low[t][s], 0, 0, 0);
+      }
     }
   };
   if (chunks > 0) {
@@ -575,6 +595,7 @@ void dense_mfma_kernel(Args p) {
     for (int u = 0; u < U; ++u) step(u);
   }
 
+  if (!kEarly) outputs();
   // the adapters' terms of this thread's outputs, while other wavefronts still
   // multiply
   constexpr int kLoraRows = kSwiGLU ? 2 : 1;
@@ -587,7 +608,7 @@ void dense_mfma_kernel(Args p) {
       for (int r = 0; r < kLoraRows; ++r) {
         float d = adapter[q] == -2 ? __builtin_nanf("") : 0.f;
         if (adapter[q] >= 0) {
-          const int row = row0 + (e / (kEdge * kEdge)) * kEdge + e % kEdge + (r ? p.N : 0);
+          const int row = row0 + (e / (T * kEdge * kEdge)) * kEdge + e % kEdge + (r ? p.N : 0);
           const uint16_t* lb = p.lora_b + (int64_t)adapter[q] * p.adapter_stride + (int64_t)row * p.rank;
           const float* lt = lora_t(p, out_b[q], row);
 #pragma unroll 4
@@ -609,20 +630,24 @@ void dense_mfma_kernel(Args p) {
   }
   __syncthreads();   // the staged chunks are no longer read
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    // an infinite weight makes `low` NaN where an input's lower pieces are
-    // zero: a sum of the leading pieces that is not finite is the result
-    f32x4 t;
+  for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = fabsf(acc[s][i]) < INFINITY ? acc[s][i] + low[s][i] : acc[s][i];
-    sm.acc[wave][s][lane] = t;
-  }
+    for (int s = 0; s < S; ++s) {
+      // an infinite weight makes `low` NaN where an input's lower pieces are
+      // zero: a sum of the leading pieces that is not finite is the result
+      const f32x4 a = acc[t][s], b = low[t][s];
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = fabsf(a[i]) < INFINITY ? a[i] + b[i] : a[i];
+      sm.acc[wave][t][s][lane] = v;
+    }
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
     if (out_b[q] < 0) continue;
     const int e = threadIdx.x + q * kThreads;
-    const int tile = e / (kEdge * kEdge), row = e % kEdge, col = e / kEdge % kEdge;
+    const int tile = e / (T * kEdge * kEdge), row = e % kEdge, col = e / kEdge % kEdge;
+    const int t = e / (kEdge * kEdge) % T;
     float v = 0.f, v2 = 0.f, sq = 0.f;
 #pragma unroll
     for (int half = 0; half < (kHalf ? 2 : 1); ++half) {
@@ -630,9 +655,9 @@ void dense_mfma_kernel(Args p) {
       const int at = (hr / 4) * 16 + hcol;              // the lane that holds rows 4j..4j+3 of the column
 #pragma unroll
       for (int wv = 0; wv < kMfmaWaves; ++wv) {
-        v += sm.acc[wv][tile][at][hr % 4];
-        if (kSwiGLU) v2 += sm.acc[wv][P + tile][at][hr % 4];
-        if (kNorm) sq += sm_ss[wv][hcol];
+        v += sm.acc[wv][t][tile][at][hr % 4];
+        if (kSwiGLU) v2 += sm.acc[wv][t][P + tile][at][hr % 4];
+        if (kNorm) sq += sm_ss[wv][kMfmaRows * t + hcol];
       }
     }
     if constexpr (kLora) {
@@ -645,16 +670,16 @@ void dense_mfma_kernel(Args p) {
   }
 }
 
-template <bool kSwiGLU, int P, bool kHalf, class Args>
+template <bool kSwiGLU, int P, int T, bool kHalf, class Args>
 oda_status launch_dense_mfma(const Args& a, hipStream_t stream) {
   constexpr int kEdge = kHalf ? 8 : kMfmaRows;
-  const int64_t groups = oda::ceil_div(oda::ceil_div(a.N, P * kEdge), 8) * 8 * oda::ceil_div(a.B, kEdge);
+  const int64_t groups = oda::ceil_div(oda::ceil_div(a.N, P * kEdge), 8) * 8 * oda::ceil_div(a.B, T * kEdge);
   if (groups > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "layer too large");
   const dim3 grid((unsigned)groups), block(kMfmaWaves * 64);
   if (a.gain)
-    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, true, P, kHalf, Args>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, true, P, T, kHalf, Args>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, false, P, kHalf, Args>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((dense_mfma_kernel<kSwiGLU, false, P, T, kHalf, Args>), grid, block, 0, stream, a);
   return ODA_OK;
 }
 
@@ -903,23 +928,33 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
   const auto groups_of = [&](int tiles, int edge) {
     return oda::ceil_div(N, tiles * edge) * oda::ceil_div(a.B, edge);
   };
+  // Where that leaves more than two rounds, one of workgroups with 64 rows and 32
+  // requests takes as long as two of those with 32 and 16 (2048 -> 4096: 96
+  // requests 16.7 us against 22.4, 64 requests 15.9 against 15.5; 6144 -> 2048: 160
+  // requests 31.5 against 36.0, 128 requests 30.6 against 27.0; 2048 -> 151936, 160
+  // requests 760 against 1241).  The SwiGLU pair has no room for it: half the rows
+  // were slower than three tiles up to 64 requests and within 8% above.
+  const int64_t wide_rounds =
+      oda::ceil_div(oda::ceil_div(N, 4 * kMfmaRows) * oda::ceil_div(a.B, 2 * kMfmaRows), kTargetGroups);
   const bool one = !swiglu && groups_of(2, kMfmaRows) >= 8 * kTargetGroups && a.K >= 3 * kMfmaWaves * kChunk &&
                    a.K % (kMfmaWaves * kChunk) == 0;
   if ((a.B > 1 || one) && a.K < kMfmaMaxK) {
     oda_status st;
     const auto fits = [&](int tiles, int edge) { return groups_of(tiles, edge) <= kTargetGroups; };
     if (swiglu) {
-      if (fits(1, 8)) st = launch_dense_mfma<true, 1, true>(a, stream);
-      else if (fits(2, 8)) st = launch_dense_mfma<true, 2, true>(a, stream);
-      else if (fits(3, 8)) st = launch_dense_mfma<true, 3, true>(a, stream);
-      else if (fits(1, kMfmaRows)) st = launch_dense_mfma<true, 1, false>(a, stream);
-      else if (fits(2, kMfmaRows)) st = launch_dense_mfma<true, 2, false>(a, stream);
-      else st = launch_dense_mfma<true, 3, false>(a, stream);
+      if (fits(1, 8)) st = launch_dense_mfma<true, 1, 1, true>(a, stream);
+      else if (fits(2, 8)) st = launch_dense_mfma<true, 2, 1, true>(a, stream);
+      else if (fits(3, 8)) st = launch_dense_mfma<true, 3, 1, true>(a, stream);
+      else if (fits(1, kMfmaRows)) st = launch_dense_mfma<true, 1, 1, false>(a, stream);
+      else if (fits(2, kMfmaRows)) st = launch_dense_mfma<true, 2, 1, false>(a, stream);
+      else st = launch_dense_mfma<true, 3, 1, false>(a, stream);
     } else {
-      if (fits(1, 8)) st = launch_dense_mfma<false, 1, true>(a, stream);
-      else if (fits(2, 8)) st = launch_dense_mfma<false, 2, true>(a, stream);
-      else if (fits(1, kMfmaRows)) st = launch_dense_mfma<false, 1, false>(a, stream);
-      else st = launch_dense_mfma<false, 2, false>(a, stream);
+      if (fits(1, 8)) st = launch_dense_mfma<false, 1, 1, true>(a, stream);
+      else if (fits(2, 8)) st = launch_dense_mfma<false, 2, 1, true>(a, stream);
+      else if (fits(1, kMfmaRows)) st = launch_dense_mfma<false, 1, 1, false>(a, stream);
+      else if (groups_of(2, kMfmaRows) > 2 * kTargetGroups * wide_rounds)
+        st = launch_dense_mfma<false, 4, 2, false>(a, stream);
+      else st = launch_dense_mfma<false, 2, 1, false>(a, stream);
     }
     return st == ODA_OK ? launch_status() : st;
   }
@@ -961,7 +996,7 @@ extern "C" oda_status oda_dense_bf16(const oda_dense_desc* desc, int32_t batch, 
 
 namespace {
 
-constexpr int kShrinkWaves = 2048;
+constexpr int kShrinkGroups = 1024;
 constexpr int kMaxRank = 128;   // rank / 8 lanes of a wavefront hold a row of the second factor
 
 oda_status check_lora(const oda_lora_desc* lora, int64_t* rows) {
@@ -1036,11 +1071,12 @@ extern "C" oda_status oda_dense_lora_bf16(const oda_dense_desc* desc, const oda_
   }
   if (batch > 65535) return oda::fail(ODA_ERR_SHAPE, "batch %d above 65535", batch);
   (void)hipGetLastError();
-  // the most rows per wavefront (each reads the request's input) that leave
-  // kShrinkWaves wavefronts: 64 rows of 6,144 for 160 requests 16 us with one row
-  // each, 10 with four
-  const auto leaves = [&](int rows) { return (int64_t)batch * t_rows / rows >= kShrinkWaves; };
-  const auto grid = [&](int rows) { return dim3((unsigned)oda::ceil_div(t_rows / rows, kWaves), (unsigned)batch); };
+  // the most rows per workgroup (its wavefronts read the request's input once for
+  // them) that leave kShrinkGroups workgroups: 64 rows of 6,144 for 160 requests
+  // 11.0 us with eight rows each, 11.4 with four; 128 rows of 2,048 for 32
+  // requests 4.15 with one or two, 4.5 with eight
+  const auto leaves = [&](int rows) { return (int64_t)batch * t_rows / rows >= kShrinkGroups; };
+  const auto grid = [&](int rows) { return dim3((unsigned)(t_rows / rows), (unsigned)batch); };
   if (leaves(8)) hipLaunchKernelGGL(lora_shrink_kernel<8>, grid(8), dim3(256), 0, stream, sh);
   else if (leaves(4)) hipLaunchKernelGGL(lora_shrink_kernel<4>, grid(4), dim3(256), 0, stream, sh);
   else if (leaves(2)) hipLaunchKernelGGL(lora_shrink_kernel<2>, grid(2), dim3(256), 0, stream, sh);
