@@ -61,8 +61,8 @@ struct VerifyArgs {
   const int32_t* work_list;
   const int32_t* n_work;
   SplitStat* stats;       // [B][K + 1][splits]
-  double* sums;           // [B][kMaxSplits]: weights of the row that the next token is drawn from
-  uint32_t* tickets;      // [B], zero between calls
+  double* sums;           // [slot][kMaxSplits]: weights of the row that the next token is drawn from
+  uint32_t* tickets;      // [slot], zero between calls (slots, as a request may be listed twice)
   int32_t B, K, V;
   int32_t splits, chunk;            // of a row in the first launch
   int32_t draw_splits, draw_chunk;  // of a refused row in the second
@@ -425,9 +425,9 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   __shared__ FindScratch s_find;
   __shared__ int s_from_p, s_split, s_last;
   __shared__ double s_below, s_goal;
-  const int split = blockIdx.x;
+  const int split = blockIdx.x, slot = blockIdx.y;
   int b;
-  if (!selected_request(a, blockIdx.y, b)) return;
+  if (!selected_request(a, slot, b)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const double slope = slope_of(a, b);
   const bool greedy = slope == 0.0;
@@ -482,13 +482,13 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     if (tid == 0) {
       double all = 0.0;
       for (int w = 0; w < kWaves; ++w) all += s_scan[w];
-      publish(a.sums + (int64_t)b * kMaxSplits + split, all);
+      publish(a.sums + (int64_t)slot * kMaxSplits + split, all);
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (tid == 0) {
       const uint32_t k =
-          __builtin_amdgcn_atomic_inc32(a.tickets + b, (uint32_t)(a.draw_splits - 1), __ATOMIC_RELAXED, "agent");
+          __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.draw_splits - 1), __ATOMIC_RELAXED, "agent");
       s_last = k == (uint32_t)(a.draw_splits - 1) ? 1 : 0;
     }
     __syncthreads();
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
       double part = 0.0, all = 0.0;
       bool from_p = !summed;
       if (summed) {
-        if (lane < a.draw_splits) part = published(a.sums + (int64_t)b * kMaxSplits + lane);
+        if (lane < a.draw_splits) part = published(a.sums + (int64_t)slot * kMaxSplits + lane);
         all = wave_sum(part);
         from_p = !(all > 0.0);
       }

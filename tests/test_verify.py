@@ -217,3 +217,11 @@ def test_captured_call_replays():
         np.testing.assert_array_equal(t.acc.cpu().numpy(), ra)
         np.testing.assert_array_equal(t.tok.cpu().numpy(), rt)
         _ = (t.dev[0] * 2).sum().item()
+
+
+def test_a_request_listed_twice():
+    """Each place of the list has its own sums and words: a request listed several times gets its one result."""
+    t = Drafts(41, 9, 3, 20011, temps=(1.0, 0.7, 1.3))
+    t.check([2, 2, 2, 5, 2, 7, 5, 2])
+    t.check([8] * 9)
+    t.check()
