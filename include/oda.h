@@ -451,7 +451,8 @@ oda_status oda_argmax(int32_t batch, int32_t n, const float *x, int32_t *index, 
  * group_start[j + 1] - 1]; the first prefix_blocks[j] entries of all their block
  * table rows name the same blocks (the call reads the first attended member's).
  * prefix_blocks[j] == 0: a group that shares nothing, such as a single request.
- * A request belongs to one group; requests in none are left alone. */
+ * A request belongs to one group and is listed once; requests in none are left
+ * alone. */
 typedef struct {
   int32_t num_groups;           /* 1..2048                                          */
   int32_t tokens;               /* T: current tokens per request, 1..16             */
@@ -551,7 +552,8 @@ typedef struct {
   const int32_t *draft_tokens; /* int32 [batch][K]; NULL iff K == 0                  */
   const int32_t *n_drafts;     /* int32 [batch], clamped to [0, K]; NULL: K each     */
   const float *temperature;    /* fp32 [batch]; NULL: 1.  Above 0: softmax of logits /
-                                  temperature; else (0, negative, NaN) greedy       */
+                                  temperature, clamped to [2^-100, 2^100]; else (0,
+                                  negative, NaN) greedy                             */
   const float *uniform;        /* fp32 [batch][K + 1] in [0, 1): u_0..u_{K-1} for the
                                   drafts, u_K for the next token                    */
 } oda_verify_desc;
@@ -573,8 +575,8 @@ oda_status oda_verify_workspace_size(int32_t batch, int32_t vocab, int32_t max_d
  *               then -1
  * A draft outside [0, V) is refused.  A row with no logit above -infinity
  * refuses its draft and gives the next token -1; logits of +infinity share the
- * row's probability evenly.  Weights and sums are fp64.  Rows past n_drafts are
- * not read.  work_list / n_work as in oda_dense_bf16. */
+ * row's probability evenly.  Weights and sums are fp64 (weights below 2^-1000 of
+ * the row's largest are 0).  Rows past n_drafts are not read.  work_list / n_work as in oda_dense_bf16. */
 oda_status oda_verify_drafts(const oda_verify_desc *desc, int32_t batch, int32_t *n_accepted, int32_t *tokens,
                              const int32_t *work_list, const int32_t *n_work, void *workspace,
                              size_t workspace_bytes, hipStream_t stream);

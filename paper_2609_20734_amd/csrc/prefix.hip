@@ -1056,7 +1056,8 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
 // ---------------------------------------------------------------------------
 
 // Sizes that host and plan agree on.  Items beyond one per piece fill the CUs
-// twice; each of them has at most kMaxCols partial columns.
+// twice; each of them has at most kMaxCols partial columns, and no more than the
+// batch has.
 struct Sizes {
   int group, chunk_cols, extra_items, part_cols, max_items;
   size_t plan_bytes, off_ml, ws_bytes;
@@ -1078,7 +1079,7 @@ oda_status sizes_of(const oda_attn_shape* s, const oda_prefix_groups* p, Sizes* 
   z->chunk_cols = kMaxCols / z->group * z->group;
   const int64_t cols = (int64_t)s->batch * p->tokens * z->group;
   z->extra_items = (int)oda::ceil_div(2 * kCus, units);
-  z->part_cols = (int)(2 * cols + (int64_t)z->extra_items * kMaxCols);
+  z->part_cols = (int)(2 * cols + (int64_t)z->extra_items * std::min<int64_t>(kMaxCols, cols));
   z->max_items = (int)(s->batch + std::min<int64_t>(p->num_groups, s->batch) + cols / z->chunk_cols + z->extra_items);
   z->plan_bytes = (size_t)oda::round_up(
       (items_at(s->batch * p->tokens) + (int64_t)z->max_items * (int64_t)(sizeof(Item) / 4)) * 4, 256);
