@@ -14,6 +14,8 @@ starting from the exact input values (bf16 and fp32 widen to fp64 exactly):
                     the decision rule of §2.1 / Alg. 1 and its compaction;
 * ``step``       -- one decode step (Alg. 1, attention part): Local, score,
                     conditional Full, selected output (App. A.5);
+* ``drafts``     -- adapters beside dense layers, verification and commit of
+                    drafted tokens, attention of requests that share a prefix;
 * ``ledger``     -- the bytes each step reads (App. A.6 and B.7 accounting).
 
 Parity status: every function is pinned by ``tests/test_oracle_*.py`` except

@@ -3,9 +3,11 @@
 The product is the C-ABI library ``liboda.so`` (include/oda.h): hand-written
 HIP kernels for Local decode attention (over the paged cache, or over the
 direct-ring workspace), the recall gate with its device predicate, Full
-decode attention for flagged requests only, the selected-state commit, and
-the decoder layers around them (``decoder`` composes a whole
-synthetic decode step from those entry points).  This package
+decode attention for flagged requests only, the selected-state commit, the
+operators of a step of many tenants with drafted tokens (attention over shared
+prefixes, adapters beside dense layers, verification and commit of drafts), and
+the decoder layers around them (``decoder`` composes whole synthetic decode
+steps from those entry points).  This package
 holds its sources (``csrc/``), its build step (``build.py``), a ctypes
 binding with the same entry-point names (``_lib``), the byte accounting used
 to report bandwidth (``ledger``) and the synthetic workload shapes
@@ -24,8 +26,8 @@ _EXPORTS = ("HEAD_MLP", "HEAD_PAPER", "OdaError", "Shape", "attn_workspace_size"
             "recall_gate_static", "qkv_prep", "prepare_local_qkv", "prepare_full_qkv",
             "ring_elements", "ring_fill", "local_decode_attn_ring", "commit_kv_ring", "prepare_local_ring",
             "prefix_groups", "prefix_plan_size", "prefix_workspace_size", "prefix_plan", "prefix_decode_attn",
-            "prepare_prefix_plan", "prepare_prefix_decode_attn", "lora_desc", "lora_workspace_size", "dense_lora_bf16", "prepare_dense_lora", "verify_desc",
-            "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts")
+            "prepare_prefix_plan", "prepare_prefix_decode_attn", "lora_desc", "lora_workspace_size", "dense_lora_bf16",
+            "prepare_dense_lora", "verify_desc", "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts")
 
 
 def __getattr__(name):

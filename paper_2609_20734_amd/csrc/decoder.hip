@@ -1073,7 +1073,7 @@ extern "C" oda_status oda_dense_lora_bf16(const oda_dense_desc* desc, const oda_
   (void)hipGetLastError();
   // the most rows per workgroup (its wavefronts read the request's input once for
   // them) that leave kShrinkGroups workgroups: 64 rows of 6,144 for 160 requests
-  // 11.0 us with eight rows each, 11.4 with four; 128 rows of 2,048 for 32
+  // 11.0 us with eight rows each, 11.4 with four; 32 rows of 2,048 for 32
   // requests 4.15 with one or two, 4.5 with eight
   const auto leaves = [&](int rows) { return (int64_t)batch * t_rows / rows >= kShrinkGroups; };
   const auto grid = [&](int rows) { return dim3((unsigned)(t_rows / rows), (unsigned)batch); };
