@@ -102,6 +102,8 @@ constexpr float kBlockCost = 8.f;
 constexpr float kItemCost = 160.f;      // start-up, the join and the partial's share of the merge
 constexpr float kLeastCost = 16 * kBlockCost;   // shortest split: two blocks per wavefront
 
+constexpr int kBuckets = 32;
+
 // What the plan holds in LDS per slot (place in `members`), per group and per
 // piece of work (the groups' prefixes, then the slots' own blocks).
 struct PlanSlot {
@@ -175,11 +177,13 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
   __shared__ int2 s_wave[kPlanThreads / 64];
   __shared__ float s_sum[kPlanThreads / 64], s_most[kPlanThreads / 64];
   __shared__ int s_count[kPlanThreads / 64][64];
+  __shared__ int s_bucket[kBuckets];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   PlanHeader* head = reinterpret_cast<PlanHeader*>(a.plan);
   Row* rows = reinterpret_cast<Row*>(a.plan + rows_at());
   Item* items = reinterpret_cast<Item*>(a.plan + items_at(a.B * a.T));
 
+  if (tid < kBuckets) s_bucket[tid] = 0;
   // the first round of members comes with the group arrays
   int member = tid < a.B ? a.members[tid] : -1;
   // group starts, kept in [0, B] and ascending whatever the array holds
@@ -317,7 +321,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
   int n_items = 0, n_part = 0;
   for (int i0 = 0; i0 < n_pieces; i0 += kPlanThreads) {
     const int i = i0 + tid;
-    int splits = 0, cols = 0, chunks = 0;
+    int splits = 0, cols = 0, chunks = 0, bucket = 0;
     if (i < n_pieces) {
       chunks = i < a.NG ? groups[i].chunks : 1;
       splits = split_count(pieces[i].cost, inv_best);
@@ -326,6 +330,9 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
         const int blocks = i < a.NG ? groups[i].blocks : own_blocks(slots[i - a.NG]);
         const int length = split_length(blocks, splits);
         splits = (blocks + length - 1) / length;
+        const float cost = pieces[i].cost * (float)min(length, blocks) / (float)blocks;
+        bucket = min(max((int)((1.f - cost * inv_best) * (float)kBuckets), 0), kBuckets - 1);
+        atomicAdd(&s_bucket[bucket], chunks * splits);
       }
     }
     int2 total;
@@ -333,10 +340,32 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
     if (i < n_pieces) {
       pieces[i].splits = splits;
       pieces[i].item = n_items + at.x;
+      pieces[i].cost = (float)bucket;
       pieces[i].part = n_part + at.y;
     }
     n_items += total.x;
     n_part += total.y;
+  }
+  // More than one round of items: listed by their cost, the largest first (in
+  // kBuckets steps, within one in any order), so that the launch ends evenly (32
+  // requests behind 16,384 positions 56.7 us against 60.1; the places cost 0.35).
+  if ((int64_t)a.units * n_items > kCus) {
+    __syncthreads();
+    if (tid < 64) {
+      int v = lane < kBuckets ? s_bucket[lane] : 0;
+      const int own = v;
+#pragma unroll
+      for (int s = 1; s < kBuckets; s <<= 1) {
+        const int y = __shfl_up(v, s);
+        if (lane >= s) v += y;
+      }
+      if (lane < kBuckets) s_bucket[lane] = v - own;
+    }
+    __syncthreads();
+    for (int i = tid; i < n_pieces; i += kPlanThreads) {
+      const PlanPiece p = pieces[i];
+      if (p.splits > 0) pieces[i].item = atomicAdd(&s_bucket[(int)p.cost], p.splits * (i < a.NG ? groups[i].chunks : 1));
+    }
   }
   __syncthreads();
   for (int j = 0; j < a.NG; ++j) {
