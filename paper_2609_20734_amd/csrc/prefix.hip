@@ -460,8 +460,9 @@ struct PrefixArgs {
 };
 
 __device__ __forceinline__ bool plan_fits(const PrefixArgs& a, const PlanHeader& h) {
-  return h.magic == kMagic && h.batch == a.B && h.tokens == a.T && h.group == a.G && h.max_blocks == a.MB &&
-         h.cached == (a.k_cur == nullptr ? 1 : 0) && h.part_cols == a.part_cols;
+  // (no short cuts: each would be a wait of its own)
+  return (h.magic == kMagic) & (h.batch == a.B) & (h.tokens == a.T) & (h.group == a.G) & (h.max_blocks == a.MB) &
+         (h.cached == (a.k_cur == nullptr ? 1 : 0)) & (h.part_cols == a.part_cols);
 }
 
 __device__ __forceinline__ bf16x8 load16(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
@@ -592,20 +593,38 @@ __device__ __forceinline__ u32x2 mask_values(int room, u32x2 v) {
   return u32x2{v.x & w0, v.y & w1};
 }
 
-// The queries of a wavefront's column tiles as B operands.
-template <int D, int N>
-__device__ __forceinline__ void load_queries(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int tile0,
-                                             bf16x8 (&qf)[N][D / 32]) {
-  const int lane = threadIdx.x & 63, h16 = lane & 15, j = lane >> 4;
+// The queries of a wavefront's column tiles as B operands, in two steps, so that
+// the rows' ids and the first table entries come in one trip to memory.
+template <int N>
+struct QueryRows {
+  int id[N], head[N];
+  bool in[N];
+};
+template <int N>
+__device__ __forceinline__ void find_rows(const PrefixArgs& a, const Item& it, const Row* rows, int tile0, QueryRows<N>& q) {
+  const int h16 = threadIdx.x & 15;
 #pragma unroll
   for (int c = 0; c < N; ++c) {
     const int col = (tile0 + c) * kBlock + h16;
-    const bool in = col < it.ncols;
-    const int at = in ? it.col0 + col : it.col0;
-    const int row = at / a.G, h = at - row * a.G;
-    const uint16_t* q = a.q + (((int64_t)l * a.B * a.T + rows[it.row0 + row].id) * a.Hq + g * a.G + h) * D;
+    q.in[c] = col < it.ncols;
+    const int at = q.in[c] ? it.col0 + col : it.col0;
+    const int row = at / a.G;
+    q.head[c] = at - row * a.G;
+    q.id[c] = rows[it.row0 + row].id;
+  }
+}
+template <int D, int N>
+__device__ __forceinline__ void load_queries(const PrefixArgs& a, const QueryRows<N>& r, int l, int g,
+                                             bf16x8 (&qf)[N][D / 32]) {
+  const int j = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) qf[c][kk] = in ? load16(q + 32 * kk + 8 * j) : bf16x8{};
+  for (int c = 0; c < N; ++c) {
+    const uint16_t* q = a.q + (((int64_t)l * a.B * a.T + r.id[c]) * a.Hq + g * a.G + r.head[c]) * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) qf[c][kk] = load16(q + 32 * kk + 8 * j);
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk)
+      if (!r.in[c]) qf[c][kk] = bf16x8{};
   }
 }
 
@@ -699,14 +718,17 @@ __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, 
     const uint16_t* vbase = a.v_cache + base + h16 * kBlock + 4 * j;
     const int32_t* table = a.block_table + (int64_t)it.request * a.MB;
     const int64_t blk_stride = (int64_t)a.Hkv * kBlock * D;
+    int tbl = 0, bad = 0, entry = lo + lane < hi ? table[lo + lane] : 0;
+    QueryRows<N> qr;
+    find_rows<N>(a, it, rows, 0, qr);
     bf16x8 qf[N][KK];
-    load_queries<D, N>(a, it, rows, l, g, 0, qf);
-    int tbl = 0, bad = 0;
+    load_queries<D, N>(a, qr, l, g, qf);
     auto pair = [&](int v, auto masked) {
       constexpr bool kMasked = decltype(masked)::value;
       const int i0 = (v - lo) & 63;
       if (i0 == 0) {
-        const int e = v + lane < hi ? table[v + lane] : 0;
+        if (v != lo) entry = v + lane < hi ? table[v + lane] : 0;
+        const int e = entry;
         const bool ok = e >= 0 && e < a.num_blocks;
         bad |= ok ? 0 : 1;
         tbl = ok ? e : 0;
@@ -785,8 +807,6 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
   const bool active = wc * N * kBlock < it.ncols;
   WaveState<D, N> w;
   w.clear();
-  bf16x8 qf[N][KK];
-  load_queries<D, N>(a, it, rows, l, g, wc * N, qf);
 
   const int64_t base = (int64_t)l * a.kv_layer_stride + (int64_t)g * kElems;
   // staged slot lane % 16 of a 16-position row of K holds position (bits 0, 1, 3, 2 of the slot)
@@ -795,12 +815,17 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
   const int64_t blk_stride = (int64_t)a.Hkv * kElems;
   const int blocks = it.blk_hi - it.blk_lo;
   const int stages = (blocks + kWaves - 1) / kWaves;
-  int tbl = 0, bad = 0;
+  int tbl = 0, bad = 0, entry = lane * kWaves + wave < blocks ? table[lane * kWaves] : 0;
+  QueryRows<N> qr;
+  find_rows<N>(a, it, rows, wc * N, qr);
+  bf16x8 qf[N][KK];
+  load_queries<D, N>(a, qr, l, g, qf);
   bf16x8 kr[kLoads], vr[kLoads];
   // a stage's block of this wavefront; past the end the cache's first (masked, and zeroed where V is used)
   auto fetch = [&](int st) {
     if ((st & 63) == 0) {
-      const int e = (st + lane) * kWaves + wave < blocks ? table[(st + lane) * kWaves] : 0;
+      if (st > 0) entry = (st + lane) * kWaves + wave < blocks ? table[(st + lane) * kWaves] : 0;
+      const int e = entry;
       const bool ok = e >= 0 && e < a.num_blocks;
       bad |= ok ? 0 : 1;
       tbl = ok ? e : 0;
@@ -921,12 +946,14 @@ template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void prefix_split_kernel(PrefixArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const PlanHeader& h = *reinterpret_cast<const PlanHeader*>(a.plan);
+  const PlanHeader h = *reinterpret_cast<const PlanHeader*>(a.plan);
   const int units = a.L * a.Hkv;
   const int i = blockIdx.x / units, u = blockIdx.x - i * units;
-  if (!plan_fits(a, h) || i >= min(h.n_items, a.max_items)) return;
   const Row* rows = reinterpret_cast<const Row*>(a.plan + rows_at());
+  // (asked for with the header: the grid has no more than the buffer's items; none
+  // has no columns, so the item is read before the branch)
   const Item it = reinterpret_cast<const Item*>(a.plan + items_at(a.B * a.T))[i];
+  if (!plan_fits(a, h) | (i >= min(h.n_items, a.max_items)) | (it.ncols <= 0)) return;
   const int l = u / a.Hkv, g = u - l * a.Hkv;
   const int tiles = (it.ncols + kBlock - 1) / kBlock;
   if (tiles == 1) run_narrow<D, 1>(a, it, rows, l, g, smem);
@@ -961,19 +988,16 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
   if (l >= a.L) return;
   const int rest = (int)(wave - l * per_layer);
   const int r = rest / a.Hq, head = rest - r * a.Hq;
-  const PlanHeader& h = *reinterpret_cast<const PlanHeader*>(a.plan);
+  const PlanHeader h = *reinterpret_cast<const PlanHeader*>(a.plan);
   const Row* rows = reinterpret_cast<const Row*>(a.plan + rows_at());
   const int all = a.B * a.T;
-  int64_t id = r;
-  const bool fits = plan_fits(a, h);
-  bool nan = !fits;                         // a plan of other sizes, or none
-  if (fits) {
-    if (r < h.n_rows) id = rows[r].id;
-    else if (r >= all - h.n_bad) {
-      id = rows[r].id;
-      nan = true;
-    } else return;
-  }
+  const Row row = rows[r];
+  const bool fits = plan_fits(a, h);        // (else a plan of other sizes, or none)
+  const bool has = r < h.n_rows, spoiled = r >= all - h.n_bad;
+  // (a planned row's id is never negative: read before the branch)
+  if (fits & ((!has & !spoiled) | (row.id < 0))) return;
+  const int64_t id = fits ? row.id : r;
+  const bool nan = !fits | !has;
   float* out = a.out + (((int64_t)l * all + id) * a.Hq + head) * D + lane * PD;
   float* lse = a.lse ? a.lse + ((int64_t)l * all + id) * a.Hq + head : nullptr;
   if (nan) {
@@ -982,13 +1006,44 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
     if (lse && lane == 0) *lse = __builtin_nanf("");
     return;
   }
-  const Row row = rows[r];
   const int g = head / a.G, hh = head - g * a.G;
   const int64_t part0 = (int64_t)(l * a.Hkv + g) * a.part_cols + hh;
   const int b = (int)(id / a.T), t = (int)(id - (int64_t)b * a.T);
   float q[PD];
 #pragma unroll
   for (int e = 0; e < PD; ++e) q[e] = bf16_to_float(a.q[(((int64_t)l * all + id) * a.Hq + head) * D + lane * PD + e]);
+
+  // the current tokens this row attends: candidates, or the cache's last positions;
+  // the first one's values are asked for before the partials, each next one's
+  // before one is used
+  const int more = a.k_cur ? t + 1 : t;
+  float k_next[PD] = {}, v_next[PD] = {};
+  bool bad = false;
+  auto fetch = [&](int i) {
+    if (a.k_cur) {
+      const int64_t at = ((((int64_t)l * a.B + b) * a.T + i) * a.Hkv + g) * D + lane * PD;
+#pragma unroll
+      for (int e = 0; e < PD; ++e) {
+        k_next[e] = bf16_to_float(a.k_cur[at + e]);
+        v_next[e] = bf16_to_float(a.v_cur[at + e]);
+      }
+    } else {
+      const int pos = row.len + i;          // below the table's end: the plan checked the length
+      const int blk = a.block_table[(int64_t)b * a.MB + pos / kBlock];
+      if (blk < 0 || blk >= a.num_blocks) {
+        bad = true;
+        return;
+      }
+      const int64_t at = (int64_t)l * a.kv_layer_stride + ((int64_t)blk * a.Hkv + g) * kBlock * D;
+#pragma unroll
+      for (int e = 0; e < PD; ++e) {
+        const int d = lane * PD + e;
+        k_next[e] = bf16_to_float(a.k_cache[at + ((d / 8) * kBlock + pos % kBlock) * 8 + d % 8]);
+        v_next[e] = bf16_to_float(a.v_cache[at + d * kBlock + pos % kBlock]);
+      }
+    }
+  };
+  if (more > 0) fetch(0);
 
   float M = -INFINITY, sum = 0.f, o[PD] = {};
   // weights against a new largest logit
@@ -1037,34 +1092,14 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
       }
     }
   }
-  // the current tokens this row attends: candidates, or the cache's last positions
-  const int more = a.k_cur ? t + 1 : t;
-  bool bad = false;
   for (int i = 0; i < more; ++i) {
-    float kd[PD], vd[PD];
-    if (a.k_cur) {
-      const int64_t at = ((((int64_t)l * a.B + b) * a.T + i) * a.Hkv + g) * D + lane * PD;
+    float kd[PD], vd[PD], dot = 0.f;
 #pragma unroll
-      for (int e = 0; e < PD; ++e) {
-        kd[e] = bf16_to_float(a.k_cur[at + e]);
-        vd[e] = bf16_to_float(a.v_cur[at + e]);
-      }
-    } else {
-      const int pos = row.len + i;          // below the table's end: the plan checked the length
-      const int blk = a.block_table[(int64_t)b * a.MB + pos / kBlock];
-      if (blk < 0 || blk >= a.num_blocks) {
-        bad = true;
-        continue;
-      }
-      const int64_t at = (int64_t)l * a.kv_layer_stride + ((int64_t)blk * a.Hkv + g) * kBlock * D;
-#pragma unroll
-      for (int e = 0; e < PD; ++e) {
-        const int d = lane * PD + e;
-        kd[e] = bf16_to_float(a.k_cache[at + ((d / 8) * kBlock + pos % kBlock) * 8 + d % 8]);
-        vd[e] = bf16_to_float(a.v_cache[at + d * kBlock + pos % kBlock]);
-      }
+    for (int e = 0; e < PD; ++e) {
+      kd[e] = k_next[e];
+      vd[e] = v_next[e];
     }
-    float dot = 0.f;
+    if (i + 1 < more) fetch(i + 1);
 #pragma unroll
     for (int e = 0; e < PD; ++e) dot += q[e] * kd[e];
     dot = wave_sum(dot) * a.scale_log2;
