@@ -82,8 +82,8 @@ __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int b) {
 }
 // log2(e) / temperature, 0 for greedy.  Temperatures count as at most 2^100 and at
 // least 2^-100, where logits a step of fp32 apart no longer or fully differ.
-__device__ __forceinline__ double slope_of(const VerifyArgs& a, int b) {
-  const float t = a.temperature ? a.temperature[b] : 1.f;
+__device__ __forceinline__ float temperature_of(const VerifyArgs& a, int b) { return a.temperature ? a.temperature[b] : 1.f; }
+__device__ __forceinline__ double slope_of(float t) {
   return t > 0.f ? kLog2e / (double)fminf(fmaxf(t, 0x1p-100f), 0x1p100f) : 0.0;
 }
 
@@ -198,8 +198,11 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyArgs a) {
   __shared__ int s_first[kThreads / 64];
   const int split = blockIdx.x, i = blockIdx.y;
   int b;
-  if (!selected_request(a, blockIdx.z, b) || i > drafts_of(a, b)) return;
-  const double slope = slope_of(a, b);
+  if (!selected_request(a, blockIdx.z, b)) return;
+  const int n = drafts_of(a, b);
+  const float t = temperature_of(a, b);
+  if (i > n) return;
+  const double slope = slope_of(t);
   const bool greedy = slope == 0.0;
   const float* row = a.logits + ((int64_t)b * (a.K + 1) + i) * a.V;
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
@@ -271,12 +274,15 @@ struct RowStat {
   double part;      // of this lane's split
   int first;        // greedy: the first index of the largest
 };
-__device__ __forceinline__ RowStat join_row(const VerifyArgs& a, int b, int i, int lane, bool greedy, double slope) {
+__device__ __forceinline__ SplitStat split_of(const VerifyArgs& a, int b, int i, int lane) {
   SplitStat s;
   s.top = -INFINITY;
   s.sum = 0.0;
   s.first = INT_MAX;
   if (lane < a.splits) s = a.stats[((int64_t)b * (a.K + 1) + i) * a.splits + lane];
+  return s;
+}
+__device__ __forceinline__ RowStat join_row(const SplitStat& s, bool greedy, double slope) {
   RowStat r;
   r.top = wave_max(s.top);
   r.part = r.top == -INFINITY || greedy ? 0.0 : s.sum * rescale(s.top, r.top, slope);
@@ -420,7 +426,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   __shared__ double s_sum[kMaxDrafts + 1];
   __shared__ float s_top[kMaxDrafts + 1];
   __shared__ int s_first[kMaxDrafts + 1];
-  __shared__ int s_ok[kMaxDrafts + 1];
+  __shared__ int s_ok[kMaxDrafts + 1], s_token[kMaxDrafts + 1];
   __shared__ double s_scan[kWaves];
   __shared__ FindScratch s_find;
   __shared__ int s_from_p, s_split, s_last;
@@ -429,26 +435,38 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   int b;
   if (!selected_request(a, slot, b)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const double slope = slope_of(a, b);
-  const bool greedy = slope == 0.0;
   const int n = drafts_of(a, b);
+  const float temperature = temperature_of(a, b);
   const float* u = a.uniform + (int64_t)b * (a.K + 1);
+  const float u_next = u[a.K];
+  // (the token and number of a wavefront's first row come with the counts)
+  const int first = min(wave, a.K);
+  int x_i = first < a.K ? a.draft_tokens[(int64_t)b * a.K + first] : -1;
+  float u_i = u[first];
+  const double slope = slope_of(temperature);
+  const bool greedy = slope == 0.0;
 
   // every row's splits joined, every draft decided (by each workgroup alike)
   for (int i = wave; i <= n; i += kWaves) {
     // the draft's own logit and probability come beside the splits
-    const int x = i < n ? uniform(a.draft_tokens[(int64_t)b * a.K + i]) : -1;
+    const SplitStat s = split_of(a, b, i, lane);
+    if (i > wave && i < n) {
+      x_i = a.draft_tokens[(int64_t)b * a.K + i];
+      u_i = u[i];
+    }
+    const int x = i < n ? uniform(x_i) : -1;
     const bool known = x >= 0 && x < a.V;
     const float z = known ? a.logits[((int64_t)b * (a.K + 1) + i) * a.V + x] : 0.f;
     const float qx = known && a.draft_probs ? a.draft_probs[((int64_t)b * a.K + i) * a.V + x] : 1.f;
-    const RowStat r = join_row(a, b, i, lane, greedy, slope);
+    const RowStat r = join_row(s, greedy, slope);
     if (lane != 0) continue;
     int ok = 0;
     if (known && r.top != -INFINITY) {
       const double p = greedy ? (x == r.first ? 1.0 : 0.0) : weight(weights_against(r.top, slope), z) / r.sum;
-      ok = (double)u[i] * (double)fmaxf(qx, 0.f) < p ? 1 : 0;
+      ok = (double)u_i * (double)fmaxf(qx, 0.f) < p ? 1 : 0;
     }
     s_ok[i] = ok;
+    s_token[i] = x;
     s_top[i] = r.top;
     s_sum[i] = r.sum;
     s_first[i] = r.first;
@@ -462,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   d.row = a.logits + ((int64_t)b * (a.K + 1) + j) * a.V;
   d.residual = refused && !greedy;
   d.q = d.residual && a.draft_probs ? a.draft_probs + ((int64_t)b * a.K + j) * a.V : nullptr;
-  d.skip = d.residual && !a.draft_probs ? a.draft_tokens[(int64_t)b * a.K + j] : -1;
+  d.skip = d.residual && !a.draft_probs ? s_token[j] : -1;
   d.w = weights_against(top, slope);
   d.scale = 1.0 / s_sum[j];
   const int begin = min(a.V, split * a.draw_chunk), end = min(a.V, begin + a.draw_chunk);
@@ -510,9 +528,9 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         all = wave_sum(part);
         from_p = !(all > 0.0);
       }
-      if (from_p) part = join_row(a, b, j, lane, false, slope).part;
+      if (from_p) part = join_row(split_of(a, b, j, lane), false, slope).part;
       const double upto = wave_scan(part);
-      const double goal = (double)u[a.K] * lane_value(upto, 63);
+      const double goal = (double)u_next * lane_value(upto, 63);
       const uint64_t past = __ballot(upto > goal && part > 0.0);
       const uint64_t some = __ballot(part > 0.0);
       const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
@@ -532,7 +550,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
   }
   int32_t* out = a.tokens + (int64_t)b * (a.K + 1);
   for (int i = tid; i <= a.K; i += kThreads)
-    out[i] = i < j ? a.draft_tokens[(int64_t)b * a.K + i] : i == j ? token : -1;
+    out[i] = i < j ? s_token[i] : i == j ? token : -1;
   if (tid == 0) a.n_accepted[b] = j;
 }
 
