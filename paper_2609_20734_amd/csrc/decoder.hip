@@ -551,10 +551,16 @@ void dense_mfma_kernel(Args p) {
         *reinterpret_cast<u32x4*>(&sm.w[wave][s][kMfmaRows / kWLoads * i + lane / kWLanes][8 * (lane % kWLanes)]) = w[s][i];
     }
   };
+  auto weights = [&](int u, int s) { return *reinterpret_cast<const bf16x8*>(&sm.w[wave][s][h][32 * u + 8 * j]); };
+  // (one tile of requests reads each operand where it is used: held for all
+  // streams they cost the second workgroup of a CU, 2048 -> 151936 142 us
+  // instead of 106)
   auto step = [&](int u) {
-    bf16x8 ws[S];
+    bf16x8 held[S];
+    if (T > 1) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) ws[s] = *reinterpret_cast<const bf16x8*>(&sm.w[wave][s][h][32 * u + 8 * j]);
+      for (int s = 0; s < S; ++s) held[s] = weights(u, s);
+    }
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       float xv[8];
@@ -569,9 +575,10 @@ void dense_mfma_kernel(Args p) {
       split_bf16x3(xv, px);
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        acc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[0], acc[t][s], 0, 0, 0);
-        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[2], low[t][s], 0, 0, 0);
-        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[s], px[1], low[t][s], 0, 0, 0);
+        const bf16x8 ws = T > 1 ? held[s] : weights(u, s);
+        acc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[0], acc[t][s], 0, 0, 0);
+        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[2], low[t][s], 0, 0, 0);
+        low[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, px[1], low[t][s], 0, 0, 0);
       }
     }
   };
@@ -928,19 +935,24 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
   const auto groups_of = [&](int tiles, int edge) {
     return oda::ceil_div(N, tiles * edge) * oda::ceil_div(a.B, edge);
   };
-  // Where that leaves more than two rounds, one of workgroups with 64 rows and 32
-  // requests takes as long as two of those with 32 and 16 (2048 -> 4096: 96
-  // requests 16.7 us against 22.4, 64 requests 15.9 against 15.5; 6144 -> 2048: 160
-  // requests 31.5 against 36.0, 128 requests 30.6 against 27.0; 2048 -> 151936, 160
-  // requests 760 against 1241).  The SwiGLU pair has no room for it: half the rows
-  // were slower than three tiles up to 64 requests and within 8% above.
-  // Of 48 rows and 32 requests where that takes no more rounds than 64 rows (6144 ->
-  // 2048, 160 requests 28.8 us against 31.5; 2048 -> 4096, 96 requests two rounds
-  // instead of one 26.7 against 16.5).
+  // Where that leaves more than two rounds (two such workgroups share a CU), one
+  // round of workgroups with 64 rows and 32 requests takes no longer than two
+  // (2048 -> 4096: 96 requests 16.3 us against 17.6, 64 requests 14.4 against 12.7;
+  // 6144 -> 2048: 160 requests 31.5 against 35.8, 128 requests 30.6 against 27.1).
+  // Over several rounds the narrow ones' even end counts for less, and rows below
+  // 4096 have to save three (2048 -> 151936: 160 requests 766 us against 899, 48
+  // requests 342 against 336; 2048 -> 4096: 160 requests 28.3 against 27.1; 4096 ->
+  // 6144: 128 requests 48.6 against 55.3).  Of 48 rows and 32 requests where that
+  // takes no more rounds than 64 rows (6144 -> 2048, 160 requests 28.1 us against
+  // 31.5; 2048 -> 4096, 96 requests two rounds instead of one 26.7 against 16.3).
+  // The SwiGLU pair has no room for 64 rows: 32 were slower than three tiles up to
+  // 64 requests and within 8% above.
   const auto wide_rounds_of = [&](int tiles) {
     return oda::ceil_div(oda::ceil_div(N, tiles * kMfmaRows) * oda::ceil_div(a.B, 2 * kMfmaRows), kTargetGroups);
   };
-  const int64_t wide_rounds = wide_rounds_of(4);
+  const int64_t wide_rounds = wide_rounds_of(4), narrow = groups_of(2, kMfmaRows);
+  const bool wide = wide_rounds == 1 || a.K >= 4096 ? narrow > 2 * kTargetGroups * wide_rounds
+                                                    : narrow >= 3 * kTargetGroups * wide_rounds;
   const bool one = !swiglu && groups_of(2, kMfmaRows) >= 8 * kTargetGroups && a.K >= 3 * kMfmaWaves * kChunk &&
                    a.K % (kMfmaWaves * kChunk) == 0;
   if ((a.B > 1 || one) && a.K < kMfmaMaxK) {
@@ -957,7 +969,7 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
       if (fits(1, 8)) st = launch_dense_mfma<false, 1, 1, true>(a, stream);
       else if (fits(2, 8)) st = launch_dense_mfma<false, 2, 1, true>(a, stream);
       else if (fits(1, kMfmaRows)) st = launch_dense_mfma<false, 1, 1, false>(a, stream);
-      else if (groups_of(2, kMfmaRows) > 2 * kTargetGroups * wide_rounds)
+      else if (wide)
         st = wide_rounds_of(3) == wide_rounds ? launch_dense_mfma<false, 3, 2, false>(a, stream)
                                               : launch_dense_mfma<false, 4, 2, false>(a, stream);
       else st = launch_dense_mfma<false, 2, 1, false>(a, stream);

@@ -28,18 +28,19 @@ def _rounds(N, B, rows):
     return -(-(-(-N // rows) * -(-B // 32)) // TARGET)
 
 
-def _is_wide(N, B):
-    return _groups(N, B, 2, 16) > 2 * TARGET * _rounds(N, B, 64)
+def _is_wide(K, N, B):
+    narrow, rounds = _groups(N, B, 2, 16), _rounds(N, B, 64)
+    return narrow > 2 * TARGET * rounds if rounds == 1 or K >= 4096 else narrow >= 3 * TARGET * rounds
 
 
 CASES = [(8, 8000, 33), (72, 4100, 96), (40, 8191, 64), (264, 8000, 37), (1000, 5003, 61), (520, 16380, 17),
-         (2088, 4161, 159), (264, 4300, 84), (1000, 8150, 150)]
+         (2088, 4113, 95), (264, 4300, 84), (1000, 8150, 160), (4104, 6100, 90)]
 
 
 def test_the_cases_take_the_wide_tiles_and_their_parts_do_not():
     assert {_rounds(N, B, 48) == _rounds(N, B, 64) for _, N, B in CASES} == {True, False}   # of 48 rows and of 64
-    for _, N, B in CASES:
-        assert _is_wide(N, B) and not _is_wide(N, 16) and _groups(N, 16, 1, 16) > TARGET, (N, B)
+    for K, N, B in CASES:
+        assert _is_wide(K, N, B) and not _is_wide(K, N, 16) and _groups(N, 16, 1, 16) > TARGET, (N, B)
 
 
 def _layer(seed, K, N, B, norm, residual):
@@ -125,11 +126,11 @@ def test_nonfinite_values_stay_where_they_are():
 
 @pytest.mark.parametrize("norm", [False, True])
 @pytest.mark.parametrize("K,parts,rank,B", [(264, [8000], 8, 40), (520, [2111, 5, 1987], 64, 94), (72, [8191], 24, 47),
-                                              (136, [4096], 40, 160)])
+                                              (136, [5003], 40, 61)])
 def test_adapters_beside_wide_tiles(K, parts, rank, B, norm):
     P = need_gpu()
     N, A = sum(parts), 3
-    assert _is_wide(N, B)
+    assert _is_wide(K, N, B)
     g, W, x, gain, r = _layer(K + N, K, N, B, norm, True)
     a = S.normal_bf16(g, (A, len(parts) * rank, K), K ** -0.5)
     b = S.normal_bf16(g, (A, N, rank), rank ** -0.5)
