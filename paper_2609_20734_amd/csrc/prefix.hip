@@ -532,7 +532,8 @@ __device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
 
 // Scores of 32 positions of column h16 (this lane: 4j.. of either block) into the
 // online softmax; p comes back as kParts bf16 parts.  Two parts keep 16 bits of
-// each weight (rms error 2.4e-6 of a sum of random values), three all of them.
+// each weight (rms error 2.4e-6 of a sum of random values), three all of them; see
+// kTwoPartLength.
 //
 // Weights are taken against the column's reference, which need not be the largest
 // score so far: fp32 and bf16 hold weights up to 2^kHeadroom as well as those
@@ -801,10 +802,10 @@ __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, 
 // with the positions of K ordered so that operand reads are free of bank
 // conflicts.  Up to four tiles: two position ranges, which share a stage's pairs alternately;
 // more: every wavefront goes through all pairs with its N tiles.
-template <int D, int N>
+template <int D, int N, int kParts>
 __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int wc_shift,
                                          char* smem) {
-  constexpr int KK = D / 32, NT = D / 16, kParts = N == 1 ? 3 : 2;
+  constexpr int KK = D / 32, NT = D / 16;
   constexpr int kLoads = block_bytes(D) / 1024;      // 16-byte loads of a block per lane
   constexpr int kElems = kBlock * D;                 // of a block
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -951,6 +952,12 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
   }
 }
 
+// More than 128 columns (where the products bound the item) over this many
+// positions take weights of two parts, whose error, 2.4e-6, is then that of a
+// product summed in fp32 (1.1e-6 at 16,384 positions, 2.5e-6 at 65,536); all else
+// takes three (3e-7): 64 requests behind 65,536 positions 405 us against 484.
+constexpr int kTwoPartLength = 49152;
+
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void prefix_split_kernel(PrefixArgs a) {
@@ -967,8 +974,9 @@ void prefix_split_kernel(PrefixArgs a) {
   const int tiles = (it.ncols + kBlock - 1) / kBlock;
   if (tiles == 1) run_narrow<D, 1>(a, it, rows, l, g, smem);
   else if (tiles == 2) run_narrow<D, 2>(a, it, rows, l, g, smem);
-  else if (tiles <= kWaves) run_wide<D, 1>(a, it, rows, l, g, tiles <= 4 ? 2 : 3, smem);
-  else run_wide<D, 2>(a, it, rows, l, g, 3, smem);
+  else if (tiles <= kWaves) run_wide<D, 1, 3>(a, it, rows, l, g, tiles <= 4 ? 2 : 3, smem);
+  else if (it.limit < kTwoPartLength) run_wide<D, 2, 3>(a, it, rows, l, g, 3, smem);
+  else run_wide<D, 2, 2>(a, it, rows, l, g, 3, smem);
 }
 
 __device__ __forceinline__ float wave_sum(float x) {

@@ -368,3 +368,18 @@ def test_random_problems():
         p = Problem(100 + case, groups, Hkv * G, Hkv, D, T=T, L=L, cur=cur, tokens=tokens, poison=True)
         p.upload()
         p.check()
+
+
+@pytest.mark.parametrize("D,blocks,parts", [(64, 3071, 3), (64, 3074, 2), (128, 3074, 2), (128, 900, 3)])
+def test_weights_of_many_columns_on_either_side_of_the_length(D, blocks, parts):
+    """160 and more columns: weights of three parts below 49,152 positions, of two from there on.  Expected error: the
+    fp32 sums of a few splits (3e-7) plus, for two parts, 2^-18 of each weight at most half the time (2.4e-6 rms)."""
+    p = Problem(47, [(blocks, [1, 40, 3, 77, 100, 9, 16, 2, 31, 5])], 16, 1, D, poison=True, spare=1)
+    assert (16 * blocks >= 49152) == (parts == 2)
+    p.upload()
+    got = p.run()
+    p.check(got)
+    ref, _ = OD.prefix_attention(p.q, p.k, p.v, p.table, p.seq, p.scale, p.counts(), p.kc, p.vc, p.attended())
+    rows = p.attended()
+    err = np.linalg.norm(got[0][:, rows] - ref[:, rows]) / np.linalg.norm(ref[:, rows])
+    assert err <= (1e-6 if parts == 3 else 4e-6), err
