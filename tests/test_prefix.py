@@ -1,7 +1,7 @@
 """oda_prefix_plan / oda_prefix_decode_attn against the fp64 oracle: groups, drafts,
 splits, odd sizes, rows that are left alone, bad device data, replays.
 
-Bars are the attention's (tests/harness.py): weights enter the product in two
+Bars are the attention's (tests/harness.py): weights enter the product in two or three
 bf16 parts (2^-18 of each is dropped) and sums are fp32, an expected error of
 about 1e-6 for these inputs."""
 import math
