@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 // V: a thread walks the tokens of one dim, whose slots are neighbours in the
 // block's [D][16] row.  Bound by partly written lines (a token is 2 of a V row's
 // 32 bytes: 32 layers of 32 requests, up to eight tokens each, write 19 MB as 67 MB
-// of lines in 24 us), so the launch has as many wavefronts as the chip holds.
+// of lines in 23 us), so the launch has as many wavefronts as the chip holds.
 struct CommitDraftsArgs {
   uint16_t* k_cache;
   uint16_t* v_cache;
@@ -157,6 +157,21 @@ __device__ __forceinline__ Slot slot_of(const CommitDraftsArgs& a, int b, int64_
   return s;
 }
 
+// Values lo..hi-1 of four neighbouring slots (8-byte aligned).
+__device__ __forceinline__ void store_slots(uint16_t* p, const uint16_t (&v)[4], int lo, int hi) {
+  const uint32_t w0 = (uint32_t)v[0] | (uint32_t)v[1] << 16, w1 = (uint32_t)v[2] | (uint32_t)v[3] << 16;
+  if (lo == 0 && hi == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(w0, w1);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; k += 2) {
+    if (lo <= k && hi >= k + 2) *reinterpret_cast<uint32_t*>(p + k) = k == 0 ? w0 : w1;
+    else if (lo <= k && hi > k) p[k] = v[k];
+    else if (lo <= k + 1 && hi > k + 1) p[k + 1] = v[k + 1];
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArgs a) {
   const int b = blockIdx.x / a.chunks;
   const int c = blockIdx.x - b * a.chunks;
@@ -180,8 +195,7 @@ __global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArg
     if (s.ring >= 0)
       *reinterpret_cast<u32x4*>(a.k_ring + ((((int64_t)l * a.B + b) * nr + s.ring) * a.Hkv + g) * kBlock * a.D + in) = k8;
   }
-  // (the tokens' values of a dim are loaded four at a time, stored two at a time
-  // where they share a word)
+  // (a dim's values go by aligned fours of slots, which share a block and a place)
   const int64_t v_step = (int64_t)a.Hkv * a.D;
   for (int i = threadIdx.x; i < nu * a.D; i += kThreads) {
     const int u = u0 + i / a.D, d = i % a.D;
@@ -189,28 +203,15 @@ __global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArg
     const uint16_t* src = a.v_cand + (((int64_t)l * a.B + b) * a.T * a.Hkv + g) * a.D + d;
     uint16_t* cache = a.v_cache + (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * a.D + d * kBlock;
     uint16_t* ring = a.v_ring + ((int64_t)l * a.B + b) * nr * a.Hkv * kBlock * a.D + (int64_t)g * kBlock * a.D + d * kBlock;
-    for (int t0 = 0; t0 < count; t0 += 4) {
+    for (int t0 = -(int)(pos0 & 3); t0 < count; t0 += 4) {
       uint16_t v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = src[min(t0 + k, count - 1) * v_step];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int t = t0 + k;
-        if (t >= count) break;
-        const Slot s = slot_of(a, b, pos0 + t, last);
-        const bool second = k > 0 && (s.at & 1) != 0;      // already stored with the token before
-        if (s.blk < 0 || second) continue;
-        const bool two = k < 3 && (s.at & 1) == 0 && t + 1 < count;   // (neighbours of one block)
-        const uint32_t w = (uint32_t)v[k] | (uint32_t)v[k < 3 ? k + 1 : k] << 16;
-        uint16_t* p = cache + s.blk * v_step * kBlock + s.at;
-        if (two) *reinterpret_cast<uint32_t*>(p) = w;
-        else *p = v[k];
-        if (s.ring >= 0) {
-          uint16_t* r = ring + s.ring * v_step * kBlock + s.at;
-          if (two) *reinterpret_cast<uint32_t*>(r) = w;
-          else *r = v[k];
-        }
-      }
+      for (int k = 0; k < 4; ++k) v[k] = src[min(max(t0 + k, 0), count - 1) * v_step];
+      const Slot s = slot_of(a, b, pos0 + t0, last);
+      if (s.blk < 0) continue;
+      const int lo = max(0, -t0), hi = min(4, count - t0);
+      store_slots(cache + s.blk * v_step * kBlock + s.at, v, lo, hi);
+      if (s.ring >= 0) store_slots(ring + s.ring * v_step * kBlock + s.at, v, lo, hi);
     }
   }
   if (a.tickets == nullptr) return;
