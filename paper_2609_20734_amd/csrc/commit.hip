@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "oda.h"
+#include "oda_commit_fours.h"
 #include "oda_internal.h"
 
 namespace {
@@ -203,10 +204,10 @@ __global__ __launch_bounds__(kThreads) void commit_drafts_kernel(CommitDraftsArg
     const uint16_t* src = a.v_cand + (((int64_t)l * a.B + b) * a.T * a.Hkv + g) * a.D + d;
     uint16_t* cache = a.v_cache + (int64_t)l * a.kv_layer_stride + (int64_t)g * kBlock * a.D + d * kBlock;
     uint16_t* ring = a.v_ring + ((int64_t)l * a.B + b) * nr * a.Hkv * kBlock * a.D + (int64_t)g * kBlock * a.D + d * kBlock;
-    for (int t0 = -(int)(pos0 & 3); t0 < count; t0 += 4) {
+    for (int t0 = oda::first_four(pos0, count); t0 < count; t0 += 4) {
       uint16_t v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = src[min(max(t0 + k, 0), count - 1) * v_step];
+      for (int k = 0; k < 4; ++k) v[k] = src[oda::token_read(t0, k, count) * v_step];
       const Slot s = slot_of(a, b, pos0 + t0, last);
       if (s.blk < 0) continue;
       const int lo = max(0, -t0), hi = min(4, count - t0);
