@@ -495,8 +495,9 @@ oda_status oda_prefix_plan(const oda_attn_shape *shape, const oda_attn_inputs *i
  * A request whose length (with its current tokens in the cache, their last
  * position) is outside [1, max_seq_len] or shorter than its group's prefix, or
  * that uses a table entry outside [0, num_blocks), gets NaN rows; an entry of the
- * prefix does that to the whole group.  A plan made for other sizes gives NaN
- * throughout.  workspace: >= oda_prefix_workspace_size bytes, 256-byte aligned;
+ * prefix does that to the whole group.  A plan made for another batch, num_groups,
+ * tokens, table width, number of query heads per KV head or kind of candidate
+ * gives NaN throughout.  workspace: >= oda_prefix_workspace_size bytes, 256-byte aligned;
  * calls that may overlap in time need separate ones (a plan may be shared). */
 oda_status oda_prefix_decode_attn(const oda_attn_shape *shape, const oda_attn_inputs *in,
                                   const oda_prefix_groups *groups, const void *plan, size_t plan_bytes, float *out,

@@ -61,7 +61,8 @@ struct PlanHeader {
   uint32_t magic;
   int32_t batch, tokens, group, max_blocks, cached, part_cols;   // what the plan was made for
   int32_t n_items, n_rows, n_bad;    // items; rows with work; rows after them that become NaN
-  int32_t reserved[6];
+  int32_t groups;                    // num_groups, on which the launch's items depend
+  int32_t reserved[5];
 };
 struct Row {
   int32_t id;                        // request * tokens + token
@@ -441,6 +442,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PlanArgs a) {
     h.n_items = n_part <= a.part_cols ? n_items : 0;
     h.n_rows = n_rows;
     h.n_bad = n_bad;
+    h.groups = a.NG;
     *head = h;
   }
 }
@@ -463,7 +465,7 @@ struct PrefixArgs {
   float* part_ml;     // [units][part_cols][2]  (m in log2 units, l)
   int64_t kv_layer_stride;
   int64_t num_blocks;
-  int32_t L, B, T, Hq, Hkv, G, MB;
+  int32_t L, B, T, Hq, Hkv, G, MB, NG;
   int32_t part_cols, max_items;
   float scale_log2;
 };
@@ -471,7 +473,7 @@ struct PrefixArgs {
 __device__ __forceinline__ bool plan_fits(const PrefixArgs& a, const PlanHeader& h) {
   // (no short cuts: each would be a wait of its own)
   return (h.magic == kMagic) & (h.batch == a.B) & (h.tokens == a.T) & (h.group == a.G) & (h.max_blocks == a.MB) &
-         (h.cached == (a.k_cur == nullptr ? 1 : 0)) & (h.part_cols == a.part_cols);
+         (h.cached == (a.k_cur == nullptr ? 1 : 0)) & (h.part_cols == a.part_cols) & (h.groups == a.NG);
 }
 
 __device__ __forceinline__ bf16x8 load16(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
@@ -1311,6 +1313,7 @@ extern "C" oda_status oda_prefix_decode_attn(const oda_attn_shape* shape, const 
   a.Hkv = shape->num_kv_heads;
   a.G = z.group;
   a.MB = shape->max_blocks_per_seq;
+  a.NG = groups->num_groups;
   a.part_cols = z.part_cols;
   a.max_items = z.max_items;
   a.scale_log2 = in->scale * kLog2e;
