@@ -497,8 +497,9 @@ __device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bi
 // V blocks are its B.
 
 // A wavefront's share of N column tiles: O = P V (rows: columns 4j..4j+3 of the
-// tile, 16 n + h16 the dimension), the reference of column h16's weights (a score
-// in log2 units, -infinity: none yet) and this lane's part of their sum.
+// tile, 16 n + h16 the dimension), the reference of column h16's weights (at or
+// above its scores, in log2 units; -infinity: none yet) and this lane's part of their
+// sum.
 template <int D, int N>
 struct WaveState {
   f32x4 o[N][D / 16];
@@ -537,14 +538,18 @@ __device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
 // each weight (rms error 2.4e-6 of a sum of random values), three all of them; see
 // kTwoPartLength.
 //
-// Weights are taken against the column's reference, which need not be the largest
-// score so far: fp32 and bf16 hold weights up to 2^kHeadroom as well as those
-// below 1, and the reference's own position keeps the sum at 1 or more.  So the
-// largest score is looked for, and sums are rescaled, only where a weight passes
-// the headroom or a column has no reference yet (its weights come out infinite or
-// NaN): a third fewer vector operations per score than with the largest score of
-// every step.
-constexpr float kHeadroom = 1.0995116e12f;   // 2^40
+// Weights are taken against the column's reference, kLag above the largest score
+// at which it was set and below no later one: weights are at most 1, so that sums
+// of weights times values stay where the values do (as with the largest score
+// itself), and the sum at 2^-kLag or more.  So the largest score is looked for, and
+// sums are rescaled, only where a lane's weights add up to more than 1 or a column
+// has no reference yet (its weights come out infinite or NaN): a third fewer vector
+// operations per score than with the largest score of every step.  A small lag
+// raises references more often, a large one costs the exponents' low bits (two
+// layers of 64 requests behind 65,536 positions at 2, 4, 6, 8, 16: 421, 411, 405,
+// 408, 409 us; 32 behind 16,384, rms error at 4, 6, 8, 16: 4.0e-7, 4.1e-7, 4.2e-7,
+// 5.0e-7).
+constexpr float kLag = 6.f;
 template <int D, int kParts>
 __device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, float scale, f32x4 (&o)[D / 16], float& m,
                                              float& l, bf16x8 (&part)[kParts]) {
@@ -558,11 +563,11 @@ __device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, f
     }
   };
   weights(m);
-  if (__any(!(sum <= kHeadroom))) {
+  if (__any(!(sum <= 1.f))) {
     float mx = s0[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, i < 4 ? s0[i] : s1[i - 4]);
-    const float m_new = fmaxf(m, column_max(mx) * scale);
+    const float m_new = fmaxf(m, column_max(mx) * scale + kLag);
     const float ref = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = exp2_fast(m - ref);
     m = m_new;
