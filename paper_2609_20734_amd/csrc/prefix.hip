@@ -20,8 +20,8 @@
 // where they are many.  Measured, plan, split and merge together: eight requests
 // of two tenants, up to five tokens each, four layers (424 MB) 88 us, the split at
 // 6 TB/s; 32 requests behind 16,384 positions, one layer (207 MB) 56 us; 64
-// requests of 64 heads behind 65,536 positions, two layers, 407 us, 1.02 PFLOP/s
-// of products.
+// requests of 64 heads behind 65,536 positions, two layers, 485 us, the split at
+// 1.2 PFLOP/s of products, what a large library product reaches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -47,6 +47,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kWaveTiles = 2;         // column tiles a wavefront holds
 constexpr int kMaxCols = kWaves * kWaveTiles * kBlock;   // columns of an item
+constexpr int kParts = 3;             // bf16 parts of a weight
 constexpr int kMaxTokens = 16;
 constexpr int kMaxBatch = 2048;       // members and groups that the plan's workgroup holds in LDS
 constexpr int kCus = 256;
@@ -534,9 +535,10 @@ __device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
 }
 
 // Scores of 32 positions of column h16 (this lane: 4j.. of either block) into the
-// online softmax; p comes back as kParts bf16 parts.  Two parts keep 16 bits of
-// each weight (rms error 2.4e-6 of a sum of random values), three all of them; see
-// kTwoPartLength.
+// online softmax; p comes back as kParts bf16 parts, which together hold all of a
+// weight's 24 bits: two would be off by 2.4e-6 (rms, of a sum of random values),
+// three leave the 3e-7 of the exponent's rounding and the sums, for a third more
+// products per value.
 //
 // Weights are taken against the column's reference, kLag above the largest score
 // at which it was set and below no later one: weights are at most 1, so that sums
@@ -546,11 +548,11 @@ __device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
 // has no reference yet (its weights come out infinite or NaN): a third fewer vector
 // operations per score than with the largest score of every step.  A small lag
 // raises references more often, a large one costs the exponents' low bits (two
-// layers of 64 requests behind 65,536 positions at 2, 4, 6, 8, 16: 421, 411, 405,
-// 408, 409 us; 32 behind 16,384, rms error at 4, 6, 8, 16: 4.0e-7, 4.1e-7, 4.2e-7,
+// layers of 64 requests behind 65,536 positions at 2, 4, 6, 8, 16: 501, 483, 485,
+// 483, 485 us; 32 behind 16,384, rms error at 4, 6, 8, 16: 4.0e-7, 4.1e-7, 4.2e-7,
 // 5.0e-7).
 constexpr float kLag = 6.f;
-template <int D, int kParts>
+template <int D>
 __device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, float scale, f32x4 (&o)[D / 16], float& m,
                                              float& l, bf16x8 (&part)[kParts]) {
   float p[8], sum;
@@ -720,7 +722,7 @@ __device__ __forceinline__ void finish(WaveState<D, N>& w, bool bad) {
 // ranges, K and V go straight to registers.
 template <int D, int N>
 __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, char* smem) {
-  constexpr int KK = D / 32, NT = D / 16, kParts = 3;
+  constexpr int KK = D / 32, NT = D / 16;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int h16 = lane & 15, j = lane >> 4;
   const int pairs = (it.blk_hi - it.blk_lo + 1) >> 1;
@@ -786,7 +788,7 @@ __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, 
           mask_scores(room - kBlock, s1);
         }
         bf16x8 part[kParts];
-        softmax_tile<D, kParts>(s0, s1, a.scale_log2, w.o[c], w.m[c], w.l[c], part);
+        softmax_tile<D>(s0, s1, a.scale_log2, w.o[c], w.m[c], w.l[c], part);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const bf16x8 vf = cat(va[n], vb[n]);
@@ -809,7 +811,7 @@ __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, 
 // with the positions of K ordered so that operand reads are free of bank
 // conflicts.  Up to four tiles: two position ranges, which share a stage's pairs alternately;
 // more: every wavefront goes through all pairs with its N tiles.
-template <int D, int N, int kParts>
+template <int D, int N>
 __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, const Row* rows, int l, int g, int wc_shift,
                                          char* smem) {
   constexpr int KK = D / 32, NT = D / 16;
@@ -890,7 +892,7 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
         mask_scores(room, s0[c]);
         mask_scores(room - 4, s1[c]);
       }
-      softmax_tile<D, kParts>(s0[c], s1[c], a.scale_log2, w.o[c], w.m[c], w.l[c], part[c]);
+      softmax_tile<D>(s0[c], s1[c], a.scale_log2, w.o[c], w.m[c], w.l[c], part[c]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -959,12 +961,6 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
   }
 }
 
-// More than 128 columns (where the products bound the item) over this many
-// positions take weights of two parts, whose error, 2.4e-6, is then that of a
-// product summed in fp32 (1.1e-6 at 16,384 positions, 2.5e-6 at 65,536); all else
-// takes three (3e-7): 64 requests behind 65,536 positions 405 us against 484.
-constexpr int kTwoPartLength = 49152;
-
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void prefix_split_kernel(PrefixArgs a) {
@@ -981,9 +977,8 @@ void prefix_split_kernel(PrefixArgs a) {
   const int tiles = (it.ncols + kBlock - 1) / kBlock;
   if (tiles == 1) run_narrow<D, 1>(a, it, rows, l, g, smem);
   else if (tiles == 2) run_narrow<D, 2>(a, it, rows, l, g, smem);
-  else if (tiles <= kWaves) run_wide<D, 1, 3>(a, it, rows, l, g, tiles <= 4 ? 2 : 3, smem);
-  else if (it.limit < kTwoPartLength) run_wide<D, 2, 3>(a, it, rows, l, g, 3, smem);
-  else run_wide<D, 2, 2>(a, it, rows, l, g, 3, smem);
+  else if (tiles <= kWaves) run_wide<D, 1>(a, it, rows, l, g, tiles <= 4 ? 2 : 3, smem);
+  else run_wide<D, 2>(a, it, rows, l, g, 3, smem);
 }
 
 __device__ __forceinline__ float wave_sum(float x) {

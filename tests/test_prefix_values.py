@@ -59,3 +59,29 @@ def test_large_and_small_values_behind_growing_scores(groups, Hq, Hkv, D, T, cur
         p.P.full_decode_attn(p.shape, p.inp, 0, None, None, None, full, flse, ws)
         torch.cuda.synchronize()
         check_close(out[:, rows, 0].astype(np.float64) / factor, full.cpu().numpy()[:, rows].astype(np.float64) / factor)
+
+
+@pytest.mark.parametrize("D,blocks", [(64, 3074), (128, 3074), (128, 4100)])
+@pytest.mark.parametrize("peaked", [False, True])
+def test_weights_of_many_columns_keep_their_bits_at_any_length(D, blocks, peaked):
+    """160 columns behind 49,184 and 65,600 positions, attended evenly or at 40 positions alone.  Expected error: weights
+    to 2e-7 (the exponent's fp32 rounding and the exponential's), sums of a few splits 3e-7; 16-bit weights would be
+    2e-6 off."""
+    p = Problem(72, [(blocks, [1, 40, 3, 77, 100, 9, 16, 2, 31, 5])], 16, 1, D, poison=True, spare=1)
+    if peaked:
+        g = S.rng(72, 5)
+        one = S.f32_to_bf16_bits(np.ones(1, np.float32))[0]
+        p.q[:] = 0
+        p.q[..., 0] = one                           # scores are the keys' first dims
+        first = p.members[0]
+        p.k[:, :, :, 0, :, 0] = S.f32_to_bf16_bits(np.full(1, -2000.0, np.float32))[0]
+        p.kc[..., 0] = S.f32_to_bf16_bits(np.full(1, -2000.0, np.float32))[0]
+        for pos in g.choice(16 * blocks, 40, replace=False):
+            p.k[0, p.table[first, pos // 16], 0, 0, pos % 16, 0] = S.f32_to_bf16_bits(g.random(1).astype(np.float32) * 8)[0]
+    p.upload()
+    out, _ = p.run()
+    rows = p.members
+    ref, _ = OD.prefix_attention(p.q, p.k, p.v, p.table, p.seq, p.scale, p.counts(), p.kc, p.vc, rows)
+    err = np.linalg.norm(out[:, rows] - ref[:, rows]) / np.linalg.norm(ref[:, rows])
+    print(f"rms error {err:.2e}", flush=True)
+    assert err <= 1e-6
