@@ -576,8 +576,8 @@ oda_status oda_verify_workspace_size(int32_t batch, int32_t vocab, int32_t max_d
  *               then -1
  * A draft outside [0, V) is refused.  A row with no logit above -infinity
  * refuses its draft and gives the next token -1; logits of +infinity share the
- * row's probability evenly.  Weights and sums are fp64 (weights below 2^-1000 of
- * the row's largest are 0).  Rows past n_drafts are not read.  work_list / n_work as in oda_dense_bf16. */
+ * row's probability evenly.  Weights and sums are fp64 (weights below about
+ * 2^-1000 of the row's largest are 0).  Rows past n_drafts are not read.  work_list / n_work as in oda_dense_bf16. */
 oda_status oda_verify_drafts(const oda_verify_desc *desc, int32_t batch, int32_t *n_accepted, int32_t *tokens,
                              const int32_t *work_list, const int32_t *n_work, void *workspace,
                              size_t workspace_bytes, hipStream_t stream);

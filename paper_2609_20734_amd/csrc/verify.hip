@@ -16,10 +16,12 @@
 // Weights and sums are fp64: the next token has to be the one whose interval
 // holds u_K, and a vocabulary of 150,000 tokens has so many borders that fp32
 // sums (2^-24 of the whole per border) would put about one draw in a hundred on
-// the other side of one.  The exponential costs 18 fp64 operations a logit, which
-// bounds many rows (32 requests with four drafts, 151,936 tokens: 41 us, the first
-// launch 24 for 88 MB); few rows are bound by the second launch's chain of trips to
-// memory (one request: 12.6 us).
+// the other side of one.  That makes 30 vector instructions a logit, 20 of them the
+// exponential's, which is most of what bounds many rows: 32 requests with four
+// drafts, 151,936 tokens, take 42 us, the first launch 25 for 88 MB, 17 of them
+// vector work by its counters (at 2.4 GHz), the rest the start and end of workgroups
+// of three tiles.  Few rows are bound by the second launch's chain of trips to memory
+// (one request: 13.4 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -90,38 +92,41 @@ __device__ __forceinline__ double slope_of(float t) {
   return t > 0.f ? kLog2e / (double)fminf(fmaxf(t, 0x1p-100f), 0x1p100f) : 0.0;
 }
 
-// 2^y for y in [-1000, 0], by 2^k 2^f with |f| <= 1/2: the polynomial through 2^f
-// at the nine Chebyshev nodes of the interval is off by 1.1e-12 of the value at
-// most (a draw sees borders moved by that share of the whole).  k comes out of the
-// low bits of y + 1.5 2^52.
-__device__ __forceinline__ double exp2_neg(double y) {
+// 2^(x slope) for x <= 0, by 2^k 2^f with |f| <= 1/2: the polynomial through 2^f at
+// the eleven Chebyshev nodes of the interval is off by 3.2e-16 of the value at most,
+// as much as fp64's own steps (with two terms fewer, off by 1.1e-12, 32 requests took
+// 41.0 us instead of 42.2, but a draw's borders moved by as much).  k comes out of
+// the low bits of x slope + 1.5 2^52, f keeps all of the product's.  0 below about
+// 2^-1000, and for NaN.
+__device__ __forceinline__ double exp2_neg(double x, double slope) {
   constexpr double kShift = 6755399441055744.0;
-  const double t = y + kShift;
-  const double f = y - (t - kShift);
-  double p = 1.3255224878668817e-06;
-  p = fma(p, f, 1.5310079402249296e-05);
-  p = fma(p, f, 0.00015403455852453838);
-  p = fma(p, f, 0.0013333450568000645);
-  p = fma(p, f, 0.009618129159402558);
-  p = fma(p, f, 0.05550410941205933);
-  p = fma(p, f, 0.2402265069581299);
-  p = fma(p, f, 0.6931471805459335);
+  const double t = fma(x, slope, kShift);
+  const double f = fma(x, slope, kShift - t);
+  double p = 7.072585949269223e-09;
+  p = fma(p, f, 1.0208690299958306e-07);
+  p = fma(p, f, 1.321544258792169e-06);
+  p = fma(p, f, 1.5252657260200837e-05);
+  p = fma(p, f, 0.0001540353044173605);
+  p = fma(p, f, 0.0013333558230164974);
+  p = fma(p, f, 0.009618129107606888);
+  p = fma(p, f, 0.05550410866444772);
+  p = fma(p, f, 0.24022650695910097);
+  p = fma(p, f, 0.69314718055995);
   p = fma(p, f, 1.0);
-  return ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
+  const double e = ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
+  return t >= kShift - 1000.0 ? e : 0.0;
 }
 
 // Weights of a row's logits against `top`, its largest (above -infinity): slope =
 // log2(e) / temperature.  (The difference first: a logit may be the type's lowest
-// value, whose product is off by more than the whole range.)  Weights below 2^-1000
-// are 0, and so is NaN's.  Where the largest is +infinity it alone weighs.
+// value, whose product is off by more than the whole range.)  Weights below about
+// 2^-1000 are 0, and so is NaN's.  Where the largest is +infinity it alone weighs.
 struct Weights {
   double slope, top;
 };
 __device__ __forceinline__ Weights weights_against(float top, double slope) { return Weights{slope, (double)top}; }
 __device__ __forceinline__ double finite_weight(const Weights& w, float z) {
-  const double y = ((double)z - w.top) * w.slope;
-  const double e = exp2_neg(y);
-  return y >= -1000.0 ? e : 0.0;
+  return exp2_neg((double)z - w.top, w.slope);
 }
 __device__ __forceinline__ double weight(const Weights& w, float z) {
   return w.top == (double)INFINITY ? (z == INFINITY ? 1.0 : 0.0) : finite_weight(w, z);
