@@ -273,7 +273,7 @@ class DraftDecoder:
 
         self.plan = zeros(P.prefix_plan_size(self.attn_shape, self.groups))
         self.ws_attn = zeros(P.prefix_workspace_size(self.attn_shape, self.groups))
-        self.ws_lora = zeros(max([P.lora_workspace_size(a[0], rows) for a in self.adapters.values()], default=0))
+        self.ws_lora = zeros(max([P.lora_workspace_size(d, rows) for a in self.adapters.values() for d in a], default=0))
         self.ws_verify = zeros(P.verify_workspace_size(B, s.vocab, T - 1))
         self.ws_commit = zeros(P.commit_workspace_size(self.commit_shape))
         w = weights
