@@ -220,7 +220,8 @@ class DraftDecoder:
     ready for the next step.
 
     groups: (group_start, members, prefix_blocks), int32 device tensors: requests
-    whose prompts share their first blocks; adapters: {"w_qkv" | "w_o" | "w_gu" |
+    whose prompts share their first blocks, every request in one group (of no blocks
+    if it shares none); adapters: {"w_qkv" | "w_o" | "w_gu" |
     "w_down": [LoraDesc per layer]}, any of them, chosen per request by adapter_ids
     [B] (-1: none); temperature: fp32 [B] or None; draft_probs: True to verify
     against `probs` [B][T - 1][V] (written before each step), else drafts count as
@@ -285,13 +286,13 @@ class DraftDecoder:
         self.d_vocab = P.dense_desc(d, s.vocab, P.DENSE_PLAIN, w["embed"])
 
     def set_drafts(self, current, drafts, n_drafts) -> None:
-        """The next step's current tokens [B], drafts [B][T - 1] and their counts [B]."""
+        """The next step's current tokens [B], drafts [B][T - 1] and their counts [B] (clamped to [0, T - 1])."""
         self.tokens[:, 0].copy_(current)
         if self.T > 1:
             self.tokens[:, 1:].copy_(drafts)
             self.drafts.copy_(drafts)
-        self.n_drafts.copy_(n_drafts)
-        self.n_tokens.copy_(n_drafts + 1)
+        self.n_drafts.copy_(n_drafts.clamp(0, self.T - 1))
+        self.n_tokens.copy_(self.n_drafts + 1)
 
     def _dense(self, name: str, l: int, x, residual, y):
         rows = self.B * self.T

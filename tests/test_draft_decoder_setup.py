@@ -50,3 +50,14 @@ def test_the_adapters_workspace_serves_every_layer(P, ranks):
     dec = _decoder(P, ranks=ranks, names=("w_o", "w_gu"))
     need = max(P.lora_workspace_size(d, dec.B * dec.T) for a in dec.adapters.values() for d in a)
     assert dec.ws_lora.numel() >= need
+
+
+@pytest.mark.parametrize("counts", [[0, 2], [-1, 1], [-2 ** 31, 3], [7, 2 ** 31 - 1]])
+def test_counts_of_drafts_are_clamped_alike(P, counts):
+    """Verification clamps the number of drafts to [0, T - 1]; attention has a current token more than that."""
+    dec = _decoder(P)
+    n = torch.tensor(counts, dtype=torch.int32)
+    dec.set_drafts(torch.zeros(2, dtype=torch.int32), torch.zeros(2, dec.T - 1, dtype=torch.int32), n)
+    want = np.clip(counts, 0, dec.T - 1)
+    np.testing.assert_array_equal(np.clip(dec.n_drafts.numpy(), 0, dec.T - 1), want)
+    np.testing.assert_array_equal(np.clip(dec.n_tokens.numpy(), 0, dec.T), want + 1)
