@@ -115,9 +115,12 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 // n - 2 + count.  Work split and ticket as in commit_kernel.  K: one 16-byte
 // store per (unit, 8 dims, token), the tokens of a block next to each other;
 // V: a thread walks the tokens of one dim, whose slots are neighbours in the
-// block's [D][16] row.  Bound by partly written lines (a token is 2 of a V row's
-// 32 bytes: 32 layers of 32 requests, up to eight tokens each, write 19 MB as 67 MB
-// of lines in 23 us), so the launch has as many wavefronts as the chip holds.
+// block's [D][16] row.  32 layers of 32 requests, up to eight tokens each, take 23 us:
+// 19 MB read and written as 57 to 67 MB of partly written lines (a token is 2 of a V
+// row's 32 bytes) would take 15 to 17 at a copy's rate, and wavefronts wait for more
+// than half their time on the trips from a table entry to its stores, so the launch
+// has as many of them as the chip holds.  Advancing the lengths adds two us for one
+// request and, by the tickets of 128 workgroups a request, 27 for these 32.
 struct CommitDraftsArgs {
   uint16_t* k_cache;
   uint16_t* v_cache;

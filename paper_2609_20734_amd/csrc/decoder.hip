@@ -945,6 +945,8 @@ oda_status launch_dense(const Args& a, bool swiglu, hipStream_t stream) {
   // 6144: 128 requests 48.6 against 55.3).  Of 48 rows and 32 requests where that
   // takes no more rounds than 64 rows (6144 -> 2048, 160 requests 28.1 us against
   // 31.5; 2048 -> 4096, 96 requests two rounds instead of one 26.7 against 16.3).
+  // Over 60 layers of 2,048 to 151,936 rows, K 512 to 14336, 24 to 256 requests the
+  // faster side is taken but for one (1024 -> 8192, 96 requests 18.3 us against 16.8).
   // The SwiGLU pair has no room for 64 rows: 32 were slower than three tiles up to
   // 64 requests and within 8% above.
   const auto wide_rounds_of = [&](int tiles) {

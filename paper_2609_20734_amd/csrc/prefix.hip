@@ -108,8 +108,10 @@ struct PlanArgs {
 // which one CU's share of HBM delivers it: a tile's products and softmax take
 // about an eighth of that, so up to eight tiles are free.
 constexpr float kBlockCost = 8.f;
-// Start-up, the join and the partial's share of the merge (32 requests behind
-// 16,384 positions: 56.7 us; 67.6 at 40, 66.0 at 80 and 120, 56.9 at 220).
+// Start-up, the join and the partial's share of the merge.  The counts of splits that
+// it leads to matter more than the figure: over 18 sizes of one to 64 requests the
+// mean time at 60, 110, 160, 220, 320 is 41.0, 41.1, 40.7, 41.1, 40.8 us, 32 requests
+// behind 16,384 positions 66, 61, 57, 57, 65.
 constexpr float kItemCost = 160.f;
 constexpr float kLeastCost = 16 * kBlockCost;   // shortest split: two blocks per wavefront
 
