@@ -20,14 +20,16 @@
 // where they are many.  Measured, plan, split and merge together: eight requests
 // of two tenants, up to five tokens each, four layers (424 MB) 88 us, the split at
 // 6 TB/s; 32 requests behind 16,384 positions, one layer (207 MB) 56 us; 64
-// requests of 64 heads behind 65,536 positions, two layers, 485 us, the split at
-// 1.2 PFLOP/s of products, what a large library product reaches.
+// requests of 64 heads behind 65,536 positions, two layers, 485 to 515 us on three
+// cards, the split at 1.1 to 1.2 PFLOP/s of products, what a large library product
+// reaches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <type_traits>
@@ -465,12 +467,13 @@ struct PrefixArgs {
   float* out;
   float* lse;
   float* part_o;      // [units][part_cols][D]
-  float* part_ml;     // [units][part_cols][2]  (m in log2 units, l)
+  float* part_ml;     // [units][part_cols][2]  (m: a reference in score units, l)
   int64_t kv_layer_stride;
   int64_t num_blocks;
   int32_t L, B, T, Hq, Hkv, G, MB, NG;
   int32_t part_cols, max_items;
-  float scale_log2;
+  float scale_log2;   // of a score, for exponents of 2
+  float lag;          // kLag in score units
 };
 
 __device__ __forceinline__ bool plan_fits(const PrefixArgs& a, const PlanHeader& h) {
@@ -492,7 +495,12 @@ __device__ __forceinline__ bf16x8 cat(u32x2 lo, u32x2 hi) {
   u32x4 t = {lo.x, lo.y, hi.x, hi.y};
   return __builtin_bit_cast(bf16x8, t);
 }
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// The weight of a score against a reference.  (The difference first: it is exact
+// where it matters, also for scores whose product with the scale would be off by
+// more than the exponents' range; one fused step instead of two saves 1%.)
+__device__ __forceinline__ float weight_of(float s, float ref, float scale_log2) {
+  return __builtin_amdgcn_exp2f((s - ref) * scale_log2);
+}
 __device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
 // Register layouts of v_mfma_f32_16x16x32_bf16 and the cache layouts' fit with
 // them are those of the decode attention (attention.hip): a K block's 16-byte
@@ -501,7 +509,7 @@ __device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bi
 
 // A wavefront's share of N column tiles: O = P V (rows: columns 4j..4j+3 of the
 // tile, 16 n + h16 the dimension), the reference of column h16's weights (at or
-// above its scores, in log2 units; -infinity: none yet) and this lane's part of their
+// above its scores; -infinity: none yet) and this lane's part of their
 // sum.
 template <int D, int N>
 struct WaveState {
@@ -550,19 +558,20 @@ __device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
 // has no reference yet (its weights come out infinite or NaN): a third fewer vector
 // operations per score than with the largest score of every step.  A small lag
 // raises references more often, a large one costs the exponents' low bits (two
-// layers of 64 requests behind 65,536 positions at 2, 4, 6, 8, 16: 501, 483, 485,
-// 483, 485 us; 32 behind 16,384, rms error at 4, 6, 8, 16: 4.0e-7, 4.1e-7, 4.2e-7,
-// 5.0e-7).
+// layers of 64 requests behind 65,536 positions at 2, 4, 6, 8, 16: 532, 518, 516,
+// 517, 515 us on one card; 32 behind 16,384, rms error: 4.0e-7, 4.1e-7, 4.2e-7,
+// 4.5e-7, 5.9e-7).
 constexpr float kLag = 6.f;
+constexpr float kMaxLag = 1e37f;     // (scores of a scale that small all weigh the same)
 template <int D>
-__device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, float scale, f32x4 (&o)[D / 16], float& m,
-                                             float& l, bf16x8 (&part)[kParts]) {
+__device__ __forceinline__ void softmax_tile(const PrefixArgs& a, const f32x4& s0, const f32x4& s1, f32x4 (&o)[D / 16],
+                                             float& m, float& l, bf16x8 (&part)[kParts]) {
   float p[8], sum;
   auto weights = [&](float ref) {
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = exp2_fast(fmaf(i < 4 ? s0[i] : s1[i - 4], scale, -ref));
+      p[i] = weight_of(i < 4 ? s0[i] : s1[i - 4], ref, a.scale_log2);
       sum += p[i];
     }
   };
@@ -571,9 +580,9 @@ __device__ __forceinline__ void softmax_tile(const f32x4& s0, const f32x4& s1, f
     float mx = s0[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, i < 4 ? s0[i] : s1[i - 4]);
-    const float m_new = fmaxf(m, column_max(mx) * scale + kLag);
+    const float m_new = fmaxf(m, fminf(column_max(mx) + a.lag, FLT_MAX));
     const float ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2_fast(m - ref);
+    const float alpha = weight_of(m, ref, a.scale_log2);
     m = m_new;
     l *= alpha;
     const int j = (threadIdx.x & 63) >> 4;
@@ -697,7 +706,7 @@ __device__ __forceinline__ void join(const PrefixArgs& a, const Item& it, int l,
       float acc0 = 0.f, acc1 = 0.f, lam = 0.f;
       for (int p = 0; p < WP; ++p) {
         const int wv = p * WC + q;
-        const float s = exp2_fast(sm_m[(wv * N + c) * kBlock + col16] - Mu);
+        const float s = weight_of(sm_m[(wv * N + c) * kBlock + col16], Mu, a.scale_log2);
         const float2 ow = *reinterpret_cast<const float2*>(sm_o + (wv * kBlock + col16) * D + d);
         acc0 += s * ow.x;
         acc1 += s * ow.y;
@@ -790,7 +799,7 @@ __device__ __forceinline__ void run_narrow(const PrefixArgs& a, const Item& it, 
           mask_scores(room - kBlock, s1);
         }
         bf16x8 part[kParts];
-        softmax_tile<D>(s0, s1, a.scale_log2, w.o[c], w.m[c], w.l[c], part);
+        softmax_tile<D>(a, s0, s1, w.o[c], w.m[c], w.l[c], part);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const bf16x8 vf = cat(va[n], vb[n]);
@@ -894,7 +903,7 @@ __device__ __forceinline__ void run_wide(const PrefixArgs& a, const Item& it, co
         mask_scores(room, s0[c]);
         mask_scores(room - 4, s1[c]);
       }
-      softmax_tile<D>(s0[c], s1[c], a.scale_log2, w.o[c], w.m[c], w.l[c], part[c]);
+      softmax_tile<D>(a, s0[c], s1[c], w.o[c], w.m[c], w.l[c], part[c]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -1070,7 +1079,7 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
   // weights against a new largest logit
   auto rescale = [&](float m) {
     const float top = fmaxf(M, m);
-    const float s = M == -INFINITY ? 0.f : exp2_fast(M - top);
+    const float s = M == -INFINITY ? 0.f : weight_of(M, top, a.scale_log2);
     sum *= s;
 #pragma unroll
     for (int e = 0; e < PD; ++e) o[e] *= s;
@@ -1100,7 +1109,7 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
     };
     load(0);
     rescale(wave_max(m));
-    const float w = exp2_fast(m - (M == -INFINITY ? 0.f : M));    // NaN of a bad entry stays
+    const float w = weight_of(m, M == -INFINITY ? 0.f : M, a.scale_log2);    // NaN of a bad entry stays
     sum += wave_sum(lane < n ? w * part : 0.f);
     for (int k0 = 0; k0 < n; k0 += kMergeLoads) {
       if (k0 > 0) load(k0);
@@ -1123,9 +1132,9 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
     if (i + 1 < more) fetch(i + 1);
 #pragma unroll
     for (int e = 0; e < PD; ++e) dot += q[e] * kd[e];
-    dot = wave_sum(dot) * a.scale_log2;
+    dot = wave_sum(dot);
     rescale(dot);
-    const float w = exp2_fast(dot - (M == -INFINITY ? 0.f : M));
+    const float w = weight_of(dot, M == -INFINITY ? 0.f : M, a.scale_log2);
     sum += w;
 #pragma unroll
     for (int e = 0; e < PD; ++e) o[e] += w * vd[e];
@@ -1133,7 +1142,7 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixArgs a) {
   if (bad) sum = __builtin_nanf("");
 #pragma unroll
   for (int e = 0; e < PD; ++e) out[e] = o[e] / sum;
-  if (lse && lane == 0) *lse = (M + __log2f(sum)) * kLn2;
+  if (lse && lane == 0) *lse = (M * a.scale_log2 + __log2f(sum)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------
@@ -1319,5 +1328,6 @@ extern "C" oda_status oda_prefix_decode_attn(const oda_attn_shape* shape, const 
   a.part_cols = z.part_cols;
   a.max_items = z.max_items;
   a.scale_log2 = in->scale * kLog2e;
+  a.lag = std::min(kLag / a.scale_log2, kMaxLag);
   return shape->head_dim == 128 ? launch_attention<128>(a, stream) : launch_attention<64>(a, stream);
 }

@@ -85,3 +85,35 @@ def test_weights_of_many_columns_keep_their_bits_at_any_length(D, blocks, peaked
     err = np.linalg.norm(out[:, rows] - ref[:, rows]) / np.linalg.norm(ref[:, rows])
     print(f"rms error {err:.2e}", flush=True)
     assert err <= 1e-6
+
+
+@pytest.mark.parametrize("groups", [[(0, [300])], [(20, [40, 90, 3, 8])], [(33, list(range(1, 40, 3)))]],
+                         ids=["one tile", "four tiles", "thirteen tiles"])
+@pytest.mark.parametrize("cur", [True, False])
+@pytest.mark.parametrize("score", [1e4, 1e9, 1e20, 3e38, -1e4, -1e20, -3e38])
+def test_scores_of_any_size(score, cur, groups):
+    """All keys alike, at a score whose product with the scale is off by more than exponents hold; then every third at
+    the type's lowest value; then all but a few of each request's own there.  The lse's fp32 steps are seven (two
+    constants, the scale in log2 units, the reference, its product, the sum, the product back)."""
+    bits = lambda x: S.f32_to_bf16_bits(np.full(1, x, np.float32))[0]  # noqa: E731
+    p = Problem(73, groups, 16, 1, 64, cur=cur, spare=1)
+    p.q[:] = 0
+    p.q[..., 0] = bits(1.0)                         # scores are the keys' first dims
+    for step in range(3):
+        low = bits(-3e38)
+        if step == 0:
+            p.k[:, :, :, 0, :, 0] = bits(score)
+        elif step == 1:
+            p.k[:, :, :, 0, ::3, 0] = low
+        else:
+            p.k[:, :, :, 0, :, 0] = low
+            for b in p.members:
+                p.k[:, p.table[b, (int(p.seq[b]) - 1) // 16], :, 0, :, 0] = bits(score)
+        if cur:
+            p.kc[..., 0] = bits(score) if step != 1 else low
+        p.upload()
+        out, lse = p.run()
+        ref, ref_lse = OD.prefix_attention(p.q, p.k, p.v, p.table, p.seq, p.scale, p.counts(), p.kc, p.vc, p.members)
+        rows = p.members
+        check_close(out[:, rows], ref[:, rows], f"step {step}")
+        np.testing.assert_allclose(lse[:, rows], ref_lse[:, rows], rtol=7 * 2.0 ** -24, atol=LSE_ABS)
