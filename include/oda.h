@@ -603,6 +603,139 @@ oda_status oda_commit_drafts(const oda_attn_shape *shape, int32_t tokens, uint16
                              int32_t n_sink, int32_t window, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Prompts.  A chunk of new tokens per request, from single tokens to whole
+ * prompts, side by side in the rows of every buffer (no padding between requests):
+ * their K/V is appended to the paged cache, their attention runs over it, and the
+ * log probabilities of their tokens are formed.  decoder.PromptDecoder composes the
+ * forward of a chunk from these and the dense layers above.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { ODA_F32 = 0, ODA_BF16 = 1 } oda_type;
+
+/* Rows of a batch (host struct holding device pointers): request b has the rows
+ * row_start[b] .. row_start[b + 1] - 1, possibly none.  Starts are taken into
+ * [0, num_rows] and as ascending, whatever the array holds; rows in front of the
+ * first or behind the last request's are neither read nor written. */
+typedef struct {
+  int32_t num_rows;           /* rows of the buffers, >= 1                          */
+  const int32_t *row_start;   /* int32 [B + 1]                                      */
+} oda_prompt_rows;
+
+/* What oda_append_qkv does to the rows on their way (host struct holding device
+ * pointers).
+ *   qkv        fp32 or bf16 [num_rows][(Hq + 2 Hkv) D]: q heads, then k heads, then
+ *              v heads (k and v heads alone where q_out is NULL, q heads alone where
+ *              the caches are); 16-byte aligned
+ *   q_gain, k_gain  fp32 [D] per-head RMSNorm gains, or NULL (no norm)
+ *   rope_theta > 1: dims i and i + D/2 of q and k heads turn by p theta^(-2i/D),
+ *              angles in double; 0: no rotation
+ *   positions  int32 [num_rows][num_axes]: p of a pair is its axis's position; NULL
+ *              (one axis): the row's place in the history
+ *   axis_pairs pairs of each axis (time, height, width ...): the first axis_pairs[0]
+ *              pairs take the first, and so on; their sum is D/2.  Ignored for one axis */
+#define ODA_MAX_AXES 4
+typedef struct {
+  const void *qkv;
+  int32_t qkv_type;             /* oda_type                                          */
+  float rms_eps;                /* >= 0                                              */
+  const float *q_gain;
+  const float *k_gain;
+  double rope_theta;
+  const int32_t *positions;
+  int32_t num_axes;             /* 1..ODA_MAX_AXES                                   */
+  int32_t axis_pairs[ODA_MAX_AXES];
+} oda_append_desc;
+
+/* Appends a chunk of one layer (num_layers == 1): row i of a request's m rows is
+ * place seq_lens[b] - m + i of its history, seq_lens[b] counting the chunk.  Heads
+ * are normed, turned and rounded to bf16 (nearest-even) as by oda_qk_norm_rope; q
+ * goes to q_out, K and V to the paged cache and, if given, to the rings (what they
+ * still hold after the chunk), in one launch.
+ *   q_out    bf16 [num_rows][Hq][D], or NULL: the rows have no q heads
+ *   k_cache, v_cache  both NULL: the rows have q heads alone (the queries of an
+ *            attention over other states); block_table is then not read
+ *   k_ring, v_ring, n_sink, window: as in oda_commit_kv_ring, or NULL, 0, 0
+ * A request whose length is outside [0, max_seq_len] or shorter than its rows gets
+ * NaN queries and appends nothing; a table entry outside [0, num_blocks) drops the
+ * K/V of its places.  Places are written once: requests must not share the blocks
+ * that they append to. */
+oda_status oda_append_qkv(const oda_attn_shape *shape, const oda_prompt_rows *rows, const oda_append_desc *desc,
+                          uint16_t *k_cache, uint16_t *v_cache, const int32_t *block_table, const int32_t *seq_lens,
+                          uint16_t *q_out, uint16_t *k_ring, uint16_t *v_ring, int32_t n_sink, int32_t window,
+                          hipStream_t stream);
+
+/* Bytes of the plan buffer and of the workspace of calls with these sizes (the
+ * shape and num_rows) (host out).  Neither needs to be cleared. */
+oda_status oda_prompt_plan_size(const oda_attn_shape *shape, const oda_prompt_rows *rows, size_t *bytes);
+oda_status oda_prompt_workspace_size(const oda_attn_shape *shape, const oda_prompt_rows *rows, size_t *bytes);
+
+/* Plans oda_prompt_attn on the device: the rows' tiles, and how their histories are
+ * split over the chip.  One plan serves every call whose shape, rows, lengths and
+ * mask are the plan's (all layers of a step).  When lengths or row starts change,
+ * plan again: the attention reads them from the plan.
+ *   causal:        1: row i of a request's m rows attends places 0 .. seq_lens[b] - m + i;
+ *                  0: every row attends all of 0 .. seq_lens[b] - 1 (states of another
+ *                  length, such as an encoder's; seq_lens[b] may be 0: the rows are then
+ *                  zeros, their lse -infinity)
+ *   native_window: > 0 (causal): only the last native_window of them (natively
+ *                  windowed layers)
+ *   plan:          >= oda_prompt_plan_size bytes, 256-byte aligned
+ * shape->num_layers must be 1 and split_blocks 0; batch at most 2048. */
+oda_status oda_prompt_plan(const oda_attn_shape *shape, const oda_prompt_rows *rows, const int32_t *seq_lens,
+                           int32_t causal, int32_t native_window, void *plan, size_t plan_bytes, hipStream_t stream);
+
+/* Attention of the planned rows over the paged cache, which holds all they attend
+ * (the chunk's own K/V too: oda_append_qkv).  in->seq_lens is not read (the plan has
+ * the lengths); in->k_cur and v_cur must be NULL.
+ *   q    bf16 [num_rows][Hq][D]
+ *   out  fp32 or bf16 (out_type) [num_rows][Hq][D], 16-byte aligned: the weights of an
+ *        fp32 output hold all of their 24 bits, as in decode attention; those of a bf16
+ *        output are rounded to bf16, which takes half the matrix operations
+ *   lse  fp32 [num_rows][Hq] (natural log), or NULL
+ * A request whose length is outside [0, max_seq_len] or (causal) shorter than its
+ * rows gets NaN rows, and so does a row that attends a block whose table entry is
+ * outside [0, num_blocks); other rows do not see it.  Slots that no row attends may
+ * hold anything; a value that is not finite reaches the rows that attend it alone.
+ * A plan made for another batch, num_rows, head counts, table width or max_seq_len
+ * gives NaN throughout.  workspace: >= oda_prompt_workspace_size bytes, 256-byte
+ * aligned; calls that may overlap in time need separate ones (a plan may be shared). */
+oda_status oda_prompt_attn(const oda_attn_shape *shape, const oda_attn_inputs *in, const oda_prompt_rows *rows,
+                           const void *plan, size_t plan_bytes, void *out, int32_t out_type, float *lse,
+                           void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+#define ODA_MAX_TOP 32
+
+/* Rows of logits to score (host struct holding device pointers). */
+typedef struct {
+  int32_t vocab;                /* V >= 1                                            */
+  int32_t top;                  /* k: alternatives per row, 0..ODA_MAX_TOP            */
+  int64_t row_stride;           /* floats from one row to the next; 0: V, else >= V   */
+  const float *logits;          /* fp32; NaN counts as -infinity                      */
+  const int32_t *tokens;        /* int32 [rows]: the given tokens, or NULL            */
+} oda_logprob_desc;
+
+/* Bytes of workspace oda_token_logprobs needs (host out).  Zero-fill it before its
+ * first use (ticket words; every call leaves them zero); it serves any later call on
+ * the stream. */
+oda_status oda_logprob_workspace_size(const oda_logprob_desc *desc, int32_t rows, size_t *bytes);
+
+/* With p = softmax(logits of the row) and tokens in the order of their logits (equal
+ * ones by their index):
+ *   logprob      fp32 [rows]: log p(tokens[r]); rank int32 [rows]: its place in the
+ *                order, from 1.  A token outside [0, V): NaN and 0.  Both NULL where
+ *                tokens is NULL; either may be NULL
+ *   entropy      fp32 [rows]: -sum p log p, or NULL
+ *   top_logprobs fp32 [rows][k], top_tokens int32 [rows][k]: the first k of the order;
+ *                where fewer logits are above -infinity, -infinity and -1 behind
+ *                them.  Both NULL iff k == 0
+ * Logits of +infinity share the row's probability evenly.  A row with no logit above
+ * -infinity has no distribution: logprob and entropy are NaN.  work_list / n_work as
+ * in oda_dense_bf16 (the listed rows alone are read and written). */
+oda_status oda_token_logprobs(const oda_logprob_desc *desc, int32_t rows, float *logprob, int32_t *rank, float *entropy,
+                              float *top_logprobs, int32_t *top_tokens, const int32_t *work_list, const int32_t *n_work,
+                              void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aid (not a step of the method): the streaming-read ceiling that
  * the attention kernels' bandwidth is quoted against.
  * ------------------------------------------------------------------------- */

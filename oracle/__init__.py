@@ -16,6 +16,8 @@ starting from the exact input values (bf16 and fp32 widen to fp64 exactly):
                     conditional Full, selected output (App. A.5);
 * ``drafts``     -- adapters beside dense layers, verification and commit of
                     drafted tokens, attention of requests that share a prefix;
+* ``prompt``     -- rows appended to the paged cache, their attention over it, log
+                    probabilities of their tokens;
 * ``ledger``     -- the bytes each step reads (App. A.6 and B.7 accounting).
 
 Parity status: every function is pinned by ``tests/test_oracle_*.py`` except

@@ -5,7 +5,9 @@ HIP kernels for Local decode attention (over the paged cache, or over the
 direct-ring workspace), the recall gate with its device predicate, Full
 decode attention for flagged requests only, the selected-state commit, the
 operators of a step of many tenants with drafted tokens (attention over shared
-prefixes, adapters beside dense layers, verification and commit of drafts), and
+prefixes, adapters beside dense layers, verification and commit of drafts), those
+that take prompts in (rows appended to the paged cache, their attention over it,
+log probabilities of their tokens), and
 the decoder layers around them (``decoder`` composes whole synthetic decode
 steps from those entry points).  This package
 holds its sources (``csrc/``), its build step (``build.py``), a ctypes
@@ -27,7 +29,10 @@ _EXPORTS = ("HEAD_MLP", "HEAD_PAPER", "OdaError", "Shape", "attn_workspace_size"
             "ring_elements", "ring_fill", "local_decode_attn_ring", "commit_kv_ring", "prepare_local_ring",
             "prefix_groups", "prefix_plan_size", "prefix_workspace_size", "prefix_plan", "prefix_decode_attn",
             "prepare_prefix_plan", "prepare_prefix_decode_attn", "lora_desc", "lora_workspace_size", "dense_lora_bf16",
-            "prepare_dense_lora", "verify_desc", "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts")
+            "prepare_dense_lora", "verify_desc", "verify_workspace_size", "verify_drafts", "prepare_verify_drafts", "commit_drafts", "prepare_commit_drafts",
+            "F32", "BF16", "MAX_AXES", "MAX_TOP", "prompt_rows", "append_desc", "append_qkv", "prepare_append_qkv",
+            "prompt_plan_size", "prompt_workspace_size", "prompt_plan", "prepare_prompt_plan", "prompt_attn",
+            "prepare_prompt_attn", "logprob_desc", "logprob_workspace_size", "token_logprobs", "prepare_token_logprobs")
 
 
 def __getattr__(name):

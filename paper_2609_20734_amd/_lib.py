@@ -39,6 +39,12 @@ HEAD_MLP = 1
 DENSE_PLAIN = 0
 DENSE_SWIGLU = 1
 
+F32 = 0
+BF16 = 1
+
+MAX_AXES = 4
+MAX_TOP = 32
+
 EXPORTED = ("oda_attn_workspace_size", "oda_local_decode_attn", "oda_full_decode_attn",
             "oda_local_decode_attn_qkv", "oda_full_decode_attn_qkv",
             "oda_gate_param_count", "oda_gate_workspace_size", "oda_recall_gate", "oda_recall_gate_static",
@@ -47,7 +53,9 @@ EXPORTED = ("oda_attn_workspace_size", "oda_local_decode_attn", "oda_full_decode
             "oda_dense_bf16", "oda_qk_norm_rope", "oda_embed_bf16", "oda_copy_rows", "oda_rms_norm_rows",
             "oda_argmax", "oda_prefix_plan_size", "oda_prefix_workspace_size", "oda_prefix_plan",
             "oda_prefix_decode_attn", "oda_lora_workspace_size", "oda_dense_lora_bf16", "oda_verify_workspace_size",
-            "oda_verify_drafts", "oda_commit_drafts", "oda_stream_read", "oda_status_string", "oda_last_error")
+            "oda_verify_drafts", "oda_commit_drafts", "oda_append_qkv", "oda_prompt_plan_size",
+            "oda_prompt_workspace_size", "oda_prompt_plan", "oda_prompt_attn", "oda_logprob_workspace_size",
+            "oda_token_logprobs", "oda_stream_read", "oda_status_string", "oda_last_error")
 
 
 class OdaError(RuntimeError):
@@ -104,6 +112,21 @@ class VerifyDesc(ctypes.Structure):
     _fields_ = [("vocab", ctypes.c_int32), ("max_drafts", ctypes.c_int32), ("logits", ctypes.c_void_p),
                 ("draft_probs", ctypes.c_void_p), ("draft_tokens", ctypes.c_void_p), ("n_drafts", ctypes.c_void_p),
                 ("temperature", ctypes.c_void_p), ("uniform", ctypes.c_void_p)]
+
+
+class PromptRows(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int32), ("row_start", ctypes.c_void_p)]
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = [("qkv", ctypes.c_void_p), ("qkv_type", ctypes.c_int32), ("rms_eps", ctypes.c_float),
+                ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("rope_theta", ctypes.c_double),
+                ("positions", ctypes.c_void_p), ("num_axes", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * MAX_AXES)]
+
+
+class LogprobDesc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("top", ctypes.c_int32), ("row_stride", ctypes.c_int64),
+                ("logits", ctypes.c_void_p), ("tokens", ctypes.c_void_p)]
 
 
 _P = ctypes.POINTER
@@ -187,6 +210,22 @@ _lib.oda_verify_drafts.restype = ctypes.c_int
 _lib.oda_commit_drafts.argtypes = [_P(AttnShape), ctypes.c_int32, _V, _V, _V, _V, _V, _V, _V, ctypes.c_int32, _V, _V,
                                    ctypes.c_size_t, _V, _V, ctypes.c_int32, ctypes.c_int32, _V]
 _lib.oda_commit_drafts.restype = ctypes.c_int
+_lib.oda_append_qkv.argtypes = [_P(AttnShape), _P(PromptRows), _P(AppendDesc), _V, _V, _V, _V, _V, _V, _V, ctypes.c_int32,
+                                ctypes.c_int32, _V]
+_lib.oda_append_qkv.restype = ctypes.c_int
+_lib.oda_prompt_plan_size.argtypes = [_P(AttnShape), _P(PromptRows), _P(ctypes.c_size_t)]
+_lib.oda_prompt_plan_size.restype = ctypes.c_int
+_lib.oda_prompt_workspace_size.argtypes = [_P(AttnShape), _P(PromptRows), _P(ctypes.c_size_t)]
+_lib.oda_prompt_workspace_size.restype = ctypes.c_int
+_lib.oda_prompt_plan.argtypes = [_P(AttnShape), _P(PromptRows), _V, ctypes.c_int32, ctypes.c_int32, _V, ctypes.c_size_t, _V]
+_lib.oda_prompt_plan.restype = ctypes.c_int
+_lib.oda_prompt_attn.argtypes = [_P(AttnShape), _P(AttnInputs), _P(PromptRows), _V, ctypes.c_size_t, _V, ctypes.c_int32, _V,
+                                 _V, ctypes.c_size_t, _V]
+_lib.oda_prompt_attn.restype = ctypes.c_int
+_lib.oda_logprob_workspace_size.argtypes = [_P(LogprobDesc), ctypes.c_int32, _P(ctypes.c_size_t)]
+_lib.oda_logprob_workspace_size.restype = ctypes.c_int
+_lib.oda_token_logprobs.argtypes = [_P(LogprobDesc), ctypes.c_int32, _V, _V, _V, _V, _V, _V, _V, _V, ctypes.c_size_t, _V]
+_lib.oda_token_logprobs.restype = ctypes.c_int
 _lib.oda_stream_read.argtypes = [_V, ctypes.c_size_t, _V, ctypes.c_int32, _V]
 _lib.oda_stream_read.restype = ctypes.c_int
 _lib.oda_status_string.argtypes = [ctypes.c_int]
@@ -484,6 +523,81 @@ def commit_drafts(shape: Shape, tokens: int, k_cache, v_cache, block_table, seq_
                           row_lens, workspace, k_ring, v_ring, n_sink, window, workspace_bytes, stream)()
 
 
+def _type(t, name: str) -> int:
+    """oda_type of a tensor (None and a plain address count as fp32)."""
+    if t is None or isinstance(t, int) or t.dtype == torch.float32:
+        return F32
+    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        return BF16
+    raise ValueError(f"{name} must be fp32 or bf16 (got {t.dtype})")
+
+
+def prompt_rows(num_rows: int, row_start) -> PromptRows:
+    """The C description of a batch's rows; it keeps the starts alive."""
+    s = PromptRows(num_rows, _ptr(row_start))
+    s._keep = row_start
+    return s
+
+
+def append_desc(qkv, q_gain, k_gain, rms_eps: float, rope_theta: float, positions=None, axis_pairs=None) -> AppendDesc:
+    """The C description of rows to append (qkv fp32 or bf16); it keeps the tensors alive.  axis_pairs: pairs of each
+    axis of `positions` [rows][axes], or None for one axis."""
+    axes = [] if axis_pairs is None else list(axis_pairs)
+    if len(axes) > MAX_AXES:
+        raise ValueError(f"positions have up to {MAX_AXES} axes (got {len(axes)})")
+    s = AppendDesc(_ptr(qkv), _type(qkv, "qkv"), float(rms_eps), _ptr(q_gain), _ptr(k_gain), float(rope_theta), _ptr(positions),
+                   max(1, len(axes)), (ctypes.c_int32 * MAX_AXES)(*axes))
+    s._keep = (qkv, q_gain, k_gain, positions)
+    return s
+
+
+def append_qkv(shape: Shape, rows: PromptRows, desc: AppendDesc, k_cache, v_cache, block_table, seq_lens, q_out, k_ring=None,
+               v_ring=None, n_sink: int = 0, window: int = 0, stream=None) -> None:
+    prepare_append_qkv(shape, rows, desc, k_cache, v_cache, block_table, seq_lens, q_out, k_ring, v_ring, n_sink, window,
+                       stream)()
+
+
+def prompt_plan_size(shape: Shape, rows: PromptRows) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_prompt_plan_size(ctypes.byref(shape.c()), ctypes.byref(rows), ctypes.byref(out)))
+    return out.value
+
+
+def prompt_workspace_size(shape: Shape, rows: PromptRows) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_prompt_workspace_size(ctypes.byref(shape.c()), ctypes.byref(rows), ctypes.byref(out)))
+    return out.value
+
+
+def prompt_plan(shape: Shape, rows: PromptRows, seq_lens, causal: bool, native_window: int, plan,
+                plan_bytes: int | None = None, stream=None) -> None:
+    prepare_prompt_plan(shape, rows, seq_lens, causal, native_window, plan, plan_bytes, stream)()
+
+
+def prompt_attn(shape: Shape, inp: AttnInputs, rows: PromptRows, plan, out, lse, workspace, plan_bytes: int | None = None,
+                workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_prompt_attn(shape, inp, rows, plan, out, lse, workspace, plan_bytes, workspace_bytes, stream)()
+
+
+def logprob_desc(vocab: int, top: int, logits, tokens=None, row_stride: int = 0) -> LogprobDesc:
+    """The C description of rows to score; it keeps the tensors alive."""
+    s = LogprobDesc(vocab, top, row_stride, _ptr(logits), _ptr(tokens))
+    s._keep = (logits, tokens)
+    return s
+
+
+def logprob_workspace_size(desc: LogprobDesc, rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.oda_logprob_workspace_size(ctypes.byref(desc), rows, ctypes.byref(out)))
+    return out.value
+
+
+def token_logprobs(desc: LogprobDesc, rows: int, logprob, rank, entropy, top_logprobs, top_tokens, workspace, work_list=None,
+                   n_work=None, workspace_bytes: int | None = None, stream=None) -> None:
+    prepare_token_logprobs(desc, rows, logprob, rank, entropy, top_logprobs, top_tokens, workspace, work_list, n_work,
+                           workspace_bytes, stream)()
+
+
 def stream_read(src, nbytes: int, sink, groups: int = 0, stream=None) -> None:
     """Measurement aid: read nbytes of src once (the streaming-read ceiling)."""
     _check(_lib.oda_stream_read(_ptr(src), int(nbytes), _ptr(sink), groups, _stream(stream)))
@@ -658,6 +772,38 @@ def prepare_commit_drafts(shape: Shape, tokens: int, k_cache, v_cache, block_tab
             _nbytes(workspace, workspace_bytes), _ptr(k_ring), _ptr(v_ring), n_sink, window, _stream(stream))
     return Call(_lib.oda_commit_drafts, args, (cs, k_cache, v_cache, block_table, seq_lens, k_cand, v_cand, n_accepted,
                                                row_lens, workspace, k_ring, v_ring))
+
+
+def prepare_append_qkv(shape: Shape, rows: PromptRows, desc: AppendDesc, k_cache, v_cache, block_table, seq_lens, q_out,
+                       k_ring=None, v_ring=None, n_sink: int = 0, window: int = 0, stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), ctypes.byref(rows), ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(seq_lens), _ptr(q_out), _ptr(k_ring), _ptr(v_ring), n_sink, window, _stream(stream))
+    return Call(_lib.oda_append_qkv, args, (cs, rows, desc, k_cache, v_cache, block_table, seq_lens, q_out, k_ring, v_ring))
+
+
+def prepare_prompt_plan(shape: Shape, rows: PromptRows, seq_lens, causal: bool, native_window: int, plan,
+                        plan_bytes: int | None = None, stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), ctypes.byref(rows), _ptr(seq_lens), 1 if causal else 0, native_window, _ptr(plan),
+            _nbytes(plan, plan_bytes), _stream(stream))
+    return Call(_lib.oda_prompt_plan, args, (cs, rows, seq_lens, plan))
+
+
+def prepare_prompt_attn(shape: Shape, inp: AttnInputs, rows: PromptRows, plan, out, lse, workspace,
+                        plan_bytes: int | None = None, workspace_bytes: int | None = None, stream=None) -> Call:
+    cs = shape.c()
+    args = (ctypes.byref(cs), ctypes.byref(inp), ctypes.byref(rows), _ptr(plan), _nbytes(plan, plan_bytes), _ptr(out),
+            _type(out, "out"), _ptr(lse), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+    return Call(_lib.oda_prompt_attn, args, (cs, inp, rows, plan, out, lse, workspace))
+
+
+def prepare_token_logprobs(desc: LogprobDesc, rows: int, logprob, rank, entropy, top_logprobs, top_tokens, workspace,
+                           work_list=None, n_work=None, workspace_bytes: int | None = None, stream=None) -> Call:
+    args = (ctypes.byref(desc), rows, _ptr(logprob), _ptr(rank), _ptr(entropy), _ptr(top_logprobs), _ptr(top_tokens),
+            _ptr(work_list), _ptr(n_work), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+    return Call(_lib.oda_token_logprobs, args, (desc, logprob, rank, entropy, top_logprobs, top_tokens, work_list, n_work,
+                                                workspace))
 
 
 def prepare_stream_read(src, nbytes: int, sink, groups: int = 0, stream=None) -> Call:

@@ -1,0 +1,407 @@
+// Log probabilities of given tokens, entropy and the most probable alternatives
+// (oda_token_logprobs).  With m the row's largest logit:
+//
+//   S = sum e^(z - m), T = sum e^(z - m) (m - z)
+//   log p(v) = z_v - m - log S,   H = log S + T / S   (every term >= 0: nothing cancels)
+//
+// One pass over the logits with a running m, S and T per lane; the place of the given
+// token is counted and the first k tokens are kept on the way.  A row is split over
+// workgroups where rows are few; the last of a row's workgroups joins them.
+//
+// Bound by HBM: four bytes a logit, about a dozen vector instructions.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "oda.h"
+#include "oda_internal.h"
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / 64;
+constexpr int kLoads = 4;                     // 16-byte loads of a lane's batch
+constexpr int kBatch = 64 * 4 * kLoads;       // logits of a wavefront's batch
+constexpr int kMaxTop = ODA_MAX_TOP;
+constexpr int kMaxSplits = 64;                // of a row: one per lane where they are joined
+constexpr int kTickets = 1024;                // rows that may be split
+constexpr int kGroups = 1024;                 // workgroups that split rows make at most
+constexpr int kLeastSplit = kWaves * kBatch / 2;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kFar = 1e30f;                 // stands for an infinite distance (its weight is 0)
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // rows start anywhere
+
+struct LogprobArgs {
+  const float* logits;
+  const int32_t* tokens;
+  float* logprob;
+  int32_t* rank;
+  float* entropy;
+  float* top_logprobs;
+  int32_t* top_tokens;
+  const int32_t* work_list;
+  const int32_t* n_work;
+  uint32_t* tickets;       // [kTickets], zero between calls
+  uint64_t* parts;         // [slot][splits][2 + top]: (m, S), (T, ahead), then (logit, token)
+  int64_t stride;
+  int32_t R, V, top, splits, chunk;
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float lane_value(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+__device__ __forceinline__ uint64_t pack(float x, uint32_t y) { return (uint64_t)__float_as_uint(x) << 32 | y; }
+__device__ __forceinline__ float first_of(uint64_t w) { return __uint_as_float((uint32_t)(w >> 32)); }
+// Parts pass between workgroups of different XCDs: write-through stores, loads that
+// bypass the caches.
+__device__ __forceinline__ void publish(uint64_t* p, uint64_t x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t published(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// A running largest logit with the sums of weights against it.
+struct Stat {
+  float m, s, t;
+};
+// The factor of sums against m where they are taken against top >= m (infinite
+// logits weigh 1 against an infinite largest one, everything else 0).
+__device__ __forceinline__ float factor(float m, float top) {
+  return m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * kLog2e);
+}
+__device__ __forceinline__ Stat against(Stat x, float top) {
+  if (x.s == 0.f) return Stat{top, 0.f, 0.f};
+  const float f = factor(x.m, top);
+  const float d = x.m == top ? 0.f : fminf(top - x.m, kFar);
+  return Stat{top, f * x.s, f * (x.t + d * x.s)};
+}
+__device__ __forceinline__ Stat joined(Stat a, Stat b) {
+  const float top = fmaxf(a.m, b.m);
+  a = against(a, top);
+  b = against(b, top);
+  return Stat{top, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ Stat wave_join(Stat x) {
+  float top = x.m;
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+  x = against(x, top);
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) {
+    x.s += __shfl_xor(x.s, s);
+    x.t += __shfl_xor(x.t, s);
+  }
+  return x;
+}
+
+// A wavefront's first tokens: lane i < k holds place i (-infinity, -1: none yet).
+struct Best {
+  float z;
+  int id;
+};
+// A logit above the last place's, behind those that are equal to it.
+__device__ __forceinline__ void insert(Best& best, float z, int id) {
+  const int lane = threadIdx.x & 63;
+  const int at = __builtin_popcountll(__ballot(best.z >= z));
+  const float zs = __shfl_up(best.z, 1);
+  const int is = __shfl_up(best.id, 1);
+  if (lane > at) {
+    best.z = zs;
+    best.id = is;
+  }
+  if (lane == at) {
+    best.z = z;
+    best.id = id;
+  }
+}
+
+__device__ __forceinline__ float log_prob(float z, float m, double log_s) {
+  if (m == -INFINITY) return __builtin_nanf("");
+  if (z == m) return (float)-log_s;
+  return (float)((double)z - (double)m - log_s);
+}
+
+struct Scratch {
+  float m[kWaves], s[kWaves], t[kWaves];
+  int ahead[kWaves];
+  float z[kMaxSplits * kMaxTop];
+  int id[kMaxSplits * kMaxTop];
+  int last;
+};
+
+// Outputs of a row: lane i < k of the wavefront holds place i.
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat x, int ahead, float zt, bool known, Best best) {
+  const int lane = threadIdx.x & 63;
+  const double log_s = log((double)x.s);
+  if (lane < a.top) {
+    const bool there = best.z > -INFINITY;
+    a.top_logprobs[(int64_t)row * a.top + lane] = there ? log_prob(best.z, x.m, log_s) : -INFINITY;
+    a.top_tokens[(int64_t)row * a.top + lane] = there ? best.id : -1;
+  }
+  if (lane != 0) return;
+  if (a.entropy) a.entropy[row] = x.m == -INFINITY ? __builtin_nanf("") : (float)(log_s + (double)x.t / (double)x.s);
+  if (a.logprob) a.logprob[row] = known ? log_prob(zt, x.m, log_s) : __builtin_nanf("");
+  if (a.rank) a.rank[row] = known ? ahead + 1 : 0;
+}
+
+__global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
+  __shared__ Scratch sm;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int slot = blockIdx.x, split = blockIdx.y;
+  const int count = a.n_work ? min(max(a.n_work[0], 0), a.R) : a.R;
+  if (slot >= count) return;
+  const int row = uniform(a.work_list ? a.work_list[slot] : slot);
+  if (row < 0 || row >= a.R) return;
+  const float* z_row = a.logits + (int64_t)row * a.stride;
+  const int token = a.tokens ? uniform(a.tokens[row]) : -1;
+  const bool known = token >= 0 && token < a.V;
+  float zt = known ? fmaxf(z_row[token], -INFINITY) : 0.f;       // (NaN counts as -infinity)
+
+  // the wavefront's logits: one run of the split's, in ascending order
+  const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
+  const int run = ((end - begin + kWaves - 1) / kWaves + 255) & ~255;
+  const int from = min(end, begin + wave * run), to = min(end, from + run);
+  float z[4 * kLoads], next[4 * kLoads];
+  auto load = [&](int v0, float (&x)[4 * kLoads]) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int v = v0 + (u * 64 + lane) * 4;
+      if (v + 4 <= to) {
+        const f32x4u w = *reinterpret_cast<const f32x4u*>(z_row + v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * u + e] = w[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * u + e] = v + e < to ? z_row[v + e] : -INFINITY;
+      }
+    }
+  };
+  Stat x{-INFINITY, 0.f, 0.f};
+  Best best{-INFINITY, -1};
+  float least = -INFINITY;          // the last place's logit
+  int ahead = 0;
+  if (from < to) load(from, next);
+  for (int v0 = from; v0 < to; v0 += kBatch) {
+#pragma unroll
+    for (int i = 0; i < 4 * kLoads; ++i) z[i] = fmaxf(next[i], -INFINITY);
+    if (v0 + kBatch < to) load(v0 + kBatch, next);
+    float top = z[0];
+#pragma unroll
+    for (int i = 1; i < 4 * kLoads; ++i) top = fmaxf(top, z[i]);
+    if (top > x.m) x = against(x, top);
+    if (__any(x.m == INFINITY)) {
+#pragma unroll
+      for (int i = 0; i < 4 * kLoads; ++i) {
+        const float w = z[i] == -INFINITY ? 0.f : factor(z[i], x.m);
+        x.s += w;
+        x.t += w == 0.f ? 0.f : w * (z[i] == x.m ? 0.f : x.m - z[i]);
+      }
+    } else if (x.m != -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < 4 * kLoads; ++i) {
+        const float d = x.m - z[i], w = __builtin_amdgcn_exp2f(-d * kLog2e);
+        x.s += w;
+        x.t += w * fminf(d, kFar);
+      }
+    }
+    if (a.rank) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = v0 + (u * 64 + lane) * 4 + e;
+          const float y = z[4 * u + e];
+          // (past the run's end -infinity stands, which is ahead of nothing there)
+          ahead += y > zt || (y == zt && v < token && v < to) ? 1 : 0;
+        }
+    }
+    if (a.top > 0 && __any(top > least)) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float most = fmaxf(fmaxf(z[4 * u], z[4 * u + 1]), fmaxf(z[4 * u + 2], z[4 * u + 3]));
+        uint64_t todo = __ballot(most > least);
+        while (todo != 0) {
+          const int l = __builtin_ctzll(todo);
+          todo &= todo - 1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float y = lane_value(z[4 * u + e], l);
+            if (y > least) {
+              insert(best, y, v0 + (u * 64 + l) * 4 + e);
+              least = lane_value(best.z, a.top - 1);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // the workgroup's wavefronts
+  x = wave_join(x);
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
+  if (lane == 0) {
+    sm.m[wave] = x.m;
+    sm.s[wave] = x.s;
+    sm.t[wave] = x.t;
+    sm.ahead[wave] = ahead;
+  }
+  if (lane < a.top) {
+    sm.z[wave * a.top + lane] = best.z;
+    sm.id[wave * a.top + lane] = best.id;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+
+  // Joins `lists` lists of k places in LDS, the first lists' tokens before the later
+  // ones' where logits are equal: k rounds over the lists' heads.
+  auto merge = [&](int lists) {
+    Best b{-INFINITY, -1};
+    int at = 0;
+    float head = lane < lists && a.top > 0 ? sm.z[lane * a.top] : -INFINITY;
+    int id = lane < lists && a.top > 0 ? sm.id[lane * a.top] : -1;
+    for (int i = 0; i < a.top; ++i) {
+      float most = head;
+#pragma unroll
+      for (int s = 32; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+      const uint64_t who = __ballot(head == most);
+      const int l = __builtin_ctzll(who);
+      const int taken = __builtin_amdgcn_readlane(id, l);
+      if (lane == i) {
+        b.z = most;
+        b.id = taken;
+      }
+      if (lane == l) {
+        ++at;
+        head = at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
+        id = at < a.top ? sm.id[lane * a.top + at] : -1;
+      }
+    }
+    return b;
+  };
+  x = lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f};
+  x = wave_join(x);
+  ahead = lane < kWaves ? sm.ahead[lane] : 0;
+#pragma unroll
+  for (int s = 4; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
+  ahead = uniform(ahead);
+  best = merge(kWaves);
+  if (a.splits == 1) {
+    write_row(a, row, x, ahead, zt, known, best);
+    return;
+  }
+  const int words = 2 + a.top;
+  uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
+  if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
+  if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
+  if (lane < a.top) publish(part + 2 + lane, pack(best.z, (uint32_t)best.id));
+  __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_wave_barrier();
+  int last = 0;
+  if (lane == 0)
+    last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
+                   (uint32_t)(a.splits - 1)
+               ? 1
+               : 0;
+  if (uniform(last) == 0) return;
+  const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
+  x = Stat{-INFINITY, 0.f, 0.f};
+  ahead = 0;
+  if (lane < a.splits) {
+    const uint64_t p0 = published(parts + (int64_t)lane * words), p1 = published(parts + (int64_t)lane * words + 1);
+    x = Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)};
+    ahead = (int)(uint32_t)p1;
+  }
+  for (int e = lane; e < a.splits * a.top; e += 64) {
+    const int s = e / a.top, i = e - s * a.top;
+    const uint64_t p = published(parts + (int64_t)s * words + 2 + i);
+    sm.z[e] = first_of(p);
+    sm.id[e] = (int)(uint32_t)p;
+  }
+  x = wave_join(x);
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  best = merge(a.splits);
+  write_row(a, row, x, ahead, zt, known, best);
+}
+
+// Workgroups of a row: at most kGroups in all, each of at least kLeastSplit logits.
+void split_row(int64_t rows, int64_t vocab, int* splits, int* chunk) {
+  int64_t n = 1;
+  if (rows <= kTickets)
+    n = std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, kGroups / rows, vocab / kLeastSplit}));
+  *chunk = (int)oda::round_up(oda::ceil_div(vocab, n), 4);
+  *splits = (int)oda::ceil_div(vocab, *chunk);
+}
+
+oda_status check(const oda_logprob_desc* desc, int32_t rows, size_t* bytes, int* splits, int* chunk) {
+  if (desc == nullptr) return oda::fail(ODA_ERR_NULL, "desc is NULL");
+  if (rows < 1) return oda::fail(ODA_ERR_SHAPE, "rows must be >= 1");
+  if (desc->vocab < 1 || desc->vocab > (1 << 30)) return oda::fail(ODA_ERR_SHAPE, "vocab %d not in 1..2^30", desc->vocab);
+  if (desc->top < 0 || desc->top > ODA_MAX_TOP) return oda::fail(ODA_ERR_SHAPE, "top %d not in 0..%d", desc->top, ODA_MAX_TOP);
+  if (desc->row_stride != 0 && desc->row_stride < desc->vocab)
+    return oda::fail(ODA_ERR_SHAPE, "row_stride must be 0 or at least vocab");
+  split_row(rows, desc->vocab, splits, chunk);
+  // (rows that are split have kGroups parts at most, whatever the call's sizes)
+  *bytes = kTickets * 4 + (size_t)kGroups * (2 + ODA_MAX_TOP) * 8;
+  return ODA_OK;
+}
+
+}  // namespace
+
+extern "C" oda_status oda_logprob_workspace_size(const oda_logprob_desc* desc, int32_t rows, size_t* bytes) {
+  int splits, chunk;
+  size_t need;
+  const oda_status st = check(desc, rows, &need, &splits, &chunk);
+  if (st != ODA_OK) return st;
+  if (bytes == nullptr) return oda::fail(ODA_ERR_NULL, "bytes is NULL");
+  *bytes = need;
+  return oda::ok();
+}
+
+extern "C" oda_status oda_token_logprobs(const oda_logprob_desc* desc, int32_t rows, float* logprob, int32_t* rank,
+                                        float* entropy, float* top_logprobs, int32_t* top_tokens,
+                                        const int32_t* work_list, const int32_t* n_work, void* workspace,
+                                        size_t workspace_bytes, hipStream_t stream) {
+  LogprobArgs a;
+  size_t need;
+  const oda_status st = check(desc, rows, &need, &a.splits, &a.chunk);
+  if (st != ODA_OK) return st;
+  if (!desc->logits) return oda::fail(ODA_ERR_NULL, "logits is required");
+  if ((logprob || rank) && !desc->tokens) return oda::fail(ODA_ERR_NULL, "logprob and rank need tokens");
+  if ((top_logprobs == nullptr) != (desc->top == 0) || (top_tokens == nullptr) != (desc->top == 0))
+    return oda::fail(ODA_ERR_NULL, "top_logprobs and top_tokens must be set iff top > 0");
+  if (!logprob && !rank && !entropy && desc->top == 0) return oda::fail(ODA_ERR_NULL, "no output");
+  if ((work_list == nullptr) != (n_work == nullptr))
+    return oda::fail(ODA_ERR_NULL, "work_list and n_work must both be NULL or both be set");
+  if (workspace == nullptr) return oda::fail(ODA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (workspace_bytes < need) return oda::fail(ODA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  if (!oda::aligned(workspace, 256)) return oda::fail(ODA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  a.logits = desc->logits;
+  a.tokens = desc->tokens;
+  a.logprob = logprob;
+  a.rank = rank;
+  a.entropy = entropy;
+  a.top_logprobs = top_logprobs;
+  a.top_tokens = top_tokens;
+  a.work_list = work_list;
+  a.n_work = n_work;
+  a.tickets = static_cast<uint32_t*>(workspace);
+  a.parts = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + kTickets * 4);
+  a.stride = desc->row_stride != 0 ? desc->row_stride : desc->vocab;
+  a.R = rows;
+  a.V = desc->vocab;
+  a.top = desc->top;
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(logprob_kernel, dim3((unsigned)rows, (unsigned)a.splits), dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return oda::fail(ODA_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return oda::ok();
+}
