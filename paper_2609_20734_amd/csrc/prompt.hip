@@ -37,7 +37,6 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 16;            // positions per KV block
 constexpr int kPair = 2 * kBlock;     // positions per score tile
@@ -45,7 +44,7 @@ constexpr int kCols = 32;             // columns of an MFMA tile, of a wavefront
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kTile = kWaves * kCols; // columns of an item
-constexpr int kStageBlocks = 8;       // blocks staged together: one of K and one of V per wavefront
+constexpr int kStageBlocks = 4;       // blocks staged together: one of K or V per wavefront
 constexpr int kMaxBatch = 2048;
 constexpr int kCus = 256;
 constexpr int kPlanThreads = 1024;
@@ -378,9 +377,8 @@ __device__ __forceinline__ bool plan_fits(const PromptArgs& a, const PlanHeader&
 }
 
 __device__ __forceinline__ bf16x8 load16(const uint16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
-__device__ __forceinline__ float bf16_to_float(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
 
-// Two floats to bf16, and what the rounding leaves of them.
+// Two floats to bf16.
 __device__ __forceinline__ uint32_t round_pair(float x, float y) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -399,20 +397,68 @@ __device__ __forceinline__ float column_max(float x) {
 template <typename Out>
 constexpr int kPartsOf = std::is_same<Out, float>::value ? 3 : 1;
 
-// A wavefront's columns (one per lane pair): o[n][4 i + j] is dimension 32 n + 8 i +
-// 4 h + j of column lane % 32, h = lane / 32; c the reference of its weights in
-// exponents of 2 (-infinity: none yet), l this lane's part of their sum; attended
-// positions [lo, hi).
+// A wavefront's columns: o[n][4 i + j] is dimension 32 n + 8 i + 4 h + j of column
+// lane % 32, h = lane / 32; ref the reference of its weights in exponents of 2
+// (-infinity: none yet), sum this lane's part of their sum; attended positions [lo, hi).
 template <int D>
 struct Columns {
   f32x16 o[D / 32];
-  float c, l;
+  float ref, sum;
   int lo, hi;
 };
+// A pair's weights as bf16 parts, by the block.
+template <int P>
+struct Parts {
+  bf16x8 x[P][2];
+};
 
-// Scores of a pair of blocks (this lane: positions 8 h .. 8 h + 7 of either block)
-// into the online softmax; the weights come back as bf16 parts, [0..3] of the first
-// block and [4..7] of the second.
+// S^T = K Q^T of a pair of blocks: [8 b + e] is position 8 h + e of block b.  k(kk): the
+// lane's operand.  Operand row 16 b + r is position r of block b with bits 2 and 3 of r
+// exchanged, so that lane half h gets positions 8 h .. 8 h + 7 of both blocks, which is
+// how it holds V's operand.
+template <int D, typename KOp>
+__device__ __forceinline__ f32x16 score_pair(const bf16x8 (&qf)[D / 16], KOp k) {
+  f32x16 s = {};
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k(kk), qf[kk], s, 0, 0, 0);
+  return s;
+}
+
+template <int P>
+__device__ __forceinline__ Parts<P> parts_of(f32x16 p) {
+  Parts<P> r;
+#pragma unroll
+  for (int q = 0; q < P; ++q) {
+    u32x4 t[2];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t x = round_pair(p[2 * e], p[2 * e + 1]);
+      t[e >> 2][e & 3] = x;
+      if (q + 1 < P) {                 // what the rounding leaves
+        p[2 * e] -= __uint_as_float(x << 16);
+        p[2 * e + 1] -= __uint_as_float(x & 0xffff0000u);
+      }
+    }
+    r.x[q][0] = __builtin_bit_cast(bf16x8, t[0]);
+    r.x[q][1] = __builtin_bit_cast(bf16x8, t[1]);
+  }
+  return r;
+}
+
+// O^T += V^T P^T.  v(n, b): the lane's operand.
+template <int D, int P, typename VOp>
+__device__ __forceinline__ void weigh_pair(const Parts<P>& part, Columns<D>& w, VOp v) {
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const bf16x8 x = v(n, b);
+#pragma unroll
+      for (int q = 0; q < P; ++q) w.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, part.x[q][b], w.o[n], 0, 0, 0);
+    }
+}
+
+// Weights of a pair's scores against the column's reference, and the lane's sum.
 //
 // Weights are taken against a reference kLag above the largest score at which it
 // was set and below no later one: at most 1, and their sum 2^-kLag or more.  The
@@ -421,54 +467,39 @@ struct Columns {
 // NaN).  The reference is kept as the exponent that is taken off, so that all weights
 // of a column are against the same number, to the bit, whatever its size.
 constexpr float kLag = 6.f;
-template <int D, int P>
-__device__ __forceinline__ void softmax_pair(float scale_log2, const f32x16& s, Columns<D>& w, bf16x8 (&part)[P][2]) {
-  float p[16], sum;
-  auto weights = [&](float ref) {
-    float t[4] = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ float weights_of(float scale_log2, const f32x16& s, float ref, f32x16& p) {
+  float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -ref));
-      t[i & 3] += p[i];
-    }
-    sum = (t[0] + t[1]) + (t[2] + t[3]);
-  };
-  weights(w.c);
+  for (int i = 0; i < 16; ++i) {
+    p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -ref));
+    t[i & 3] += p[i];
+  }
+  return (t[0] + t[1]) + (t[2] + t[3]);
+}
+// The sum's check, after all products of earlier pairs: raises the reference where it fails.
+template <int D>
+__device__ __forceinline__ void settle(float scale_log2, const f32x16& s, Columns<D>& w, f32x16& p, float sum) {
   if (__any(!(sum <= 1.f))) {
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    const float c_new = fmaxf(w.c, column_max(mx) * scale_log2 + kLag);
-    const float ref = c_new == -INFINITY ? 0.f : c_new;
-    const float alpha = __builtin_amdgcn_exp2f(w.c - ref);
-    w.c = c_new;
-    w.l *= alpha;
+    const float top = fmaxf(w.ref, column_max(mx) * scale_log2 + kLag);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float alpha = __builtin_amdgcn_exp2f(w.ref - ref);
+    w.ref = top;
+    w.sum *= alpha;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) w.o[n][i] *= alpha;
-    weights(ref);
+    sum = weights_of(scale_log2, s, ref, p);
   }
-  w.l += sum;
-#pragma unroll
-  for (int q = 0; q < P; ++q) {
-    u32x4 r[2];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t x = round_pair(p[2 * e], p[2 * e + 1]);
-      r[e >> 2][e & 3] = x;
-      if (q + 1 < P) {
-        p[2 * e] -= __uint_as_float(x << 16);
-        p[2 * e + 1] -= __uint_as_float(x & 0xffff0000u);
-      }
-    }
-    part[q][0] = __builtin_bit_cast(bf16x8, r[0]);
-    part[q][1] = __builtin_bit_cast(bf16x8, r[1]);
-  }
+  w.sum += sum;
 }
 
 // Scores of positions that a column does not attend.  at: the first block's position
-// of this lane's scores; bad: bit i = block i has no memory (its scores are NaN).
+// of this lane's scores; end: of the item; bad: bit b = block b has no memory (its
+// scores are NaN).
 __device__ __forceinline__ void mask_scores(int at, int lo, int hi, int bad, f32x16& s) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -487,73 +518,56 @@ __device__ __forceinline__ bf16x8 first_values(int room, bf16x8 v) {
     w[i] &= (room > 2 * i ? 0x0000FFFFu : 0u) | (room > 2 * i + 1 ? 0xFFFF0000u : 0u);
   return __builtin_bit_cast(bf16x8, w);
 }
-
-// The largest exponent fields' bits over values (0x7f80 or more: one is not finite).
-__device__ __forceinline__ u16x2 most_of(u16x2 m, bf16x8 v) {
-  const u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
-  return m;
-}
-__device__ __forceinline__ bf16x8 finite_values(bf16x8 v) {
+// Values that are not finite become 0, and are told.
+__device__ __forceinline__ bf16x8 finite_values(bf16x8 v, bool& odd) {
   u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0x0000ffffu;
+    const bool lo = (w[i] & 0x7f80u) == 0x7f80u, hi = (w[i] & 0x7f800000u) == 0x7f800000u;
+    odd |= lo | hi;
+    w[i] &= (lo ? 0u : 0x0000ffffu) | (hi ? 0u : 0xffff0000u);
   }
   return __builtin_bit_cast(bf16x8, w);
 }
-
-// One pair of blocks against a wavefront's columns.  k(kk), v(n, blk): this lane's
-// operands; raw(d, pos): a value of the pair, for the masked form's rare case.
-//
-// K operand rows: row 16 b + r of the tile is position r of block b with bits 2 and 3
-// of r exchanged, so that lane half h gets positions 8 h .. 8 h + 7 of both blocks,
-// which is how it holds V's operand.
-//
-// Masked: a position that one column attends and another does not may hold a value
-// that is not finite, which 0 * V would bring to both.  Such values are taken out of
-// the product and added where they are attended (a weight is positive: it does not
-// change an infinity or NaN).
-template <int D, int P, bool kMasked, typename KOp, typename VOp, typename Raw>
-__device__ __forceinline__ void attend_pair(float scale_log2, const bf16x8 (&qf)[D / 16], Columns<D>& w, int pos, int bad,
-                                            KOp k, VOp v, Raw raw) {
-  f32x16 s = {};
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k(kk), qf[kk], s, 0, 0, 0);
+// Positions that one column attends and another does not may hold values that are not
+// finite, which 0 * V would bring to both.  There such values are taken out of the
+// product (finite_values) and added to the columns that attend them (a weight is
+// positive: it does not change an infinity or NaN).  v0, v1: the pair's blocks.
+template <int D>
+__device__ __forceinline__ void add_odd_values(const uint16_t* v0, const uint16_t* v1, int pos, int end, Columns<D>& w) {
   const int h = (threadIdx.x & 63) >> 5;
-  if (kMasked) mask_scores(pos + 8 * h, w.lo, w.hi, bad, s);
-  bf16x8 part[P][2];
-  softmax_pair<D, P>(scale_log2, s, w, part);
-  bool finite = true;
-  if (kMasked) {
-    u16x2 m = {0, 0};
+#pragma unroll 1
+  for (int i = 0; i < kPair; ++i) {
+    const uint16_t* src = (i < kBlock ? v0 : v1) + 4 * h * kBlock + (i & (kBlock - 1));
+    const bool in = pos + i >= w.lo && pos + i < min(w.hi, end);
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) m = most_of(most_of(m, v(n, 0)), v(n, 1));
-    finite = !__any(m[0] >= 0x7f80 || m[1] >= 0x7f80);
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t x = src[(32 * n + 8 * (r >> 2) + (r & 3)) * kBlock];
+        if (in && (x & 0x7f80u) == 0x7f80u) w.o[n][r] += __uint_as_float(x << 16);
+        __builtin_amdgcn_sched_barrier(0);     // one load at a time: no registers for a rare case
+      }
+  }
+}
+
+// The order of a full step: operands two reads ahead of their product, the weights'
+// exponentials and what belongs to them between the products.
+template <int D, int P>
+__device__ __forceinline__ void interleave() {
+  constexpr int kHalf = D / 16;                             // reads of K, of V
+  __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);        // reads of LDS
+#pragma unroll
+  for (int i = 0; i < kHalf; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // products
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 32 / kHalf, 0);    // vector operations
   }
 #pragma unroll
-  for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      bf16x8 x = v(n, b);
-      if (kMasked && !finite) x = finite_values(x);
-#pragma unroll
-      for (int q = 0; q < P; ++q) w.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, part[q][b], w.o[n], 0, 0, 0);
-    }
-  if (kMasked && !finite) {
-#pragma unroll 1
-    for (int i = 0; i < kPair; ++i) {
-      const bool in = pos + i >= w.lo && pos + i < w.hi;
-#pragma unroll
-      for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint16_t x = raw(32 * n + 8 * (r >> 2) + 4 * h + (r & 3), i);
-          if (in && (x & 0x7f80u) == 0x7f80u) w.o[n][r] += bf16_to_float(x);
-        }
-    }
+  for (int i = 0; i < kHalf; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, P, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 32 / kHalf, 0);
   }
 }
 
@@ -563,23 +577,39 @@ __device__ __forceinline__ void load_columns(const PromptArgs& a, const PlanHead
                                              Columns<D>& w, bf16x8 (&qf)[D / 16]) {
   const int lane = threadIdx.x & 63;
   const int col = first + (lane & 31);
-  const bool in = col < it.ncols;
-  const int at = it.col0 + (in ? col : 0);
+  const int at = it.col0 + (col < it.ncols ? col : 0);       // (past the last column the first again, not written)
   const int token = at / a.G, head = at - token * a.G;
   const uint16_t* q = a.q + ((int64_t)(it.row0 + token) * a.Hq + g * a.G + head) * D + 8 * (lane >> 5);
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) qf[kk] = load16(q + 16 * kk);
   w.hi = h.causal ? it.place0 + token + 1 : it.n;
   w.lo = h.causal && h.window > 0 ? max(0, w.hi - h.window) : 0;
-  w.c = -INFINITY;
-  w.l = 0.f;
+  w.ref = -INFINITY;
+  w.sum = 0.f;
 #pragma unroll
   for (int n = 0; n < D / 32; ++n) w.o[n] = f32x16{};
 }
+// Positions that any, and that every, one of `count` columns from `first` on attends.
+struct Reach {
+  int any_lo, any_hi, all_lo, all_hi;
+};
+__device__ __forceinline__ Reach reach_of(const PromptArgs& a, const PlanHeader& h, const Item& it, int first, int count) {
+  const int end = min(first + count, it.ncols) - 1;
+  if (!h.causal) return Reach{0, first <= end ? it.n : 0, 0, it.n};
+  // columns are in the order of their tokens
+  const int lo = it.place0 + (it.col0 + first) / a.G + 1, hi = it.place0 + (it.col0 + max(first, end)) / a.G + 1;
+  Reach r;
+  r.any_lo = h.window > 0 ? max(0, lo - h.window) : 0;
+  r.all_lo = h.window > 0 ? max(0, hi - h.window) : 0;
+  r.any_hi = first <= end ? hi : 0;
+  r.all_hi = lo;
+  return r;
+}
 
-// LDS: two stages of K and V blocks, or the wavefronts' O where ranges are joined.
-// V's 16-byte groups (eight positions of a dimension) are kept by their half of the
-// block, the halves 16 groups apart modulo the banks.
+// LDS: a ring of four stages of K and V blocks, or the wavefronts' O where ranges are
+// joined.  V's 16-byte groups (eight positions of a dimension) are kept by their half
+// of the block, the halves 16 groups apart modulo the banks.
+constexpr int kStages = 4;
 __host__ __device__ constexpr int v_half(int D) { return D * 8 + 64; }                 // elements
 __host__ __device__ constexpr int k_elems(int D) { return kBlock * D; }
 __host__ __device__ constexpr int v_elems(int D) { return 2 * v_half(D); }
@@ -587,11 +617,11 @@ __host__ __device__ constexpr int stage_elems(int D) { return kStageBlocks * (k_
 __host__ __device__ constexpr int o_stride(int D) { return D + 4; }                    // floats
 __host__ __device__ constexpr int join_bytes(int D) { return kWaves * kCols * o_stride(D) * 4; }
 __host__ __device__ constexpr int data_bytes(int D) {
-  return 2 * stage_elems(D) * 2 > join_bytes(D) ? 2 * stage_elems(D) * 2 : join_bytes(D);
+  return kStages * stage_elems(D) * 2 > join_bytes(D) ? kStages * stage_elems(D) * 2 : join_bytes(D);
 }
-__host__ __device__ constexpr int lds_bytes(int D) { return data_bytes(D) + 2 * kWaves * kCols * 4; }
+__host__ __device__ constexpr int lds_bytes(int D) { return data_bytes(D) + 2 * kWaves * kCols * 4 + kStages * kStageBlocks * 4; }
 static_assert(lds_bytes(128) <= 160 * 1024, "an item fits LDS");
-static_assert(kStageBlocks == kWaves, "a wavefront stages one block of K and one of V");
+static_assert(2 * kStageBlocks == kWaves, "a wavefront stages one block of K or V");
 
 __device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t* p, float4 x) {
@@ -600,9 +630,8 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 x) {
 __device__ __forceinline__ float lse_of(float c, float l) { return l == 0.f ? -INFINITY : (c + __log2f(l)) * kLn2; }
 __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
-// Columns to the partials, or, normalised, to the outputs.  put(col, f): f(d) gives
-// four dimensions from d on.
-template <int D, typename Out>
+// Where a column goes: a partial, or the outputs.
+template <typename Out>
 struct Target {
   Out* out;
   float* lse;
@@ -610,8 +639,8 @@ struct Target {
   float* part_ml;
 };
 template <int D, typename Out>
-__device__ __forceinline__ Target<D, Out> target_of(const PromptArgs& a, const Item& it, int g, int col) {
-  Target<D, Out> t{};
+__device__ __forceinline__ Target<Out> target_of(const PromptArgs& a, const Item& it, int g, int col) {
+  Target<Out> t{};
   if (it.part >= 0) {
     const int64_t at = (int64_t)g * a.part_cols + it.part + col;
     t.part_o = a.part_o + at * D;
@@ -625,20 +654,20 @@ __device__ __forceinline__ Target<D, Out> target_of(const PromptArgs& a, const I
   return t;
 }
 
-// Joins the position ranges (wavefront = range * WC + column tile) and writes.
-template <int D, typename Out>
-__device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g, int wc_shift, Columns<D>& w, char* smem) {
+// Joins position ranges (wavefront = range * WC + column tile) and writes.
+template <int D, int WC, typename Out>
+__device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g, Columns<D>& w, char* smem) {
+  constexpr int WP = kWaves / WC;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int WC = 1 << wc_shift, WP = kWaves >> wc_shift;
   float* sm_o = reinterpret_cast<float*>(smem);                      // [waves][32][D + 4]
   float* sm_c = reinterpret_cast<float*>(smem + data_bytes(D));      // [waves][32]
   float* sm_l = sm_c + kWaves * kCols;
-  const int h = lane >> 5, c = lane & 31;
+  const int h = lane >> 5, at = wave * kCols + (lane & 31);
   if (h == 0) {
-    sm_c[wave * kCols + c] = w.c;
-    sm_l[wave * kCols + c] = w.l;
+    sm_c[at] = w.ref;
+    sm_l[at] = w.sum;
   }
-  float* dst = sm_o + (wave * kCols + c) * o_stride(D) + 4 * h;
+  float* dst = sm_o + at * o_stride(D) + 4 * h;
 #pragma unroll
   for (int n = 0; n < D / 32; ++n)
 #pragma unroll
@@ -650,21 +679,23 @@ __device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g,
     const int d = e % (D / 4) * 4, col = e / (D / 4);
     if (col >= it.ncols) break;
     float top = -INFINITY;
+#pragma unroll
     for (int p = 0; p < WP; ++p) top = fmaxf(top, sm_c[p * WC * kCols + col]);
     const float ref = top == -INFINITY ? 0.f : top;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
+#pragma unroll
     for (int p = 0; p < WP; ++p) {
-      const int at = p * WC * kCols + col;
-      const float s = __builtin_amdgcn_exp2f(sm_c[at] - ref);
-      const float4 x = *reinterpret_cast<const float4*>(sm_o + at * o_stride(D) + d);
+      const int from = p * WC * kCols + col;
+      const float s = __builtin_amdgcn_exp2f(sm_c[from] - ref);
+      const float4 x = *reinterpret_cast<const float4*>(sm_o + from * o_stride(D) + d);
       acc.x += s * x.x;
       acc.y += s * x.y;
       acc.z += s * x.z;
       acc.w += s * x.w;
-      l += s * sm_l[at];
+      l += s * sm_l[from];
     }
-    const Target<D, Out> t = target_of<D, Out>(a, it, g, col);
+    const Target<Out> t = target_of<D, Out>(a, it, g, col);
     if (it.part >= 0) {
       store4(t.part_o + d, acc);
       if (d == 0) *reinterpret_cast<float2*>(t.part_ml) = make_float2(ref, l);
@@ -681,9 +712,9 @@ template <int D, typename Out>
 __device__ __forceinline__ void write_columns(const PromptArgs& a, const Item& it, int g, int first, const Columns<D>& w) {
   const int lane = threadIdx.x & 63, h = lane >> 5, col = first + (lane & 31);
   if (col >= it.ncols) return;
-  const Target<D, Out> t = target_of<D, Out>(a, it, g, col);
-  const float ref = w.c == -INFINITY ? 0.f : w.c;
-  const float inv = it.part >= 0 ? 1.f : inverse_of(w.l);
+  const Target<Out> t = target_of<D, Out>(a, it, g, col);
+  const float ref = w.ref == -INFINITY ? 0.f : w.ref;
+  const float inv = it.part >= 0 ? 1.f : inverse_of(w.sum);
 #pragma unroll
   for (int n = 0; n < D / 32; ++n)
 #pragma unroll
@@ -695,12 +726,12 @@ __device__ __forceinline__ void write_columns(const PromptArgs& a, const Item& i
       else store4(t.out + d, x);
     }
   if (h != 0) return;
-  if (it.part >= 0) *reinterpret_cast<float2*>(t.part_ml) = make_float2(ref, w.l);
-  else if (t.lse) *t.lse = lse_of(ref, w.l);
+  if (it.part >= 0) *reinterpret_cast<float2*>(t.part_ml) = make_float2(ref, w.sum);
+  else if (t.lse) *t.lse = lse_of(ref, w.sum);
 }
 
-// One column tile: the wavefronts take contiguous ranges of pairs, K and V go
-// straight to registers.
+// One column tile: the wavefronts take contiguous ranges of pairs, K and V go straight
+// to registers.
 template <int D, typename Out>
 __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader& head, const Item& it, int g, char* smem) {
   constexpr int P = kPartsOf<Out>;
@@ -715,30 +746,22 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
   Columns<D> w;
   bf16x8 qf[D / 16];
   load_columns<D>(a, head, it, g, 0, w, qf);
+  const Reach reach = reach_of(a, head, it, 0, kCols);
   const int64_t blk_stride = (int64_t)a.Hkv * k_elems(D);
   const int pos16 = (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1);
   const uint16_t* kbase = a.k_cache + (int64_t)g * k_elems(D) + (h * kBlock + pos16) * 8;
   const uint16_t* vbase = a.v_cache + (int64_t)g * k_elems(D) + m * kBlock + 8 * h;
-  // positions that every column attends
-  int all_lo = m < it.ncols ? w.lo : 0, all_hi = m < it.ncols ? w.hi : INT_MAX;
-#pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) {
-    all_lo = max(all_lo, __shfl_xor(all_lo, s));
-    all_hi = min(all_hi, __shfl_xor(all_hi, s));
-  }
-  all_lo = uniform(all_lo);
-  all_hi = uniform(all_hi);
+  const int end = hi * kBlock;
   int tbl = 0;
   for (int v = lo; v < hi; v += 2) {
     const int i0 = (v - lo) & 63;
     if (i0 == 0) {
-      if (v != lo) entry = v + lane < hi ? table[v + lane] : 0;
       tbl = entry >= 0 && entry < a.num_blocks ? entry : -1;
+      entry = v + 64 + lane < hi ? table[v + 64 + lane] : 0;
     }
-    // (past an odd end the first block again, masked: no column attends it)
-    const bool has1 = v + 1 < hi;
+    // (past an odd end the first block again: no column attends it)
     const int e0 = __builtin_amdgcn_readlane(tbl, i0);
-    const int e1 = has1 ? __builtin_amdgcn_readlane(tbl, i0 + 1) : e0;
+    const int e1 = v + 1 < hi ? __builtin_amdgcn_readlane(tbl, i0 + 1) : e0;
     const int bad = (e0 < 0 ? 1 : 0) | (e1 < 0 ? 2 : 0);
     const int64_t b0 = (int64_t)max(e0, 0) * blk_stride, b1 = (int64_t)max(e1, 0) * blk_stride;
     const int64_t kb = m < kBlock ? b0 : b1;
@@ -751,156 +774,227 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
       vr[n][1] = load16(vbase + b1 + n * 32 * kBlock);
     }
     const int pos = v * kBlock;
-    auto raw = [&](int d, int i) {
-      const uint16_t* src = a.v_cache + (int64_t)g * k_elems(D) + (i < kBlock ? b0 : b1);
-      return src[d * kBlock + (i & (kBlock - 1))];
-    };
-    auto k = [&](int kk) { return kr[kk]; };
-    auto vv = [&](int n, int b) { return vr[n][b]; };
-    if (has1 && bad == 0 && pos >= all_lo && pos + kPair <= all_hi) {
-      attend_pair<D, P, false>(a.scale_log2, qf, w, pos, 0, k, vv, raw);
-    } else {
+    f32x16 s = score_pair<D>(qf, [&](int kk) { return kr[kk]; });
+    bool odd = false;
+    if (v + 1 >= hi || bad != 0 || pos < reach.all_lo || pos + kPair > reach.all_hi) {
+      mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s);
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n)     // slots behind the history may hold anything
+      for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) vr[n][b] = first_values(it.n - pos - kBlock * b - 8 * h, vr[n][b]);
-      const int hi_all = w.hi;
-      w.hi = min(w.hi, hi * kBlock);       // the block beyond an odd end is another wavefront's
-      attend_pair<D, P, true>(a.scale_log2, qf, w, pos, bad, k, vv, raw);
-      w.hi = hi_all;
+        for (int b = 0; b < 2; ++b) vr[n][b] = finite_values(first_values(it.n - pos - kBlock * b - 8 * h, vr[n][b]), odd);
+    }
+    f32x16 p;
+    const float sum = weights_of(a.scale_log2, s, w.ref, p);
+    settle<D>(a.scale_log2, s, w, p, sum);
+    weigh_pair<D, P>(parts_of<P>(p), w, [&](int n, int b) { return vr[n][b]; });
+    if (__any(odd)) {
+      const uint16_t* v0 = a.v_cache + (int64_t)g * k_elems(D);
+      add_odd_values<D>(v0 + b0, v0 + b1, pos, end, w);
     }
   }
-  w.l += __shfl_xor(w.l, 32);
-  join<D, Out>(a, it, g, 0, w, smem);
+  w.sum += __shfl_xor(w.sum, 32);
+  join<D, 1, Out>(a, it, g, w, smem);
 }
 
-// More column tiles: K and V are staged through LDS, eight blocks a stage (wavefront
-// i brings block i while the stage before it is used).  Up to 64 and 128 columns the
-// wavefronts are four and two position ranges, which share a stage's pairs
-// alternately; more: every wavefront goes through all pairs with its 32 columns.
-template <int D, typename Out>
-__device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& head, const Item& it, int g, int wc_shift,
-                                         char* smem) {
+// More column tiles: K and V are staged through LDS, four blocks a stage, a wavefront
+// bringing one of them.  Up to 128 columns two position ranges share a stage's pairs;
+// more: every wavefront goes through all pairs with its 32 columns.
+//
+// While the weights of pair i are formed (vector operations), the matrix cores form the
+// scores of the wavefront's next pair and add the products of the one before.  That
+// reads stages st - 1 to st + 1 in one round while st + 2 is written: a ring of four,
+// one barrier a stage.
+template <int D, int WC, typename Out>
+__device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& head, const Item& it, int g, char* smem) {
   constexpr int P = kPartsOf<Out>;
+  constexpr int WP = kWaves / WC;                    // 1 or 2
   constexpr int kLoads = k_elems(D) / 512;           // 16-byte loads of a block per lane
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int h = lane >> 5, m = lane & 31;
-  const int WP = kWaves >> wc_shift;
-  const int wc = wave & ((1 << wc_shift) - 1), wp = wave >> wc_shift;
+  const int wc = wave & (WC - 1), wp = wave / WC;
   const int blocks = it.blk_hi - it.blk_lo;
   const int stages = (blocks + kStageBlocks - 1) / kStageBlocks;
   const int32_t* table = a.block_table + (int64_t)it.request * a.MB + it.blk_lo;
-  int entry = lane < blocks ? table[lane] : 0;       // 64 blocks, eight stages
+  int entry = lane < blocks ? table[lane] : 0;       // 64 blocks, sixteen stages
   Columns<D> w;
   bf16x8 qf[D / 16];
   load_columns<D>(a, head, it, g, wc * kCols, w, qf);
-  // positions that any, and that every, column of the wavefront attends
-  const bool in = wc * kCols + m < it.ncols;
-  int any_lo = in ? w.lo : INT_MAX, any_hi = in ? w.hi : 0, all_lo = in ? w.lo : 0, all_hi = in ? w.hi : INT_MAX;
-#pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) {
-    any_lo = min(any_lo, __shfl_xor(any_lo, s));
-    any_hi = max(any_hi, __shfl_xor(any_hi, s));
-    all_lo = max(all_lo, __shfl_xor(all_lo, s));
-    all_hi = min(all_hi, __shfl_xor(all_hi, s));
-  }
-  any_lo = uniform(any_lo);
-  any_hi = uniform(any_hi);
-  all_lo = uniform(all_lo);
-  all_hi = uniform(all_hi);
+  const Reach own = reach_of(a, head, it, wc * kCols, kCols), all = reach_of(a, head, it, 0, it.ncols);
+  const int base_pos = it.blk_lo * kBlock, end = it.blk_hi * kBlock;
+  // the column tile's pairs
+  const int own_end = min(own.any_hi, end) - base_pos;
+  const int first = max(0, own.any_lo - base_pos) / kPair, last = own_end > 0 ? (own_end + kPair - 1) / kPair : 0;
 
   const int64_t blk_stride = (int64_t)a.Hkv * k_elems(D);
   const int64_t base = (int64_t)g * k_elems(D);
   uint16_t* lds = reinterpret_cast<uint16_t*>(smem);
-  bf16x8 kr[kLoads], vr[kLoads];
-  int tbl_next = 0, bad_next = 0;    // of the stage that is fetched: valid entry of block i in lane 8 (st % 8) + i
+  int* sm_odd = reinterpret_cast<int*>(smem + lds_bytes(D) - kStages * kStageBlocks * 4);     // [stage][block]
+  const bool brings_v = wave >= kStageBlocks;
+  const int mine = wave & (kStageBlocks - 1);
+  const uint16_t* cache = (brings_v ? a.v_cache : a.k_cache) + base + lane * 8;
+  bf16x8 fr[kLoads];
+  int tbl = 0;
+  uint32_t bad_ring = 0;             // of the stages, four bits each, the one fetched last in the low ones
   auto fetch = [&](int st) {
-    if ((st & 7) == 0) {
-      tbl_next = entry >= 0 && entry < a.num_blocks ? entry : -1;
-      const int next = (st + 8) * kStageBlocks + lane;       // asked for eight stages ahead
+    if ((st & 15) == 0) {
+      tbl = entry >= 0 && entry < a.num_blocks ? entry : -1;
+      const int next = (st + 16) * kStageBlocks + lane;       // asked for sixteen stages ahead
       entry = next < blocks ? table[next] : 0;
     }
-    const int i0 = (st & 7) * kStageBlocks;
-    bad_next = (int)((__ballot(tbl_next < 0) >> i0) & 0xff);
-    const int e = __builtin_amdgcn_readlane(tbl_next, i0 + wave);
-    const int64_t at = (int64_t)max(e, 0) * blk_stride + base + lane * 8;
+    const int i0 = (st & 15) * kStageBlocks;
+    bad_ring = bad_ring << 4 | (uint32_t)((__ballot(tbl < 0) >> i0) & 0xf);
+    const uint16_t* src = cache + (int64_t)max(__builtin_amdgcn_readlane(tbl, i0 + mine), 0) * blk_stride;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      kr[i] = load16(a.k_cache + at + i * 512);
-      vr[i] = load16(a.v_cache + at + i * 512);
-    }
+    for (int i = 0; i < kLoads; ++i) fr[i] = load16(src + i * 512);
   };
-  // lane's group of V: dimension lane / 2 (+ 32 per load), half lane % 2
-  uint16_t* k_put = lds + wave * k_elems(D) + lane * 8;
-  uint16_t* v_put = lds + kStageBlocks * k_elems(D) + wave * v_elems(D) + (lane & 1) * v_half(D) + (lane >> 1) * 8;
+  // a lane's group of V: dimension lane / 2 (+ 32 per load), half lane % 2
+  uint16_t* put_at = brings_v ? lds + kStageBlocks * k_elems(D) + mine * v_elems(D) + (lane & 1) * v_half(D) + (lane >> 1) * 8
+                              : lds + mine * k_elems(D) + lane * 8;
+  const int put_step = brings_v ? 256 : 512;
   auto put = [&](int st) {
-    const int off = (st & 1) * stage_elems(D);
-    const int room = it.n - (it.blk_lo + st * kStageBlocks + wave) * kBlock;
-    if (room < kBlock) {             // the history ends in or before this block: slots behind it may hold anything
+    const int pos = base_pos + st * kStageBlocks * kBlock;
+    if (brings_v) {
+      int told = 0;
+      if ((bad_ring >> mine) & 1) {        // no memory: the block's attended weights are NaN, the others 0
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) vr[i] = first_values(room - 8 * (lane & 1), vr[i]);
-    }
+        for (int i = 0; i < kLoads; ++i) fr[i] = bf16x8{};
+      } else if (pos < all.all_lo || pos + kStageBlocks * kBlock > all.all_hi) {
+        const int room = it.n - pos - mine * kBlock - 8 * (lane & 1);
+        bool odd = false;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      *reinterpret_cast<bf16x8*>(k_put + off + i * 512) = kr[i];
-      *reinterpret_cast<bf16x8*>(v_put + off + i * 256) = vr[i];
+        for (int i = 0; i < kLoads; ++i) fr[i] = finite_values(first_values(room, fr[i]), odd);
+        told = __any(odd) ? 1 : 0;
+      }
+      if (lane == 0) sm_odd[(st & (kStages - 1)) * kStageBlocks + mine] = told;
     }
+    uint16_t* dst = put_at + (st & (kStages - 1)) * stage_elems(D);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<bf16x8*>(dst + i * put_step) = fr[i];
   };
   const int pos16 = (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1);
   const uint16_t* k_get = lds + (m >> 4) * k_elems(D) + (h * kBlock + pos16) * 8;
   const uint16_t* v_get = lds + kStageBlocks * k_elems(D) + h * v_half(D) + m * 8;
-  const uint16_t* v_raw = lds + kStageBlocks * k_elems(D);
+  auto stage_of = [&](int i) { return ((i >> 1) & (kStages - 1)) * stage_elems(D); };
 
-  int bad = 0;
-  if (stages > 0) {
-    fetch(0);
-    bad = bad_next;
-    put(0);
-    if (stages > 1) fetch(1);
-  }
-  __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    const int off = (st & 1) * stage_elems(D);
-    for (int pr = wp; pr < kStageBlocks / 2; pr += WP) {
-      const int pos = (it.blk_lo + st * kStageBlocks + 2 * pr) * kBlock;
-      if (pos >= min(any_hi, it.blk_hi * kBlock)) break;
-      if (pos + kPair <= any_lo) continue;
-      const uint16_t* ks = k_get + off + 2 * pr * k_elems(D);
-      const uint16_t* vs = v_get + off + 2 * pr * v_elems(D);
-      const uint16_t* vraw = v_raw + off + 2 * pr * v_elems(D);
-      auto k = [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); };
-      auto v = [&](int n, int b) { return load16(vs + b * v_elems(D) + n * 32 * 8); };
-      auto raw = [&](int d, int i) {
-        return vraw[(i >> 4) * v_elems(D) + ((i >> 3) & 1) * v_half(D) + d * 8 + (i & 7)];
-      };
-      const int b = (bad >> (2 * pr)) & 3;
-      if (b == 0 && pos >= all_lo && pos + kPair <= min(all_hi, it.blk_hi * kBlock)) {
-        attend_pair<D, P, false>(a.scale_log2, qf, w, pos, 0, k, v, raw);
-      } else {
-        const int hi_all = w.hi;
-        w.hi = min(w.hi, it.blk_hi * kBlock);
-        attend_pair<D, P, true>(a.scale_log2, qf, w, pos, b, k, v, raw);
-        w.hi = hi_all;
+  f32x16 s;              // scores of the pair whose weights come next
+  Parts<P> part;         // weights of the pair before
+  auto keys_of = [&](int i) { return k_get + stage_of(i) + (i & 1) * 2 * k_elems(D); };
+  auto values_of = [&](int i) { return v_get + stage_of(i) + (i & 1) * 2 * v_elems(D); };
+  auto scores = [&](int i) {
+    const uint16_t* ks = keys_of(i);
+    return score_pair<D>(qf, [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); });
+  };
+  auto products = [&](int i) {
+    const uint16_t* vs = values_of(i);
+    weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * v_elems(D) + n * 32 * 8); });
+  };
+  // pair i's weights beside the next pair's scores and the products of the one before,
+  // whichever of them there are; bad: pair i's blocks
+  auto step = [&](int i, int bad) {
+    const int j = i + WP, k0 = i - WP;
+    const bool next = j >= first && j < last, now = i >= first && i < last, before = k0 >= first && k0 < last;
+    const int pos = base_pos + i * kPair, pos0 = base_pos + k0 * kPair;
+    f32x16 s_next = {}, p = {};
+    float sum = 0.f;
+    if (next) s_next = scores(j);
+    if (now && (bad != 0 || pos < own.all_lo || pos + kPair > min(own.all_hi, end)))
+      mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s);
+    if (now) sum = weights_of(a.scale_log2, s, w.ref, p);
+    if (before) {
+      products(k0);
+      if (pos0 < all.all_lo || pos0 + kPair > all.all_hi) {    // its values may have been taken out
+        const int blk = 2 * k0;
+        const int* odd = sm_odd + ((blk >> 2) & (kStages - 1)) * kStageBlocks + (blk & 2);
+        if (uniform(odd[0] | odd[1]) != 0) {
+          int64_t at[2];
+          for (int b = 0; b < 2; ++b) {
+            const int e = blk + b < blocks ? table[blk + b] : 0;
+            at[b] = (int64_t)(e >= 0 && e < a.num_blocks ? e : 0) * blk_stride + base;
+          }
+          add_odd_values<D>(a.v_cache + at[0], a.v_cache + at[1], pos0, end, w);
+        }
       }
     }
-    // the other buffer was last read before the barrier that ended the stage before
-    if (st + 1 < stages) {
-      bad = bad_next;
-      put(st + 1);
-      if (st + 2 < stages) fetch(st + 2);
+    if (now) {
+      settle<D>(a.scale_log2, s, w, p, sum);
+      part = parts_of<P>(p);
     }
+    s = s_next;
+  };
+  // the same where all three are there and nothing is masked
+  auto full_step = [&](int i, f32x16& s_now, f32x16& s_next) {
+    f32x16 p;
+    s_next = scores(i + WP);
+    const float sum = weights_of(a.scale_log2, s_now, w.ref, p);
+    products(i - WP);
+    interleave<D, P>();
+    settle<D>(a.scale_log2, s_now, w, p, sum);
+    part = parts_of<P>(p);
+  };
+  // pairs whose steps are full: of no bad block, after the first and before the last
+  const int full_lo = max(first + WP, (max(all.all_lo, own.all_lo) - base_pos + kPair - 1) / kPair + WP);
+  const int full_hi = min(last - WP, (min(min(all.all_hi, own.all_hi), end) - base_pos) / kPair);
+
+  if (stages > 0) {
+    fetch(0);
+    put(0);
+    if (stages > 1) {
+      fetch(1);
+      put(1);
+    } else {
+      bad_ring <<= 4;
+    }
+    if (stages > 2) fetch(2);
+    else bad_ring <<= 4;
     __syncthreads();
+    step(wp - WP, 0);
+    // (the stage written in a round was last read in the one before its barrier)
+    auto advance = [&](int st) {
+      if (st + 2 < stages) put(st + 2);
+      if (st + 3 < stages) fetch(st + 3);
+      else bad_ring <<= 4;
+    };
+    auto bad_now = [&] { return (int)(bad_ring >> 12) & 0xf; };
+    auto is_full = [&](int st) {       // before advance
+      return WP == 1 && ((bad_ring >> 8) & 0xf) == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi;
+    };
+    // (loops of their own, so that a path's registers need not be the other's)
+    for (int st = 0; st < stages;) {
+      for (; st < stages && is_full(st); ++st) {
+        advance(st);
+        f32x16 t;
+        full_step(2 * st, s, t);
+        full_step(2 * st + 1, t, s);
+        __syncthreads();
+      }
+      for (; st < stages && !is_full(st); ++st) {
+        advance(st);
+        const int bad = bad_now();
+        if (WP == 1) {
+#pragma unroll 1
+          for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3);
+        } else {
+          step(2 * st + wp, (bad >> (2 * wp)) & 3);
+        }
+        __syncthreads();
+      }
+    }
+    step(2 * stages + wp, 0);
   }
-  w.l += __shfl_xor(w.l, 32);
-  if (wc_shift != 3) join<D, Out>(a, it, g, wc_shift, w, smem);
-  else write_columns<D, Out>(a, it, g, wc * kCols, w);
+  w.sum += __shfl_xor(w.sum, 32);
+  if (WP > 1) {
+    __syncthreads();
+    join<D, WC, Out>(a, it, g, w, smem);
+  } else {
+    write_columns<D, Out>(a, it, g, wc * kCols, w);
+  }
 }
 
 __device__ __forceinline__ void put_nan(float* p) { *p = __builtin_nanf(""); }
 __device__ __forceinline__ void put_nan(uint16_t* p) { *p = 0x7fc0; }
 
 template <int D, typename Out>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void prompt_attn_kernel(PromptArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const PlanHeader h = *reinterpret_cast<const PlanHeader*>(a.plan);
@@ -917,7 +1011,7 @@ void prompt_attn_kernel(PromptArgs a) {
   if (i >= min(h.n_items, a.max_items)) return;
   if (it.n < 0) {                    // a request whose length is out of range
     for (int e = threadIdx.x; e < it.ncols * D; e += kThreads) {
-      const Target<D, Out> t = target_of<D, Out>(a, it, g, e / D);
+      const Target<Out> t = target_of<D, Out>(a, it, g, e / D);
       put_nan(t.out + e % D);
       if (t.lse && e % D == 0) put_nan(t.lse);
     }
@@ -925,7 +1019,8 @@ void prompt_attn_kernel(PromptArgs a) {
   }
   const int tiles = (it.ncols + kCols - 1) / kCols;
   if (tiles == 1) run_narrow<D, Out>(a, h, it, g, smem);
-  else run_wide<D, Out>(a, h, it, g, tiles <= 2 ? 1 : tiles <= 4 ? 2 : 3, smem);
+  else if (tiles <= kWaves / 2) run_wide<D, kWaves / 2, Out>(a, h, it, g, smem);
+  else run_wide<D, kWaves, Out>(a, h, it, g, smem);
 }
 
 // One workgroup per (split tile, KV head, kCols columns): the ranges in order.
