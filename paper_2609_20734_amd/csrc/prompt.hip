@@ -551,16 +551,15 @@ __device__ __forceinline__ void add_odd_values(const uint16_t* v0, const uint16_
   }
 }
 
-// The order of a full step: operands two reads ahead of their product, the weights'
-// exponentials and what belongs to them between the products.
+// The order of a full step: beside each product one operand's read, for a product of
+// the other kind, and a share of the weights' vector operations.
 template <int D, int P>
 __device__ __forceinline__ void interleave() {
   constexpr int kHalf = D / 16;                             // reads of K, of V
-  __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);        // reads of LDS
 #pragma unroll
   for (int i = 0; i < kHalf; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // products
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // reads of LDS
     __builtin_amdgcn_sched_group_barrier(0x002, 32 / kHalf, 0);    // vector operations
   }
 #pragma unroll
@@ -606,22 +605,53 @@ __device__ __forceinline__ Reach reach_of(const PromptArgs& a, const PlanHeader&
   return r;
 }
 
-// LDS: a ring of four stages of K and V blocks, or the wavefronts' O where ranges are
-// joined.  V's 16-byte groups (eight positions of a dimension) are kept by their half
-// of the block, the halves 16 groups apart modulo the banks.
+// LDS: a ring of four stages of K blocks and one of V blocks, or the wavefronts' O where
+// ranges are joined.  Blocks lie as in the cache, but for V's 16-byte groups (eight
+// positions of a dimension), whose halves are exchanged in every other eight dimensions:
+// sixteen lanes' operand reads then meet all banks.
 constexpr int kStages = 4;
-__host__ __device__ constexpr int v_half(int D) { return D * 8 + 64; }                 // elements
-__host__ __device__ constexpr int k_elems(int D) { return kBlock * D; }
-__host__ __device__ constexpr int v_elems(int D) { return 2 * v_half(D); }
-__host__ __device__ constexpr int stage_elems(int D) { return kStageBlocks * (k_elems(D) + v_elems(D)); }
+__host__ __device__ constexpr int block_elems(int D) { return kBlock * D; }
+__host__ __device__ constexpr int stage_elems(int D) { return kStageBlocks * block_elems(D); }
 __host__ __device__ constexpr int o_stride(int D) { return D + 4; }                    // floats
 __host__ __device__ constexpr int join_bytes(int D) { return kWaves * kCols * o_stride(D) * 4; }
 __host__ __device__ constexpr int data_bytes(int D) {
-  return kStages * stage_elems(D) * 2 > join_bytes(D) ? kStages * stage_elems(D) * 2 : join_bytes(D);
+  return 2 * kStages * stage_elems(D) * 2 > join_bytes(D) ? 2 * kStages * stage_elems(D) * 2 : join_bytes(D);
 }
 __host__ __device__ constexpr int lds_bytes(int D) { return data_bytes(D) + 2 * kWaves * kCols * 4 + kStages * kStageBlocks * 4; }
 static_assert(lds_bytes(128) <= 160 * 1024, "an item fits LDS");
-static_assert(2 * kStageBlocks == kWaves, "a wavefront stages one block of K or V");
+static_assert(2 * kStageBlocks == kWaves, "a wavefront brings one block of K or V");
+
+// A block from memory straight to LDS: 1 KiB per load, lane i's 16 bytes to place i.
+// (In assembly, as the compiler would wait for all of them before any read of LDS.  No
+// registers are written; the address is read when the load is issued; the caller waits
+// with wait_loads and a barrier before the block is read.)
+template <int D>
+__device__ __forceinline__ void load_to_lds(const uint16_t* src, uint32_t dst) {
+  if constexpr (D == 128)
+    asm volatile(
+        "s_mov_b32 m0, %1\n\t"
+        "global_load_lds_dwordx4 %0, off\n\t"
+        "global_load_lds_dwordx4 %0, off offset:1024\n\t"
+        "global_load_lds_dwordx4 %0, off offset:2048\n\t"
+        "global_load_lds_dwordx4 %0, off offset:3072"
+        :
+        : "v"(src), "s"(dst)
+        : "memory", "m0");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %1\n\t"
+        "global_load_lds_dwordx4 %0, off\n\t"
+        "global_load_lds_dwordx4 %0, off offset:1024"
+        :
+        : "v"(src), "s"(dst)
+        : "memory", "m0");
+}
+// Waits for all of this wavefront's loads but one block's (the one issued last), or all.
+template <int D>
+__device__ __forceinline__ void wait_loads(bool but_one) {
+  if (!but_one) __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
+  else __builtin_amdgcn_s_waitcnt(D == 128 ? 0x0f74 : 0x0f72);   // vmcnt(4), vmcnt(2)
+}
 
 __device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t* p, float4 x) {
@@ -747,10 +777,10 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
   bf16x8 qf[D / 16];
   load_columns<D>(a, head, it, g, 0, w, qf);
   const Reach reach = reach_of(a, head, it, 0, kCols);
-  const int64_t blk_stride = (int64_t)a.Hkv * k_elems(D);
+  const int64_t blk_stride = (int64_t)a.Hkv * block_elems(D);
   const int pos16 = (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1);
-  const uint16_t* kbase = a.k_cache + (int64_t)g * k_elems(D) + (h * kBlock + pos16) * 8;
-  const uint16_t* vbase = a.v_cache + (int64_t)g * k_elems(D) + m * kBlock + 8 * h;
+  const uint16_t* kbase = a.k_cache + (int64_t)g * block_elems(D) + (h * kBlock + pos16) * 8;
+  const uint16_t* vbase = a.v_cache + (int64_t)g * block_elems(D) + m * kBlock + 8 * h;
   const int end = hi * kBlock;
   int tbl = 0;
   for (int v = lo; v < hi; v += 2) {
@@ -788,7 +818,7 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
     settle<D>(a.scale_log2, s, w, p, sum);
     weigh_pair<D, P>(parts_of<P>(p), w, [&](int n, int b) { return vr[n][b]; });
     if (__any(odd)) {
-      const uint16_t* v0 = a.v_cache + (int64_t)g * k_elems(D);
+      const uint16_t* v0 = a.v_cache + (int64_t)g * block_elems(D);
       add_odd_values<D>(v0 + b0, v0 + b1, pos, end, w);
     }
   }
@@ -801,14 +831,13 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
 // more: every wavefront goes through all pairs with its 32 columns.
 //
 // While the weights of pair i are formed (vector operations), the matrix cores form the
-// scores of the wavefront's next pair and add the products of the one before.  That
-// reads stages st - 1 to st + 1 in one round while st + 2 is written: a ring of four,
-// one barrier a stage.
+// scores of the wavefront's next pair and add the products of the one before: round st
+// reads K of stages st and st + 1 and V of st - 1 and st, one barrier a round.  K of
+// st + 3 and V of st + 2 are asked for in round st, so that a load has two rounds.
 template <int D, int WC, typename Out>
 __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& head, const Item& it, int g, char* smem) {
   constexpr int P = kPartsOf<Out>;
   constexpr int WP = kWaves / WC;                    // 1 or 2
-  constexpr int kLoads = k_elems(D) / 512;           // 16-byte loads of a block per lane
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int h = lane >> 5, m = lane & 31;
   const int wc = wave & (WC - 1), wp = wave / WC;
@@ -825,68 +854,70 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
   const int own_end = min(own.any_hi, end) - base_pos;
   const int first = max(0, own.any_lo - base_pos) / kPair, last = own_end > 0 ? (own_end + kPair - 1) / kPair : 0;
 
-  const int64_t blk_stride = (int64_t)a.Hkv * k_elems(D);
-  const int64_t base = (int64_t)g * k_elems(D);
+  const int64_t blk_stride = (int64_t)a.Hkv * block_elems(D);
+  const int64_t base = (int64_t)g * block_elems(D);
   uint16_t* lds = reinterpret_cast<uint16_t*>(smem);
+  uint16_t* lds_v = lds + kStages * stage_elems(D);
   int* sm_odd = reinterpret_cast<int*>(smem + lds_bytes(D) - kStages * kStageBlocks * 4);     // [stage][block]
   const bool brings_v = wave >= kStageBlocks;
+  const int lead = brings_v ? 2 : 3;                 // stages from the round's to the one asked for
   const int mine = wave & (kStageBlocks - 1);
-  const uint16_t* cache = (brings_v ? a.v_cache : a.k_cache) + base + lane * 8;
-  bf16x8 fr[kLoads];
+  const int v_swap = (lane >> 4) & 1;                // whether the lane's group of V is its dimension's other half
+  const uint16_t* cache = brings_v ? a.v_cache + base + (lane ^ v_swap) * 8 : a.k_cache + base + lane * 8;
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem +
+                          ((brings_v ? kStages * stage_elems(D) : 0) + mine * block_elems(D)) * 2;
   int tbl = 0;
-  uint32_t bad_ring = 0;             // of the stages, four bits each, the one fetched last in the low ones
+  uint32_t bad_ring = 0;             // of the stages, four bits each, the one asked for last in the low ones
   auto fetch = [&](int st) {
+    bad_ring <<= 4;
+    if (st >= stages) return;
     if ((st & 15) == 0) {
       tbl = entry >= 0 && entry < a.num_blocks ? entry : -1;
       const int next = (st + 16) * kStageBlocks + lane;       // asked for sixteen stages ahead
       entry = next < blocks ? table[next] : 0;
     }
     const int i0 = (st & 15) * kStageBlocks;
-    bad_ring = bad_ring << 4 | (uint32_t)((__ballot(tbl < 0) >> i0) & 0xf);
+    bad_ring |= (uint32_t)((__ballot(tbl < 0) >> i0) & 0xf);
     const uint16_t* src = cache + (int64_t)max(__builtin_amdgcn_readlane(tbl, i0 + mine), 0) * blk_stride;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) fr[i] = load16(src + i * 512);
+    load_to_lds<D>(src, uniform((int)(lds_at + (st & (kStages - 1)) * stage_elems(D) * 2)));
   };
-  // a lane's group of V: dimension lane / 2 (+ 32 per load), half lane % 2
-  uint16_t* put_at = brings_v ? lds + kStageBlocks * k_elems(D) + mine * v_elems(D) + (lane & 1) * v_half(D) + (lane >> 1) * 8
-                              : lds + mine * k_elems(D) + lane * 8;
-  const int put_step = brings_v ? 256 : 512;
-  auto put = [&](int st) {
+  // Stages that not every column attends in full, or without memory: values that nobody
+  // attends and, told in sm_odd, those that are not finite become 0.
+  auto unclean = [&](int st, int bad) {
     const int pos = base_pos + st * kStageBlocks * kBlock;
+    return bad != 0 || pos < all.all_lo || pos + kStageBlocks * kBlock > all.all_hi;
+  };
+  auto clean = [&](int st, int bad) {
     if (brings_v) {
-      int told = 0;
-      if ((bad_ring >> mine) & 1) {        // no memory: the block's attended weights are NaN, the others 0
+      uint16_t* v = lds_v + (st & (kStages - 1)) * stage_elems(D) + mine * block_elems(D) + lane * 8;
+      const int room = (bad >> mine) & 1 ? 0 : it.n - base_pos - (st * kStageBlocks + mine) * kBlock - 8 * ((lane & 1) ^ v_swap);
+      bool odd = false;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) fr[i] = bf16x8{};
-      } else if (pos < all.all_lo || pos + kStageBlocks * kBlock > all.all_hi) {
-        const int room = it.n - pos - mine * kBlock - 8 * (lane & 1);
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) fr[i] = finite_values(first_values(room, fr[i]), odd);
-        told = __any(odd) ? 1 : 0;
+      for (int i = 0; i < block_elems(D) / 512; ++i) {
+        const bf16x8 x = finite_values(first_values(room, load16(v + i * 512)), odd);
+        *reinterpret_cast<bf16x8*>(v + i * 512) = x;
       }
+      const int told = __any(odd) ? 1 : 0;
       if (lane == 0) sm_odd[(st & (kStages - 1)) * kStageBlocks + mine] = told;
     }
-    uint16_t* dst = put_at + (st & (kStages - 1)) * stage_elems(D);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<bf16x8*>(dst + i * put_step) = fr[i];
+    __syncthreads();
   };
   const int pos16 = (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1);
-  const uint16_t* k_get = lds + (m >> 4) * k_elems(D) + (h * kBlock + pos16) * 8;
-  const uint16_t* v_get = lds + kStageBlocks * k_elems(D) + h * v_half(D) + m * 8;
-  auto stage_of = [&](int i) { return ((i >> 1) & (kStages - 1)) * stage_elems(D); };
+  const uint16_t* k_get = lds + (m >> 4) * block_elems(D) + (h * kBlock + pos16) * 8;
+  const uint16_t* v_get = lds_v + (2 * m + (h ^ ((m >> 3) & 1))) * 8;
+  auto stage_of = [&](int i) { return ((i >> 1) & (kStages - 1)) * stage_elems(D) + (i & 1) * 2 * block_elems(D); };
 
   f32x16 s;              // scores of the pair whose weights come next
   Parts<P> part;         // weights of the pair before
-  auto keys_of = [&](int i) { return k_get + stage_of(i) + (i & 1) * 2 * k_elems(D); };
-  auto values_of = [&](int i) { return v_get + stage_of(i) + (i & 1) * 2 * v_elems(D); };
+  auto keys_of = [&](int i) { return k_get + stage_of(i); };
+  auto values_of = [&](int i) { return v_get + stage_of(i); };
   auto scores = [&](int i) {
     const uint16_t* ks = keys_of(i);
     return score_pair<D>(qf, [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); });
   };
   auto products = [&](int i) {
     const uint16_t* vs = values_of(i);
-    weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * v_elems(D) + n * 32 * 8); });
+    weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * block_elems(D) + n * 32 * kBlock); });
   };
   // pair i's weights beside the next pair's scores and the products of the one before,
   // whichever of them there are; bad: pair i's blocks
@@ -922,11 +953,24 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     s = s_next;
   };
   // the same where all three are there and nothing is masked
+  bf16x8 kf[D / 16];
+  auto load_keys = [&](int i) {
+    const uint16_t* ks = keys_of(i);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) kf[kk] = load16(ks + kk * 2 * kBlock * 8);
+  };
   auto full_step = [&](int i, f32x16& s_now, f32x16& s_next) {
+    const uint16_t* vs = values_of(i - 1);
+    bf16x8 vf[D / 32][2];
     f32x16 p;
-    s_next = scores(i + WP);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
+    s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
+    load_keys(i + 2);
     const float sum = weights_of(a.scale_log2, s_now, w.ref, p);
-    products(i - WP);
+    weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
     interleave<D, P>();
     settle<D>(a.scale_log2, s_now, w, p, sum);
     part = parts_of<P>(p);
@@ -936,47 +980,40 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
   const int full_hi = min(last - WP, (min(min(all.all_hi, own.all_hi), end) - base_pos) / kPair);
 
   if (stages > 0) {
-    fetch(0);
-    put(0);
-    if (stages > 1) {
-      fetch(1);
-      put(1);
-    } else {
-      bad_ring <<= 4;
-    }
-    if (stages > 2) fetch(2);
-    else bad_ring <<= 4;
+    for (int st = 0; st < lead; ++st) fetch(st);
+    wait_loads<D>(false);
     __syncthreads();
     step(wp - WP, 0);
-    // (the stage written in a round was last read in the one before its barrier)
-    auto advance = [&](int st) {
-      if (st + 2 < stages) put(st + 2);
-      if (st + 3 < stages) fetch(st + 3);
-      else bad_ring <<= 4;
+    // the blocks of stages st (asked for, or none) after the round's own request
+    auto bad_of = [&](int ahead) { return (int)(bad_ring >> (4 * ahead)) & 0xf; };
+    auto is_full = [&](int st) {       // before the round's request
+      return WP == 1 && bad_of(lead - 1) == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi;
     };
-    auto bad_now = [&] { return (int)(bad_ring >> 12) & 0xf; };
-    auto is_full = [&](int st) {       // before advance
-      return WP == 1 && ((bad_ring >> 8) & 0xf) == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi;
+    auto end_round = [&](int st) {     // what the round asked for may still be on its way
+      wait_loads<D>(st + lead < stages);
+      __syncthreads();
     };
     // (loops of their own, so that a path's registers need not be the other's)
     for (int st = 0; st < stages;) {
+      if (is_full(st)) load_keys(2 * st + 1);
       for (; st < stages && is_full(st); ++st) {
-        advance(st);
+        fetch(st + lead);
         f32x16 t;
         full_step(2 * st, s, t);
         full_step(2 * st + 1, t, s);
-        __syncthreads();
+        end_round(st);
       }
       for (; st < stages && !is_full(st); ++st) {
-        advance(st);
-        const int bad = bad_now();
+        fetch(st + lead);
+        const int bad = bad_of(lead);
+        if (unclean(st, bad)) clean(st, bad);
         if (WP == 1) {
 #pragma unroll 1
           for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3);
         } else {
           step(2 * st + wp, (bad >> (2 * wp)) & 3);
         }
-        __syncthreads();
+        end_round(st);
       }
     }
     step(2 * stages + wp, 0);
