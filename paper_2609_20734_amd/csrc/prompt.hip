@@ -47,7 +47,7 @@ constexpr int kTile = kWaves * kCols; // columns of an item
 constexpr int kStageBlocks = 4;       // blocks staged together: one of K or V per wavefront
 constexpr int kMaxBatch = 2048;
 constexpr int kCus = 256;
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 256;
 constexpr uint32_t kMagic = 0x0da9f3u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -93,13 +93,14 @@ struct PlanArgs {
   int32_t extra_items, max_items, max_merges;
 };
 
-// Cost of an item in blocks of 16 positions at the time in which one CU's share of
-// HBM delivers them: up to that many columns a block's products and softmax take no
-// longer.
-constexpr float kColsFree = 96.f;
-constexpr float kItemCost = 24.f;     // start-up, the join, the partial's share of the merge
-constexpr float kLeastCost = 16.f;    // shortest range
-constexpr int kClasses = 256;         // cost classes, eight to a factor of two
+// Costs in the time in which one CU's share of HBM delivers a block of 16 positions: a
+// block's products and softmax take no longer up to half a tile's columns.
+constexpr float kWideCost = 1.3f;      // a block's for more columns
+constexpr float kItemCost = 24.f;      // start and end of an item
+constexpr float kPartCost = 8.f;       // an item's partial, written and merged
+constexpr float kWidePartCost = 36.f;  // of more than half a tile's columns
+constexpr float kLeastCost = 16.f;     // shortest range
+constexpr int kClasses = 256;          // cost classes, eight to a factor of two
 
 struct PlanRequest {
   int32_t row0, rows, n, tile;        // tile: the request's first
@@ -148,13 +149,13 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
   __shared__ PlanRequest s_req[kMaxBatch];
   __shared__ int2 s_wave[kPlanThreads / 64];
   __shared__ int s_max[kPlanThreads / 64];
-  __shared__ int s_class[kClasses], s_place[kClasses];
+  __shared__ int s_class[2 * kClasses], s_place[kClasses];      // [wide][class]; places by the class alone
   __shared__ int s_count[kPlanThreads / 64][64];
-  __shared__ float s_cost[kPlanThreads / 64][64];
+  __shared__ float s_cost[kPlanThreads / 64][64], s_big[kPlanThreads / 64][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   Item* items = reinterpret_cast<Item*>(a.plan + items_at());
   Merge* merges = reinterpret_cast<Merge*>(a.plan + merges_at(a.max_items));
-  if (tid < kClasses) s_class[tid] = s_place[tid] = 0;
+  for (int i = tid; i < 2 * kClasses; i += kPlanThreads) s_class[i] = 0;
 
   // requests: row starts kept in [0, R] and ascending whatever the array holds
   int n_tiles = 0, carry = 0;
@@ -213,62 +214,76 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     r.lo = a.causal && a.window > 0 ? max(0, first - a.window + 1) / kBlock : 0;
     return r;
   };
-  auto cost_of = [&](const Tile& t) { return (float)(t.hi - t.lo) * fmaxf(1.f, (float)((t.ncols + kCols - 1) / kCols * kCols) / kColsFree); };
+  auto is_wide = [&](const Tile& t) { return t.ncols > kTile / 2; };
+  auto cost_of = [&](const Tile& t) { return (float)(t.hi - t.lo) * (is_wide(t) ? kWideCost : 1.f); };
 
   int most = 0;
   for (int t = tid; t < n_tiles; t += kPlanThreads) {
-    const int c = class_of(cost_of(tile_at(t)));
-    atomicAdd(&s_class[c], 1);
+    const Tile r = tile_at(t);
+    const int c = class_of(cost_of(r));
+    atomicAdd(&s_class[(is_wide(r) ? kClasses : 0) + c], 1);
     most = max(most, c);
   }
 #pragma unroll
   for (int s = 32; s >= 1; s >>= 1) most = max(most, __shfl_xor(most, s));
-  __syncthreads();
   if (lane == 0) s_max[wave] = most;
   __syncthreads();
+#pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) most = max(most, s_max[w]);
 
   // what an item may cost: every lane tries one value; the last splits nothing
   const float top = fmaxf(class_cost(most), kLeastCost);
   const float cap = lane == 63 ? top : kLeastCost * __builtin_amdgcn_exp2f(__log2f(top / kLeastCost) * (float)lane * (1.f / 63.f));
+  const float inv = 1.f / cap;
   int n = 0;
-  float sum = 0.f;
-  for (int c = wave; c < kClasses; c += kPlanThreads / 64) {
-    const int count = s_class[c];
-    if (count == 0) continue;
-    const float cost = class_cost(c);
-    const int splits = lane == 63 ? 1 : max(1, (int)ceilf(cost / cap));
-    n += count * splits;
-    sum += (float)count * (cost + kItemCost * (float)splits);
+  float sum = 0.f, big = 0.f;
+  for (int c0 = 64 * wave; c0 < 2 * kClasses; c0 += kPlanThreads) {
+    const int here = s_class[c0 + lane];
+    const float part = c0 >= kClasses ? kWidePartCost : kPartCost;
+    for (uint64_t todo = __ballot(here != 0); todo != 0; todo &= todo - 1) {
+      const int i = __builtin_ctzll(todo);
+      const int count = __builtin_amdgcn_readlane(here, i);
+      const float cost = class_cost((c0 + i) & (kClasses - 1));
+      const int splits = lane == 63 ? 1 : max(1, (int)ceilf(cost * inv));
+      n += count * splits;
+      big = fmaxf(big, cost * __builtin_amdgcn_rcpf((float)splits));
+      sum += (float)count * (cost + (float)splits * (kItemCost + (splits > 1 ? part : 0.f)));
+    }
   }
   s_count[wave][lane] = n;
   s_cost[wave][lane] = sum;
+  s_big[wave][lane] = big;
   __syncthreads();
   n = 0;
   sum = 0.f;
+#pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
     n += s_count[w][lane];
     sum += s_cost[w][lane];
+    big = fmaxf(big, s_big[w][lane]);
   }
-  float est = (float)a.Hkv * n <= (float)kCus ? cap + kItemCost : (float)a.Hkv * sum * (1.f / (float)kCus) + 0.5f * cap;
+  // rounds of items of mean cost, the last one's idle places by half; at least the largest item
+  const float rounds = (float)a.Hkv * (float)n * (1.f / (float)kCus);
+  const float mean = sum / (float)max(n, 1);
+  float est = fmaxf(big + kItemCost, mean * 0.5f * (rounds + ceilf(rounds)));
   if (n - n_tiles > a.extra_items) est = INFINITY;
   float best = est;
 #pragma unroll
   for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
   const uint64_t who = __ballot(est == best);
   const int pick = who ? 63 - __builtin_clzll(who) : 63;
-  const float cap_best = __shfl(cap, pick);
+  const float inv_best = __shfl(inv, pick);
   auto splits_of = [&](const Tile& t) {
     const int blocks = t.hi - t.lo;
     if (pick == 63 || blocks <= 0) return 1;
-    const int splits = min(blocks, max(1, (int)ceilf(cost_of(t) / cap_best)));
+    const int splits = min(blocks, max(1, (int)ceilf(cost_of(t) * inv_best)));
     const int len = range_blocks(blocks, splits);
     return (blocks + len - 1) / len;
   };
 
   // items listed by their cost, the largest class first (within one in any order)
   __syncthreads();
-  if (tid < kClasses) s_class[tid] = 0;
+  for (int i = tid; i < kClasses; i += kPlanThreads) s_class[i] = 0;
   __syncthreads();
   for (int t = tid; t < n_tiles; t += kPlanThreads) {
     const Tile r = tile_at(t);
@@ -920,8 +935,9 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * block_elems(D) + n * 32 * kBlock); });
   };
   // pair i's weights beside the next pair's scores and the products of the one before,
-  // whichever of them there are; bad: pair i's blocks
-  auto step = [&](int i, int bad) {
+  // whichever of them there are; bad: pair i's blocks; odd: whether values of the stage
+  // of the one before were taken out
+  auto step = [&](int i, int bad, int odd) {
     const int j = i + WP, k0 = i - WP;
     const bool next = j >= first && j < last, now = i >= first && i < last, before = k0 >= first && k0 < last;
     const int pos = base_pos + i * kPair, pos0 = base_pos + k0 * kPair;
@@ -933,17 +949,14 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     if (now) sum = weights_of(a.scale_log2, s, w.ref, p);
     if (before) {
       products(k0);
-      if (pos0 < all.all_lo || pos0 + kPair > all.all_hi) {    // its values may have been taken out
+      if (odd != 0) {
         const int blk = 2 * k0;
-        const int* odd = sm_odd + ((blk >> 2) & (kStages - 1)) * kStageBlocks + (blk & 2);
-        if (uniform(odd[0] | odd[1]) != 0) {
-          int64_t at[2];
-          for (int b = 0; b < 2; ++b) {
-            const int e = blk + b < blocks ? table[blk + b] : 0;
-            at[b] = (int64_t)(e >= 0 && e < a.num_blocks ? e : 0) * blk_stride + base;
-          }
-          add_odd_values<D>(a.v_cache + at[0], a.v_cache + at[1], pos0, end, w);
+        int64_t at[2];
+        for (int b = 0; b < 2; ++b) {
+          const int e = blk + b < blocks ? table[blk + b] : -1;
+          at[b] = (int64_t)max(e >= 0 && e < a.num_blocks ? e : 0, 0) * blk_stride + base;
         }
+        add_odd_values<D>(a.v_cache + at[0], a.v_cache + at[1], pos0, end, w);
       }
     }
     if (now) {
@@ -975,48 +988,59 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     settle<D>(a.scale_log2, s_now, w, p, sum);
     part = parts_of<P>(p);
   };
-  // pairs whose steps are full: of no bad block, after the first and before the last
-  const int full_lo = max(first + WP, (max(all.all_lo, own.all_lo) - base_pos + kPair - 1) / kPair + WP);
-  const int full_hi = min(last - WP, (min(min(all.all_hi, own.all_hi), end) - base_pos) / kPair);
+  // pairs whose steps are full: not masked, after the first and before the last
+  const int full_lo = max(first + 1, (own.all_lo - base_pos + kPair - 1) / kPair);
+  const int full_hi = min(last - 1, (min(own.all_hi, end) - base_pos) / kPair);
 
   if (stages > 0) {
     for (int st = 0; st < lead; ++st) fetch(st);
     wait_loads<D>(false);
     __syncthreads();
-    step(wp - WP, 0);
-    // the blocks of stages st (asked for, or none) after the round's own request
+    if (first <= wp && wp < last) s = scores(wp);
     auto bad_of = [&](int ahead) { return (int)(bad_ring >> (4 * ahead)) & 0xf; };
-    auto is_full = [&](int st) {       // before the round's request
-      return WP == 1 && bad_of(lead - 1) == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi;
+    // A round asks for later blocks, then sees to its own; whether its steps are full.
+    int odd = 0;                       // of the stage and the one before
+    auto begin_round = [&](int st) {
+      fetch(st + lead);
+      const int bad = bad_of(lead);
+      odd = odd << 1 & 2;
+      if (st < stages && unclean(st, bad)) {
+        clean(st, bad);
+        const int* f = sm_odd + (st & (kStages - 1)) * kStageBlocks;
+        odd |= uniform(f[0] | f[1] | f[2] | f[3]);
+      }
+      return uniform(WP == 1 && bad == 0 && odd == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi ? 1 : 0) != 0;
     };
     auto end_round = [&](int st) {     // what the round asked for may still be on its way
       wait_loads<D>(st + lead < stages);
       __syncthreads();
     };
-    // (loops of their own, so that a path's registers need not be the other's)
-    for (int st = 0; st < stages;) {
-      if (is_full(st)) load_keys(2 * st + 1);
-      for (; st < stages && is_full(st); ++st) {
-        fetch(st + lead);
+    // (loops of their own, so that a path's registers need not be the other's; the round
+    // after the last stage has the last pair's products alone)
+    int st = 0;
+    bool full = begin_round(0);
+    while (st <= stages) {
+      if (full) load_keys(2 * st + 1);
+      while (full) {
         f32x16 t;
         full_step(2 * st, s, t);
         full_step(2 * st + 1, t, s);
         end_round(st);
+        full = begin_round(++st);
       }
-      for (; st < stages && !is_full(st); ++st) {
-        fetch(st + lead);
+      while (!full && st <= stages) {
         const int bad = bad_of(lead);
-        if (unclean(st, bad)) clean(st, bad);
+        const int flags = odd;
         if (WP == 1) {
 #pragma unroll 1
-          for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3);
+          for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3, e == 0 ? flags >> 1 : flags & 1);
         } else {
-          step(2 * st + wp, (bad >> (2 * wp)) & 3);
+          step(2 * st + wp, (bad >> (2 * wp)) & 3, flags >> 1);
         }
         end_round(st);
+        full = begin_round(++st);
       }
     }
-    step(2 * stages + wp, 0);
   }
   w.sum += __shfl_xor(w.sum, 32);
   if (WP > 1) {
@@ -1060,45 +1084,69 @@ void prompt_attn_kernel(PromptArgs a) {
   else run_wide<D, kWaves, Out>(a, h, it, g, smem);
 }
 
-// One workgroup per (split tile, KV head, kCols columns): the ranges in order.
+// One workgroup per (split tile, KV head, kCols columns): the ranges in order, two at a
+// time, kCols / 8 columns side by side in a thread so that its loads are in flight
+// together.
 template <int D, typename Out>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
+  constexpr int kSide = kCols * (D / 4) / 256;       // columns of a thread
   const PlanHeader h = *reinterpret_cast<const PlanHeader*>(a.plan);
   const int parts = kTile / kCols;
   const int part = blockIdx.x % parts, u = blockIdx.x / parts;
   const int i = u / a.Hkv, g = u - i * a.Hkv;
   const Merge mg = reinterpret_cast<const Merge*>(a.plan + merges_at(a.max_items))[i];
-  if (!plan_fits(a, h) || i >= min(h.n_merges, a.max_merges)) return;
-  for (int e = threadIdx.x; e < kCols * (D / 4); e += 256) {
-    const int d = e % (D / 4) * 4, col = part * kCols + e / (D / 4);
-    if (col >= mg.ncols) return;
-    const int64_t at = (int64_t)g * a.part_cols + mg.part + col;
-    float top = -INFINITY;
-#pragma unroll 8
-    for (int s = 0; s < mg.splits; ++s) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (at + (int64_t)s * mg.ncols) * 2);
-      if (ml.y != 0.f) top = fmaxf(top, ml.x);
+  if (!plan_fits(a, h) || i >= min(h.n_merges, a.max_merges) || part * kCols >= mg.ncols) return;
+  const int d = threadIdx.x % (D / 4) * 4, c0 = part * kCols + threadIdx.x / (D / 4);
+  const int64_t at = (int64_t)g * a.part_cols + mg.part;
+  int col[kSide];
+  float top[kSide], l[kSide] = {};
+  float4 acc[kSide];
+#pragma unroll
+  for (int k = 0; k < kSide; ++k) {
+    col[k] = min(c0 + k * (1024 / D), mg.ncols - 1);      // (past the last column it again, not written)
+    top[k] = -INFINITY;
+    acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  auto range = [&](int s, float2 (&ml)[kSide], float4 (&x)[kSide]) {
+#pragma unroll
+    for (int k = 0; k < kSide; ++k) {
+      const int64_t from = at + (int64_t)s * mg.ncols + col[k];
+      ml[k] = *reinterpret_cast<const float2*>(a.part_ml + from * 2);
+      x[k] = *reinterpret_cast<const float4*>(a.part_o + from * D + d);
     }
-    const float ref = top == -INFINITY ? 0.f : top;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < mg.splits; ++s) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (at + (int64_t)s * mg.ncols) * 2);
-      const float4 x = *reinterpret_cast<const float4*>(a.part_o + (at + (int64_t)s * mg.ncols) * D + d);
-      // (a range of which the column attends nothing has a sum of 0 and any reference)
-      const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
-      acc.x += f * x.x;
-      acc.y += f * x.y;
-      acc.z += f * x.z;
-      acc.w += f * x.w;
-      l += f * ml.y;
+  };
+  // (a range of which a column attends nothing has a sum of 0 and any reference)
+  auto add = [&](const float2 (&ml)[kSide], const float4 (&x)[kSide]) {
+#pragma unroll
+    for (int k = 0; k < kSide; ++k) {
+      const float to = ml[k].y == 0.f ? top[k] : fmaxf(top[k], ml[k].x);
+      const float ref = to == -INFINITY ? 0.f : to;
+      const float f0 = __builtin_amdgcn_exp2f(top[k] - ref), f1 = ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - ref);
+      top[k] = to;
+      acc[k].x = f0 * acc[k].x + f1 * x[k].x;
+      acc[k].y = f0 * acc[k].y + f1 * x[k].y;
+      acc[k].z = f0 * acc[k].z + f1 * x[k].z;
+      acc[k].w = f0 * acc[k].w + f1 * x[k].w;
+      l[k] = f0 * l[k] + f1 * ml[k].y;
     }
-    const int fc = mg.col0 + col, token = fc / a.G;
+  };
+  float2 ml0[kSide], ml1[kSide];
+  float4 x0[kSide], x1[kSide];
+  range(0, ml0, x0);
+  for (int s = 0; s < mg.splits; s += 2) {
+    if (s + 1 < mg.splits) range(s + 1, ml1, x1);
+    add(ml0, x0);
+    if (s + 2 < mg.splits) range(s + 2, ml0, x0);
+    if (s + 1 < mg.splits) add(ml1, x1);
+  }
+#pragma unroll
+  for (int k = 0; k < kSide; ++k) {
+    if (c0 + k * (1024 / D) >= mg.ncols) continue;
+    const int fc = mg.col0 + col[k], token = fc / a.G;
     const int64_t row = (int64_t)(mg.row0 + token) * a.Hq + g * a.G + (fc - token * a.G);
-    const float inv = inverse_of(l);
-    store4(static_cast<Out*>(a.out) + row * D + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-    if (d == 0 && a.lse) a.lse[row] = lse_of(ref, l);
+    const float inv = inverse_of(l[k]);
+    store4(static_cast<Out*>(a.out) + row * D + d, make_float4(acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv));
+    if (d == 0 && a.lse) a.lse[row] = lse_of(top[k] == -INFINITY ? 0.f : top[k], l[k]);
   }
 }
 
