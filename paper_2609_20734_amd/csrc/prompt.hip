@@ -922,58 +922,25 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
   const uint16_t* v_get = lds_v + (2 * m + (h ^ ((m >> 3) & 1))) * 8;
   auto stage_of = [&](int i) { return ((i >> 1) & (kStages - 1)) * stage_elems(D) + (i & 1) * 2 * block_elems(D); };
 
-  f32x16 s;              // scores of the pair whose weights come next
-  Parts<P> part;         // weights of the pair before
-  auto keys_of = [&](int i) { return k_get + stage_of(i); };
-  auto values_of = [&](int i) { return v_get + stage_of(i); };
-  auto scores = [&](int i) {
-    const uint16_t* ks = keys_of(i);
-    return score_pair<D>(qf, [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); });
-  };
-  auto products = [&](int i) {
-    const uint16_t* vs = values_of(i);
-    weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * block_elems(D) + n * 32 * kBlock); });
-  };
-  // pair i's weights beside the next pair's scores and the products of the one before,
-  // whichever of them there are; bad: pair i's blocks; odd: whether values of the stage
-  // of the one before were taken out
-  auto step = [&](int i, int bad, int odd) {
-    const int j = i + WP, k0 = i - WP;
-    const bool next = j >= first && j < last, now = i >= first && i < last, before = k0 >= first && k0 < last;
-    const int pos = base_pos + i * kPair, pos0 = base_pos + k0 * kPair;
-    f32x16 s_next = {}, p = {};
-    float sum = 0.f;
-    if (next) s_next = scores(j);
-    if (now && (bad != 0 || pos < own.all_lo || pos + kPair > min(own.all_hi, end)))
-      mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s);
-    if (now) sum = weights_of(a.scale_log2, s, w.ref, p);
-    if (before) {
-      products(k0);
-      if (odd != 0) {
-        const int blk = 2 * k0;
-        int64_t at[2];
-        for (int b = 0; b < 2; ++b) {
-          const int e = blk + b < blocks ? table[blk + b] : -1;
-          at[b] = (int64_t)max(e >= 0 && e < a.num_blocks ? e : 0, 0) * blk_stride + base;
-        }
-        add_odd_values<D>(a.v_cache + at[0], a.v_cache + at[1], pos0, end, w);
-      }
-    }
-    if (now) {
-      settle<D>(a.scale_log2, s, w, p, sum);
-      part = parts_of<P>(p);
-    }
-    s = s_next;
-  };
-  // the same where all three are there and nothing is masked
-  bf16x8 kf[D / 16];
+  Parts<P> part;         // weights of the wavefront's pair before
+  bf16x8 kf[D / 16];     // K of its next pair
   auto load_keys = [&](int i) {
-    const uint16_t* ks = keys_of(i);
+    const uint16_t* ks = k_get + stage_of(i);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) kf[kk] = load16(ks + kk * 2 * kBlock * 8);
   };
+  auto add_odd = [&](int i) {
+    const int blk = 2 * i;
+    int64_t at[2];
+    for (int b = 0; b < 2; ++b) {
+      const int e = blk + b < blocks ? table[blk + b] : -1;
+      at[b] = (int64_t)(e >= 0 && e < a.num_blocks ? e : 0) * blk_stride + base;
+    }
+    add_odd_values<D>(a.v_cache + at[0], a.v_cache + at[1], base_pos + i * kPair, end, w);
+  };
+  // Where nothing is masked and the pair is neither the wavefront's first nor its last:
   auto full_step = [&](int i, f32x16& s_now, f32x16& s_next) {
-    const uint16_t* vs = values_of(i - 1);
+    const uint16_t* vs = v_get + stage_of(i - 1);
     bf16x8 vf[D / 32][2];
     f32x16 p;
 #pragma unroll
@@ -988,26 +955,64 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     settle<D>(a.scale_log2, s_now, w, p, sum);
     part = parts_of<P>(p);
   };
-  // pairs whose steps are full: not masked, after the first and before the last
   const int full_lo = max(first + 1, (own.all_lo - base_pos + kPair - 1) / kPair);
   const int full_hi = min(last - 1, (min(own.all_hi, end) - base_pos) / kPair);
+  // Any pair i, its scores in s_now: its weights beside the next pair's scores (behind the
+  // last one of what lies in LDS, not used) and the products of the one before (of the
+  // first one's values with weights of 0).  bad: its blocks; odd: whether values were
+  // taken out of its stage (bit 0) and of that of the pair before (bit 1).
+  auto step = [&](int i, int bad, int odd, f32x16& s_now) {
+    if (i < first || i >= last) return;
+    const bool fills = i - WP < first, drains = i + WP >= last;
+    if (fills) {
+      const uint16_t* ks = k_get + stage_of(i);
+      s_now = score_pair<D>(qf, [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); });
+      if (WP == 1) load_keys(i + 1);
+#pragma unroll
+      for (int q = 0; q < P; ++q) part.x[q][0] = part.x[q][1] = bf16x8{};
+    }
+    const int pos = base_pos + i * kPair;
+    if (bad != 0 || pos < own.all_lo || pos + kPair > min(own.all_hi, end))
+      mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s_now);
+    const uint16_t* vs = v_get + stage_of(fills ? i : i - WP);
+    bf16x8 vf[D / 32][2];
+    f32x16 p;
+    if (WP > 1) load_keys(i + WP);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
+    const f32x16 s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
+    if (WP == 1) load_keys(i + 2);
+    const float sum = weights_of(a.scale_log2, s_now, w.ref, p);
+    weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
+    interleave<D, P>();
+    settle<D>(a.scale_log2, s_now, w, p, sum);
+    part = parts_of<P>(p);
+    s_now = s_next;
+    if ((odd & 2) != 0 && !fills) add_odd(i - WP);
+    if (drains) {
+      vs = v_get + stage_of(i);
+      weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * block_elems(D) + n * 32 * kBlock); });
+      if ((odd & 1) != 0) add_odd(i);
+    }
+  };
 
   if (stages > 0) {
     for (int st = 0; st < lead; ++st) fetch(st);
     wait_loads<D>(false);
     __syncthreads();
-    if (first <= wp && wp < last) s = scores(wp);
-    auto bad_of = [&](int ahead) { return (int)(bad_ring >> (4 * ahead)) & 0xf; };
+    f32x16 s = {};
     // A round asks for later blocks, then sees to its own; whether its steps are full.
-    int odd = 0;                       // of the stage and the one before
+    int bad = 0, odd = 0;              // odd: of the stage and the one before
     auto begin_round = [&](int st) {
       fetch(st + lead);
-      const int bad = bad_of(lead);
+      bad = (int)(bad_ring >> (4 * lead)) & 0xf;
       odd = odd << 1 & 2;
       if (st < stages && unclean(st, bad)) {
         clean(st, bad);
         const int* f = sm_odd + (st & (kStages - 1)) * kStageBlocks;
-        odd |= uniform(f[0] | f[1] | f[2] | f[3]);
+        odd |= uniform(f[0] | f[1] | f[2] | f[3]) != 0 ? 1 : 0;
       }
       return uniform(WP == 1 && bad == 0 && odd == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi ? 1 : 0) != 0;
     };
@@ -1015,12 +1020,10 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
       wait_loads<D>(st + lead < stages);
       __syncthreads();
     };
-    // (loops of their own, so that a path's registers need not be the other's; the round
-    // after the last stage has the last pair's products alone)
+    // (loops of their own, so that a path's registers need not be the other's)
     int st = 0;
     bool full = begin_round(0);
-    while (st <= stages) {
-      if (full) load_keys(2 * st + 1);
+    while (st < stages) {
       while (full) {
         f32x16 t;
         full_step(2 * st, s, t);
@@ -1028,15 +1031,10 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
         end_round(st);
         full = begin_round(++st);
       }
-      while (!full && st <= stages) {
-        const int bad = bad_of(lead);
-        const int flags = odd;
-        if (WP == 1) {
+      while (!full && st < stages) {
 #pragma unroll 1
-          for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3, e == 0 ? flags >> 1 : flags & 1);
-        } else {
-          step(2 * st + wp, (bad >> (2 * wp)) & 3, flags >> 1);
-        }
+        for (int e = WP == 1 ? 0 : wp; e < (WP == 1 ? 2 : wp + 1); ++e)
+          step(2 * st + e, (bad >> (2 * e)) & 3, WP == 1 && e == 1 ? odd << 1 | (odd & 1) : odd, s);
         end_round(st);
         full = begin_round(++st);
       }
