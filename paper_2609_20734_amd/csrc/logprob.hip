@@ -66,6 +66,31 @@ __device__ __forceinline__ uint64_t published(const uint64_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Reductions over the wavefront in six DPP steps (row shifts by 1, 2, 4, 8, then each
+// row's last lane into the next row, then the lower half's into the upper).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float shifted(float none, float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(x), kCtrl, kRows, 0xf, false));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, shifted<0x111, 0xf>(-INFINITY, x));
+  x = fmaxf(x, shifted<0x112, 0xf>(-INFINITY, x));
+  x = fmaxf(x, shifted<0x114, 0xf>(-INFINITY, x));
+  x = fmaxf(x, shifted<0x118, 0xf>(-INFINITY, x));
+  x = fmaxf(x, shifted<0x142, 0xa>(-INFINITY, x));
+  x = fmaxf(x, shifted<0x143, 0xc>(-INFINITY, x));
+  return lane_value(x, 63);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += shifted<0x111, 0xf>(0.f, x);
+  x += shifted<0x112, 0xf>(0.f, x);
+  x += shifted<0x114, 0xf>(0.f, x);
+  x += shifted<0x118, 0xf>(0.f, x);
+  x += shifted<0x142, 0xa>(0.f, x);
+  x += shifted<0x143, 0xc>(0.f, x);
+  return lane_value(x, 63);
+}
+
 // A running largest logit with the sums of weights against it.
 struct Stat {
   float m, s, t;
@@ -81,22 +106,10 @@ __device__ __forceinline__ Stat against(Stat x, float top) {
   const float d = x.m == top ? 0.f : fminf(top - x.m, kFar);
   return Stat{top, f * x.s, f * (x.t + d * x.s)};
 }
-__device__ __forceinline__ Stat joined(Stat a, Stat b) {
-  const float top = fmaxf(a.m, b.m);
-  a = against(a, top);
-  b = against(b, top);
-  return Stat{top, a.s + b.s, a.t + b.t};
-}
 __device__ __forceinline__ Stat wave_join(Stat x) {
-  float top = x.m;
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-  x = against(x, top);
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) {
-    x.s += __shfl_xor(x.s, s);
-    x.t += __shfl_xor(x.t, s);
-  }
+  x = against(x, wave_max(x.m));
+  x.s = wave_sum(x.s);
+  x.t = wave_sum(x.t);
   return x;
 }
 
@@ -109,16 +122,25 @@ struct Best {
 __device__ __forceinline__ void insert(Best& best, float z, int id) {
   const int lane = threadIdx.x & 63;
   const int at = __builtin_popcountll(__ballot(best.z >= z));
-  const float zs = __shfl_up(best.z, 1);
-  const int is = __shfl_up(best.id, 1);
-  if (lane > at) {
-    best.z = zs;
-    best.id = is;
+  const float zs = shifted<0x138, 0xf>(-INFINITY, best.z);            // from the lane before
+  const int is = __builtin_amdgcn_update_dpp(-1, best.id, 0x138, 0xf, 0xf, false);
+  best.z = lane > at ? zs : lane == at ? z : best.z;
+  best.id = lane > at ? is : lane == at ? id : best.id;
+}
+// A number that at least k lanes' values reach (-infinity where fewer are above it), near
+// the k-th of them: the upper half of its bits, in the order of floats, found bit by bit.
+__device__ __forceinline__ float kth_bound(float x, int k) {
+  const uint32_t u = __float_as_uint(x);
+  const uint32_t key = (u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) >> 16;
+  uint32_t found = 0;
+#pragma unroll
+  for (int b = 15; b >= 0; --b) {
+    const uint32_t t = found | 1u << b;
+    if (__builtin_popcountll(__ballot(key >= t)) >= k) found = t;
   }
-  if (lane == at) {
-    best.z = z;
-    best.id = id;
-  }
+  found <<= 16;
+  const float y = __uint_as_float(found & 0x80000000u ? found ^ 0x80000000u : ~found);
+  return y > -INFINITY ? y : -INFINITY;                                // (below it the bits of NaN)
 }
 
 __device__ __forceinline__ float log_prob(float z, float m, double log_s) {
@@ -187,52 +209,65 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   float least = -INFINITY;          // the last place's logit
   int ahead = 0;
   if (from < to) load(from, next);
+  const float zt_below = known && zt > -INFINITY && zt < INFINITY
+                             ? (zt > 0.f ? __uint_as_float(__float_as_uint(zt) - 1)
+                                         : __uint_as_float(__float_as_uint(fminf(zt, -0.f)) + 1))
+                             : zt;              // the float before it: above that is at or above zt
+  const bool plain_rank = zt > -INFINITY && zt < INFINITY && zt != 0.f;
   for (int v0 = from; v0 < to; v0 += kBatch) {
 #pragma unroll
-    for (int i = 0; i < 4 * kLoads; ++i) z[i] = fmaxf(next[i], -INFINITY);
+    for (int i = 0; i < 4 * kLoads; ++i) z[i] = next[i];
     if (v0 + kBatch < to) load(v0 + kBatch, next);
-    float top = z[0];
+    float top = fmaxf(z[0], -INFINITY);          // (NaN is passed over)
 #pragma unroll
     for (int i = 1; i < 4 * kLoads; ++i) top = fmaxf(top, z[i]);
     if (top > x.m) x = against(x, top);
     if (__any(x.m == INFINITY)) {
 #pragma unroll
       for (int i = 0; i < 4 * kLoads; ++i) {
-        const float w = z[i] == -INFINITY ? 0.f : factor(z[i], x.m);
+        const float y = fmaxf(z[i], -INFINITY), w = y == -INFINITY ? 0.f : factor(y, x.m);
         x.s += w;
-        x.t += w == 0.f ? 0.f : w * (z[i] == x.m ? 0.f : x.m - z[i]);
+        x.t += w == 0.f ? 0.f : w * (y == x.m ? 0.f : x.m - y);
       }
     } else if (x.m != -INFINITY) {
 #pragma unroll
       for (int i = 0; i < 4 * kLoads; ++i) {
-        const float d = x.m - z[i], w = __builtin_amdgcn_exp2f(-d * kLog2e);
+        const float d = fminf(x.m - z[i], kFar), w = __builtin_amdgcn_exp2f(d * -kLog2e);      // (NaN: kFar)
         x.s += w;
-        x.t += w * fminf(d, kFar);
+        x.t += w * d;
       }
     }
     if (a.rank) {
+      if (plain_rank && v0 + kBatch <= to && (token < v0 || token >= v0 + kBatch)) {
+        const float limit = token < v0 ? zt : zt_below;
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u)
+        for (int i = 0; i < 4 * kLoads; ++i) ahead += __builtin_popcountll(__ballot(z[i] > limit));
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int v = v0 + (u * 64 + lane) * 4 + e;
-          const float y = z[4 * u + e];
-          // (past the run's end -infinity stands, which is ahead of nothing there)
-          ahead += y > zt || (y == zt && v < token && v < to) ? 1 : 0;
-        }
+        for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = v0 + (u * 64 + lane) * 4 + e;
+            const float y = fmaxf(z[4 * u + e], -INFINITY);
+            // (past the run's end -infinity stands, which is ahead of nothing there)
+            ahead += __builtin_popcountll(__ballot(y > zt || (y == zt && v < token && v < to)));
+          }
+      }
     }
     if (a.top > 0 && __any(top > least)) {
+      // (the first batch: what k lanes' largest reach, the k-th place does)
+      const float bound = v0 == from ? kth_bound(top, a.top) : -INFINITY;
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        float most = fmaxf(fmaxf(z[4 * u], z[4 * u + 1]), fmaxf(z[4 * u + 2], z[4 * u + 3]));
-        uint64_t todo = __ballot(most > least);
+        const float most = fmaxf(fmaxf(fmaxf(z[4 * u], z[4 * u + 1]), fmaxf(z[4 * u + 2], z[4 * u + 3])), -INFINITY);
+        uint64_t todo = __ballot(most > least && most >= bound);
         while (todo != 0) {
           const int l = __builtin_ctzll(todo);
           todo &= todo - 1;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float y = lane_value(z[4 * u + e], l);
-            if (y > least) {
+            if (y > least && y >= bound) {
               insert(best, y, v0 + (u * 64 + l) * 4 + e);
               least = lane_value(best.z, a.top - 1);
             }
@@ -244,8 +279,6 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
 
   // the workgroup's wavefronts
   x = wave_join(x);
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
   if (lane == 0) {
     sm.m[wave] = x.m;
     sm.s[wave] = x.s;
@@ -263,24 +296,24 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   // ones' where logits are equal: k rounds over the lists' heads.
   auto merge = [&](int lists) {
     Best b{-INFINITY, -1};
-    int at = 0;
-    float head = lane < lists && a.top > 0 ? sm.z[lane * a.top] : -INFINITY;
-    int id = lane < lists && a.top > 0 ? sm.id[lane * a.top] : -1;
+    const bool in = lane < lists && a.top > 0;
+    int at = 1;                       // place in the list of the entry behind the head
+    float head = in ? sm.z[lane * a.top] : -INFINITY, next_z = in && a.top > 1 ? sm.z[lane * a.top + 1] : -INFINITY;
+    int id = in ? sm.id[lane * a.top] : -1, next_id = in && a.top > 1 ? sm.id[lane * a.top + 1] : -1;
     for (int i = 0; i < a.top; ++i) {
-      float most = head;
-#pragma unroll
-      for (int s = 32; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-      const uint64_t who = __ballot(head == most);
-      const int l = __builtin_ctzll(who);
+      const float most = wave_max(head);
+      const int l = __builtin_ctzll(__ballot(head == most));
       const int taken = __builtin_amdgcn_readlane(id, l);
       if (lane == i) {
         b.z = most;
         b.id = taken;
       }
       if (lane == l) {
+        head = next_z;
+        id = next_id;
         ++at;
-        head = at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
-        id = at < a.top ? sm.id[lane * a.top + at] : -1;
+        next_z = in && at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
+        next_id = in && at < a.top ? sm.id[lane * a.top + at] : -1;
       }
     }
     return b;
@@ -318,11 +351,22 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     x = Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)};
     ahead = (int)(uint32_t)p1;
   }
-  for (int e = lane; e < a.splits * a.top; e += 64) {
-    const int s = e / a.top, i = e - s * a.top;
-    const uint64_t p = published(parts + (int64_t)s * words + 2 + i);
-    sm.z[e] = first_of(p);
-    sm.id[e] = (int)(uint32_t)p;
+  // (a trip to memory for up to 1,024 places)
+  constexpr int kTrip = 16;
+  for (int e0 = lane; e0 < a.splits * a.top; e0 += 64 * kTrip) {
+    uint64_t p[kTrip];
+#pragma unroll
+    for (int j = 0; j < kTrip; ++j) {
+      const int e = min(e0 + 64 * j, a.splits * a.top - 1);
+      const int s = e / a.top;
+      p[j] = published(parts + (int64_t)s * words + 2 + (e - s * a.top));
+    }
+#pragma unroll
+    for (int j = 0; j < kTrip; ++j) {
+      const int e = min(e0 + 64 * j, a.splits * a.top - 1);
+      sm.z[e] = first_of(p[j]);
+      sm.id[e] = (int)(uint32_t)p[j];
+    }
   }
   x = wave_join(x);
 #pragma unroll
