@@ -17,6 +17,7 @@
 #include <climits>
 
 #include "oda.h"
+#include "oda_device.h"
 #include "oda_internal.h"
 
 namespace {
@@ -30,6 +31,7 @@ constexpr int kMaxSplits = 64;                // of a row: one per lane where th
 constexpr int kTickets = 1024;                // rows that may be split
 constexpr int kGroups = 1024;                 // workgroups that split rows make at most
 constexpr int kLeastSplit = kWaves * kBatch / 2;
+constexpr int kGrain = kWaves * 256;           // logits of a wavefront's load, of all of them
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = 1e30f;                 // stands for an infinite distance (its weight is 0)
 
@@ -113,20 +115,11 @@ __device__ __forceinline__ Stat wave_join(Stat x) {
   return x;
 }
 
-// A wavefront's first tokens: lane i < k holds place i (-infinity, -1: none yet).
+// The first tokens of the order: lane i holds place i (-infinity, -1: none).
 struct Best {
   float z;
   int id;
 };
-// A logit above the last place's, behind those that are equal to it.
-__device__ __forceinline__ void insert(Best& best, float z, int id) {
-  const int lane = threadIdx.x & 63;
-  const int at = __builtin_popcountll(__ballot(best.z >= z));
-  const float zs = shifted<0x138, 0xf>(-INFINITY, best.z);            // from the lane before
-  const int is = __builtin_amdgcn_update_dpp(-1, best.id, 0x138, 0xf, 0xf, false);
-  best.z = lane > at ? zs : lane == at ? z : best.z;
-  best.id = lane > at ? is : lane == at ? id : best.id;
-}
 // A number that at least k lanes' values reach (-infinity where fewer are above it), near
 // the k-th of them: the upper half of its bits, in the order of floats, found bit by bit.
 __device__ __forceinline__ float kth_bound(float x, int k) {
@@ -143,6 +136,39 @@ __device__ __forceinline__ float kth_bound(float x, int k) {
   return y > -INFINITY ? y : -INFINITY;                                // (below it the bits of NaN)
 }
 
+// A logit above the last place's, behind those that are equal to it.
+__device__ __forceinline__ void insert(Best& best, float z, int id) {
+  const int lane = threadIdx.x & 63;
+  const int at = __builtin_popcountll(__ballot(best.z >= z));
+  const float zs = shifted<0x138, 0xf>(-INFINITY, best.z);            // from the lane before
+  const int is = __builtin_amdgcn_update_dpp(-1, best.id, 0x138, 0xf, 0xf, false);
+  best.z = lane > at ? zs : lane == at ? z : best.z;
+  best.id = lane > at ? is : lane == at ? id : best.id;
+}
+// The places of n <= 64 candidates, one a lane (ids differ): by counting those ahead.
+__device__ __forceinline__ Best in_order(float z, int id, int n) {
+  const int lane = threadIdx.x & 63;
+  z = lane < n ? z : -INFINITY;
+  id = lane < n ? id : INT_MAX;
+  int ahead = 0;
+  for (int j0 = 0; j0 < n; j0 += 4) {                 // (past the last candidate none is ahead of one)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float zj = lane_value(z, j0 + j);
+      const int ij = __builtin_amdgcn_readlane(id, j0 + j);
+      ahead += (zj > z) | ((zj == z) & (ij < id)) ? 1 : 0;
+    }
+  }
+  const int to = 4 * (lane < n ? ahead : lane);
+  Best b;
+  b.z = __uint_as_float(__builtin_amdgcn_ds_permute(to, __float_as_uint(z)));
+  b.id = __builtin_amdgcn_ds_permute(to, lane < n ? id : -1);
+  return b;
+}
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
 __device__ __forceinline__ float log_prob(float z, float m, double log_s) {
   if (m == -INFINITY) return __builtin_nanf("");
   if (z == m) return (float)-log_s;
@@ -152,9 +178,11 @@ __device__ __forceinline__ float log_prob(float z, float m, double log_s) {
 struct Scratch {
   float m[kWaves], s[kWaves], t[kWaves];
   int ahead[kWaves];
-  float z[kMaxSplits * kMaxTop];
+  float deep[kWaves];                          // a place of each wavefront's, below
+  float z[kMaxSplits * kMaxTop];               // lists to merge
   int id[kMaxSplits * kMaxTop];
-  int last;
+  float pz[kWaves][64];                        // candidates
+  int pi[kWaves][64];
 };
 
 // Outputs of a row: lane i < k of the wavefront holds place i.
@@ -172,6 +200,8 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat x,
   if (a.rank) a.rank[row] = known ? ahead + 1 : 0;
 }
 
+// (Every workgroup runs most of the code once, so its size counts: one path for
+// every value, loops over registers kept few.)
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   __shared__ Scratch sm;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -181,9 +211,6 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   const int row = uniform(a.work_list ? a.work_list[slot] : slot);
   if (row < 0 || row >= a.R) return;
   const float* z_row = a.logits + (int64_t)row * a.stride;
-  const int token = a.tokens ? uniform(a.tokens[row]) : -1;
-  const bool known = token >= 0 && token < a.V;
-  float zt = known ? fmaxf(z_row[token], -INFINITY) : 0.f;       // (NaN counts as -infinity)
 
   // the wavefront's logits: one run of the split's, in ascending order
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
@@ -204,80 +231,105 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
       }
     }
   };
+  load(from, next);
+  const int token = a.tokens ? uniform(a.tokens[row]) : -1;
+  const bool known = token >= 0 && token < a.V;
+  if (tid < kWaves) sm.deep[tid] = -INFINITY;
+  __syncthreads();
+  const float zt = known ? fmaxf(z_row[token], -INFINITY) + 0.f : 0.f;       // (NaN counts as -infinity, -0 as 0)
+  // above this is at or above zt: the float before it (nothing at all before -infinity: NaN)
+  const float zt_below = zt == -INFINITY ? __builtin_nanf("")
+                         : zt > 0.f      ? __uint_as_float(__float_as_uint(zt) - 1)
+                         : zt < 0.f      ? __uint_as_float(__float_as_uint(zt) + 1)
+                                         : __uint_as_float(0x80000001u);
+
   Stat x{-INFINITY, 0.f, 0.f};
   Best best{-INFINITY, -1};
-  float least = -INFINITY;          // the last place's logit
+  float least = -INFINITY;          // the last place
+  int least_id = -1;
   int ahead = 0;
-  if (from < to) load(from, next);
-  const float zt_below = known && zt > -INFINITY && zt < INFINITY
-                             ? (zt > 0.f ? __uint_as_float(__float_as_uint(zt) - 1)
-                                         : __uint_as_float(__float_as_uint(fminf(zt, -0.f)) + 1))
-                             : zt;              // the float before it: above that is at or above zt
-  const bool plain_rank = zt > -INFINITY && zt < INFINITY && zt != 0.f;
   for (int v0 = from; v0 < to; v0 += kBatch) {
 #pragma unroll
-    for (int i = 0; i < 4 * kLoads; ++i) z[i] = next[i];
+    for (int i = 0; i < 4 * kLoads; ++i) z[i] = fmaxf(next[i], -INFINITY);
     if (v0 + kBatch < to) load(v0 + kBatch, next);
-    float top = fmaxf(z[0], -INFINITY);          // (NaN is passed over)
+    float top = z[0];
 #pragma unroll
     for (int i = 1; i < 4 * kLoads; ++i) top = fmaxf(top, z[i]);
     if (top > x.m) x = against(x, top);
-    if (__any(x.m == INFINITY)) {
+    if (x.m != -INFINITY) {
 #pragma unroll
       for (int i = 0; i < 4 * kLoads; ++i) {
-        const float y = fmaxf(z[i], -INFINITY), w = y == -INFINITY ? 0.f : factor(y, x.m);
-        x.s += w;
-        x.t += w == 0.f ? 0.f : w * (y == x.m ? 0.f : x.m - y);
-      }
-    } else if (x.m != -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < 4 * kLoads; ++i) {
-        const float d = fminf(x.m - z[i], kFar), w = __builtin_amdgcn_exp2f(d * -kLog2e);      // (NaN: kFar)
+        const float d = z[i] == x.m ? 0.f : fminf(x.m - z[i], kFar), w = __builtin_amdgcn_exp2f(d * -kLog2e);
         x.s += w;
         x.t += w * d;
       }
     }
     if (a.rank) {
-      if (plain_rank && v0 + kBatch <= to && (token < v0 || token >= v0 + kBatch)) {
-        const float limit = token < v0 ? zt : zt_below;
+      // (past the run's end -infinity stands, which is no place before the token's)
+      const int before = min(token, to) - v0 - 4 * lane;
 #pragma unroll
-        for (int i = 0; i < 4 * kLoads; ++i) ahead += __builtin_popcountll(__ballot(z[i] > limit));
-      } else {
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = v0 + (u * 64 + lane) * 4 + e;
-            const float y = fmaxf(z[4 * u + e], -INFINITY);
-            // (past the run's end -infinity stands, which is ahead of nothing there)
-            ahead += __builtin_popcountll(__ballot(y > zt || (y == zt && v < token && v < to)));
-          }
-      }
+      for (int i = 0; i < 4 * kLoads; ++i)
+        ahead += __builtin_popcountll(__ballot(!(z[i] <= (256 * (i >> 2) + (i & 3) < before ? zt_below : zt))));
     }
     if (a.top > 0 && __any(top > least)) {
-      // (the first batch: what k lanes' largest reach, the k-th place does)
-      const float bound = v0 == from ? kth_bound(top, a.top) : -INFINITY;
+      if (v0 == from) {
+        // What k lanes' largest reach, the k-th place does: those that reach it and what comes
+        // before the last place so far, up to 64 at a time.
+        const float bound = kth_bound(top, a.top);
+        for (bool more = true; more;) {
+          int n = __builtin_popcountll(__ballot(best.z > -INFINITY));
+          if (lane < n) {
+            sm.pz[wave][lane] = best.z;
+            sm.pi[wave][lane] = best.id;
+          }
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const float most = fmaxf(fmaxf(fmaxf(z[4 * u], z[4 * u + 1]), fmaxf(z[4 * u + 2], z[4 * u + 3])), -INFINITY);
-        uint64_t todo = __ballot(most > least && most >= bound);
-        while (todo != 0) {
-          const int l = __builtin_ctzll(todo);
-          todo &= todo - 1;
+          for (int i = 0; i < 4 * kLoads; ++i) {
+            const int id = v0 + ((i >> 2) * 64 + lane) * 4 + (i & 3);
+            const bool in = (z[i] >= bound) & ((z[i] > least) | ((z[i] == least) & (id < least_id)));
+            const uint64_t mask = __ballot(in);
+            const int at = n + lanes_before(mask);
+            if (in && at < 64) {
+              sm.pz[wave][at] = z[i];
+              sm.pi[wave][at] = id;
+              z[i] = -INFINITY;
+            }
+            n += __builtin_popcountll(mask);
+          }
+          more = n > 64;
+          oda::wave_lds_fence();
+          best = in_order(sm.pz[wave][lane], sm.pi[wave][lane], min(n, 64));
+          if (lane >= a.top) best = Best{-INFINITY, -1};
+          least = lane_value(best.z, a.top - 1);
+          least_id = __builtin_amdgcn_readlane(best.id, a.top - 1);
+          oda::wave_lds_fence();
+        }
+      } else {
+        // Later, what every wavefront has ceil(k / kWaves) logits at or above; the few that
+        // come before the last place one by one, in ascending order.
+        float bound = lane < kWaves ? __hip_atomic_load(&sm.deep[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : INFINITY;
+        bound = -wave_max(-bound);
+        if (__any(top > least && top >= bound)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float y = lane_value(z[4 * u + e], l);
-            if (y > least && y >= bound) {
-              insert(best, y, v0 + (u * 64 + l) * 4 + e);
-              least = lane_value(best.z, a.top - 1);
+          for (int u = 0; u < kLoads; ++u) {
+            const float most = fmaxf(fmaxf(z[4 * u], z[4 * u + 1]), fmaxf(z[4 * u + 2], z[4 * u + 3]));
+            for (uint64_t todo = __ballot(most > least && most >= bound); todo != 0; todo &= todo - 1) {
+              const int l = __builtin_ctzll(todo);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float y = lane_value(z[4 * u + e], l);
+                if (y > least && y >= bound) {
+                  insert(best, y, v0 + (u * 64 + l) * 4 + e);
+                  least = lane_value(best.z, a.top - 1);
+                }
+              }
             }
           }
         }
       }
+      const float mine = lane_value(best.z, (a.top + kWaves - 1) / kWaves - 1);
+      if (lane == 0) __hip_atomic_store(&sm.deep[wave], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   }
-
-  // the workgroup's wavefronts
   x = wave_join(x);
   if (lane == 0) {
     sm.m[wave] = x.m;
@@ -292,88 +344,91 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   __syncthreads();
   if (wave != 0) return;
 
-  // Joins `lists` lists of k places in LDS, the first lists' tokens before the later
-  // ones' where logits are equal: k rounds over the lists' heads.
-  auto merge = [&](int lists) {
-    Best b{-INFINITY, -1};
-    const bool in = lane < lists && a.top > 0;
-    int at = 1;                       // place in the list of the entry behind the head
-    float head = in ? sm.z[lane * a.top] : -INFINITY, next_z = in && a.top > 1 ? sm.z[lane * a.top + 1] : -INFINITY;
-    int id = in ? sm.id[lane * a.top] : -1, next_id = in && a.top > 1 ? sm.id[lane * a.top + 1] : -1;
-    for (int i = 0; i < a.top; ++i) {
-      const float most = wave_max(head);
-      const int l = __builtin_ctzll(__ballot(head == most));
-      const int taken = __builtin_amdgcn_readlane(id, l);
-      if (lane == i) {
-        b.z = most;
-        b.id = taken;
-      }
-      if (lane == l) {
-        head = next_z;
-        id = next_id;
-        ++at;
-        next_z = in && at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
-        next_id = in && at < a.top ? sm.id[lane * a.top + at] : -1;
-      }
-    }
-    return b;
-  };
+  // The workgroup's wavefronts joined, then, by the last of a row's workgroups, its splits.
   x = lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f};
-  x = wave_join(x);
   ahead = lane < kWaves ? sm.ahead[lane] : 0;
-#pragma unroll
-  for (int s = 4; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
-  ahead = uniform(ahead);
-  best = merge(kWaves);
-  if (a.splits == 1) {
-    write_row(a, row, x, ahead, zt, known, best);
-    return;
-  }
   const int words = 2 + a.top;
-  uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
-  if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
-  if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
-  if (lane < a.top) publish(part + 2 + lane, pack(best.z, (uint32_t)best.id));
-  __builtin_amdgcn_s_waitcnt(0);
-  __builtin_amdgcn_wave_barrier();
-  int last = 0;
-  if (lane == 0)
-    last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
-                   (uint32_t)(a.splits - 1)
-               ? 1
-               : 0;
-  if (uniform(last) == 0) return;
   const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
-  x = Stat{-INFINITY, 0.f, 0.f};
-  ahead = 0;
-  if (lane < a.splits) {
-    const uint64_t p0 = published(parts + (int64_t)lane * words), p1 = published(parts + (int64_t)lane * words + 1);
-    x = Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)};
-    ahead = (int)(uint32_t)p1;
-  }
-  // (a trip to memory for up to 1,024 places)
-  constexpr int kTrip = 16;
-  for (int e0 = lane; e0 < a.splits * a.top; e0 += 64 * kTrip) {
-    uint64_t p[kTrip];
+  bool whole = a.splits == 1;       // the lists are all of the row's
+  for (int lists = kWaves;; lists = a.splits) {
+    x = wave_join(x);
 #pragma unroll
-    for (int j = 0; j < kTrip; ++j) {
-      const int e = min(e0 + 64 * j, a.splits * a.top - 1);
-      const int s = e / a.top;
-      p[j] = published(parts + (int64_t)s * words + 2 + (e - s * a.top));
+    for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
+    // Lists of k places in LDS, a list's tokens before the later lists'.  Where the first c
+    // of each reach a bound in ceil(k / c) lists, k logits do: those that reach it are put
+    // in order; where these are too many (equal logits), k rounds over the lists' heads.
+    if (a.top > 0) {
+      const bool mine = lane < lists;
+      const int c = (a.top + lists - 1) / lists;
+      const float bound = kth_bound(mine ? sm.z[lane * a.top + c - 1] : -INFINITY, (a.top + c - 1) / c);
+      int n = 0;
+      for (int j = 0; j < a.top && n <= 64; ++j) {
+        const float y = mine ? sm.z[lane * a.top + j] : -INFINITY;
+        const bool in = y >= bound && y > -INFINITY;
+        const uint64_t mask = __ballot(in);
+        if (mask == 0) break;
+        const int at = n + lanes_before(mask);
+        if (in && at < 64) {
+          sm.pz[0][at] = y;
+          sm.pi[0][at] = sm.id[lane * a.top + j];
+        }
+        n += __builtin_popcountll(mask);
+      }
+      oda::wave_lds_fence();
+      best = Best{-INFINITY, -1};
+      if (n <= 64) {
+        best = in_order(sm.pz[0][lane], sm.pi[0][lane], n);
+      } else {
+        int at = 0;
+        for (int i = 0; i < a.top; ++i) {
+          const float head = mine && at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
+          const float most = wave_max(head);
+          const int l = __builtin_ctzll(__ballot(head == most));
+          if (lane == l && most > -INFINITY) {
+            sm.pi[0][i] = sm.id[lane * a.top + at];
+            ++at;
+          }
+          if (lane == i) best.z = most;
+        }
+        oda::wave_lds_fence();
+        if (best.z > -INFINITY) best.id = sm.pi[0][lane];
+      }
     }
+    if (whole) break;
+    whole = true;
+    uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
+    if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
+    if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
+    if (lane < a.top) publish(part + 2 + lane, pack(best.z, (uint32_t)best.id));
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_wave_barrier();
+    int last = 0;
+    if (lane == 0)
+      last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
+                     (uint32_t)(a.splits - 1)
+                 ? 1
+                 : 0;
+    if (uniform(last) == 0) return;
+    // (a lane a split; a trip to memory for sixteen places of all)
+    constexpr int kTrip = 16;
+    const uint64_t* list = parts + (int64_t)min(lane, a.splits - 1) * words;
+    const uint64_t p0 = published(list), p1 = published(list + 1);
+    for (int j0 = 0; j0 < a.top; j0 += kTrip) {
+      uint64_t p[kTrip];
 #pragma unroll
-    for (int j = 0; j < kTrip; ++j) {
-      const int e = min(e0 + 64 * j, a.splits * a.top - 1);
-      sm.z[e] = first_of(p[j]);
-      sm.id[e] = (int)(uint32_t)p[j];
+      for (int j = 0; j < kTrip; ++j) p[j] = published(list + 2 + min(j0 + j, a.top - 1));
+#pragma unroll
+      for (int j = 0; j < kTrip; ++j) {
+        if (lane >= a.splits || j0 + j >= a.top) continue;
+        sm.z[lane * a.top + j0 + j] = first_of(p[j]);
+        sm.id[lane * a.top + j0 + j] = (int)(uint32_t)p[j];
+      }
     }
+    x = lane < a.splits ? Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)} : Stat{-INFINITY, 0.f, 0.f};
+    ahead = lane < a.splits ? (int)(uint32_t)p1 : 0;
+    oda::wave_lds_fence();
   }
-  x = wave_join(x);
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  best = merge(a.splits);
-  write_row(a, row, x, ahead, zt, known, best);
+  write_row(a, row, x, uniform(ahead), zt, known, best);
 }
 
 // Workgroups of a row: at most kGroups in all, each of at least kLeastSplit logits.
@@ -381,7 +436,7 @@ void split_row(int64_t rows, int64_t vocab, int* splits, int* chunk) {
   int64_t n = 1;
   if (rows <= kTickets)
     n = std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, kGroups / rows, vocab / kLeastSplit}));
-  *chunk = (int)oda::round_up(oda::ceil_div(vocab, n), 4);
+  *chunk = (int)oda::round_up(oda::ceil_div(vocab, n), n > 1 ? kGrain : 4);
   *splits = (int)oda::ceil_div(vocab, *chunk);
 }
 
