@@ -104,15 +104,25 @@ __device__ __forceinline__ Tile find_tile(const AppendArgs& a, int tile) {
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 load4(const uint16_t* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-               __uint_as_float(w.y & 0xffff0000u)};
-}
+// Four neighbouring values as they lie in memory, and widened.
+template <typename In>
+struct Four;
+template <>
+struct Four<float> {
+  typedef f32x4 raw;
+  static __device__ __forceinline__ f32x4 wide(f32x4 x) { return x; }
+};
+template <>
+struct Four<uint16_t> {
+  typedef uint2 raw;
+  static __device__ __forceinline__ f32x4 wide(uint2 w) {
+    return f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                 __uint_as_float(w.y & 0xffff0000u)};
+  }
+};
 __device__ __forceinline__ uint2 round4(f32x4 x) {
-  return make_uint2((uint32_t)oda::bf16_rne(x[0]) | (uint32_t)oda::bf16_rne(x[1]) << 16,
-                    (uint32_t)oda::bf16_rne(x[2]) | (uint32_t)oda::bf16_rne(x[3]) << 16);
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint2, __builtin_convertvector(x, bf16x4));
 }
 
 // Four rows (one per 16 lanes) of four dimensions each to one dimension (the lane's
@@ -166,17 +176,15 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     h.in = h.head < (h.kind == 0 ? a.Hq : a.Hkv);
     return h;
   };
-  f32x4 x[kInFlight][2];
-  auto load = [&](int s) {
-#pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const Head h = head_of(min(s + u, s1 - 1));
-      const int at = h.in ? (h.kind == 0 ? h.head : h.kind == 1 ? a.Hq + h.head : a.Hq + a.Hkv + h.head) : 0;
-      x[u][0] = load4(src + (int64_t)at * D);
-      x[u][1] = load4(src + (int64_t)at * D + D / 2);
-    }
+  typename Four<In>::raw x[kInFlight][2];
+  auto load = [&](int s, int u) {
+    const Head h = head_of(min(s, s1 - 1));
+    const int at = h.in ? (h.kind == 0 ? h.head : h.kind == 1 ? a.Hq + h.head : a.Hq + a.Hkv + h.head) : 0;
+    x[u][0] = *reinterpret_cast<const typename Four<In>::raw*>(src + (int64_t)at * D);
+    x[u][1] = *reinterpret_cast<const typename Four<In>::raw*>(src + (int64_t)at * D + D / 2);
   };
-  load(s0);
+#pragma unroll
+  for (int u = 0; u < kInFlight; ++u) load(s0 + u, u);
 
   // block and ring block of the rows
   int64_t blk = -1, ring = -1;
@@ -234,18 +242,12 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   };
 
   for (int s = s0; s < s1; s += kInFlight) {
-    f32x4 y[kInFlight][2];
-#pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      y[u][0] = x[u][0];
-      y[u][1] = x[u][1];
-    }
-    if (s + kInFlight < s1) load(s + kInFlight);
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (s + u >= s1) break;
       const Head h = head_of(s + u);
-      f32x4 lo = y[u][0], hi = y[u][1];
+      f32x4 lo = Four<In>::wide(x[u][0]), hi = Four<In>::wide(x[u][1]);
+      load(s + u + kInFlight, u);
       if (h.kind < 2) {
         const float* gain = h.kind == 0 ? a.q_gain : a.k_gain;
         if (gain != nullptr) {
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 #pragma unroll
           for (int k = kLanes / 2; k >= 1; k >>= 1) ss += __shfl_xor(ss, k);
           const float inv = rsqrtf(ss / (float)D + a.eps);
-          const f32x4 g0 = load4(gain + 4 * sub), g1 = load4(gain + 4 * sub + D / 2);
+          const f32x4 g0 = *reinterpret_cast<const f32x4*>(gain + 4 * sub), g1 = *reinterpret_cast<const f32x4*>(gain + 4 * sub + D / 2);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             lo[e] = lo[e] * inv * g0[e];
