@@ -22,7 +22,7 @@
 namespace {
 
 constexpr int kBlock = 16;       // positions per KV block, rows of a workgroup
-constexpr int kWaves = 4;        // of four rows each
+constexpr int kWaves = 8;        // share the heads
 constexpr int kThreads = kWaves * 64;
 
 struct AppendArgs {
@@ -139,28 +139,24 @@ __device__ __forceinline__ uint2 transpose4(uint2 x, int r) {
 }
 
 // One workgroup per (block of a request's rows, chunk of head slots).  A wavefront
-// holds four rows, sixteen lanes each: a lane has four dimensions and those half a
-// head behind them (the pairs that the rotation mixes) of one head, or of one of two
-// heads of 64; its angles are formed once for all heads.
-constexpr int kInFlight = 4;     // head slots whose loads are in flight together
+// takes every kWaves-th slot and goes through its rows four at a time, sixteen lanes a
+// row: a lane has four dimensions and those half a head behind them (the pairs that the
+// rotation mixes) of one head, or of one of two heads of 64.  The rows' angles are formed
+// once for all heads, side by side, and lie in LDS.
+constexpr int kInFlight = 4;     // of a wavefront: loads of four rows and a slot that are in flight together
 template <int D, typename In>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   constexpr int HS = 128 / D;    // heads of a slot
   constexpr int kLanes = D / 8;  // lanes of a head
+  __shared__ __attribute__((aligned(16))) float s_cos[kBlock][D / 2], s_sin[kBlock][D / 2];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const Tile t = find_tile(a, blockIdx.x);
   if (t.request < 0) return;
   const int r = lane >> 4, sub = lane & (kLanes - 1), which = (lane >> 3) & (HS - 1);
-  const int slot0 = 4 * wave;                                    // the wavefront's first slot of the block
-  const int pos = t.block * kBlock + slot0 + r;
-  const int i = pos - t.place0;
-  const bool valid = i >= 0 && i < t.rows;
-  const uint64_t any = __ballot(valid);
-  if (any == 0) return;
-  const bool all = any == ~0ull;
-  const int row = t.row0 + min(max(i, 0), t.rows - 1);
+  const int first = max(t.place0 - t.block * kBlock, 0);                         // rows of the block
+  const int last = min(t.place0 + t.rows - t.block * kBlock, kBlock) - 1;
+  const int row0 = t.row0 + t.block * kBlock - t.place0;                          // of the block's first place
   const int heads = a.Hq + 2 * a.Hkv;
-  const In* src = static_cast<const In*>(a.qkv) + (int64_t)row * heads * D + 4 * sub;
 
   // slots: of q, then k, then v heads
   const int q_slots = (a.Hq + HS - 1) / HS, k_slots = (a.Hkv + HS - 1) / HS;
@@ -176,78 +172,73 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     h.in = h.head < (h.kind == 0 ? a.Hq : a.Hkv);
     return h;
   };
+  // items of the wavefront: its slots, of each the groups of four rows
+  const int g0 = first >> 2, groups = (last >> 2) - g0 + 1;
+  const int items = s0 + wave < s1 ? ((s1 - s0 - wave + kWaves - 1) / kWaves) * groups : 0;
   typename Four<In>::raw x[kInFlight][2];
-  auto load = [&](int s, int u) {
-    const Head h = head_of(min(s, s1 - 1));
+  int load_s = s0 + wave, load_g = 0;
+  auto load = [&](int u) {       // the next item's; past the last one it again
+    const Head h = head_of(load_s);
     const int at = h.in ? (h.kind == 0 ? h.head : h.kind == 1 ? a.Hq + h.head : a.Hq + a.Hkv + h.head) : 0;
-    x[u][0] = *reinterpret_cast<const typename Four<In>::raw*>(src + (int64_t)at * D);
-    x[u][1] = *reinterpret_cast<const typename Four<In>::raw*>(src + (int64_t)at * D + D / 2);
+    const int row = row0 + min(max(4 * (g0 + load_g) + r, first), last);
+    const In* src = static_cast<const In*>(a.qkv) + ((int64_t)row * heads + at) * D + 4 * sub;
+    x[u][0] = *reinterpret_cast<const typename Four<In>::raw*>(src);
+    x[u][1] = *reinterpret_cast<const typename Four<In>::raw*>(src + D / 2);
+    if (load_g + 1 < groups) {
+      ++load_g;
+    } else if (load_s + kWaves < s1) {
+      load_g = 0;
+      load_s += kWaves;
+    }
   };
+  if (items > 0) {
 #pragma unroll
-  for (int u = 0; u < kInFlight; ++u) load(s0 + u, u);
+    for (int u = 0; u < kInFlight; ++u) load(u);
+  }
 
   // block and ring block of the rows
   int64_t blk = -1, ring = -1;
   if (a.Hkv > 0 && !t.bad && s1 > q_slots) {
     const int e = a.block_table[(int64_t)t.request * a.MB + t.block];
     blk = e >= 0 && e < a.num_blocks ? e : -1;
-    const int last = (t.place0 + t.rows - 1) / kBlock;
-    if (a.k_ring != nullptr && (t.block < a.sink_blocks || t.block > last - a.ring_blocks))
+    const int end = (t.place0 + t.rows - 1) / kBlock;
+    if (a.k_ring != nullptr && (t.block < a.sink_blocks || t.block > end - a.ring_blocks))
       ring = (int64_t)t.request * (a.sink_blocks + a.ring_blocks) +
              (t.block < a.sink_blocks ? t.block : a.sink_blocks + t.block % a.ring_blocks);
   }
-  // the rotation of the lane's four pairs
-  float cs[4], sn[4];
-  if (a.log2_theta != 0.0 && s0 < q_slots + k_slots) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int pair = 4 * sub + e;
-      int p = pos;
-      if (a.positions != nullptr) {
-        int axis = 0;
-        for (int k = 0; k + 1 < a.axes; ++k) axis += pair >= a.axis_end[k] ? 1 : 0;
-        p = a.positions[(int64_t)row * a.axes + axis];
-      }
+  const bool turns = a.log2_theta != 0.0 && s0 < q_slots + k_slots;
+  if (turns) {
+    const int pair = threadIdx.x % (D / 2);
+    const double frequency = oda::rope_frequency(pair, D, a.log2_theta);
+    int axis = 0;
+    for (int k = 0; k + 1 < a.axes; ++k) axis += pair >= a.axis_end[k] ? 1 : 0;
+    for (int i = first + threadIdx.x / (D / 2); i <= last; i += kThreads / (D / 2)) {
+      const int p = a.positions != nullptr ? a.positions[(int64_t)(row0 + i) * a.axes + axis] : t.block * kBlock + i;
       double sd, cd;
-      oda::sincos_angle((double)p * oda::rope_frequency(pair, D, a.log2_theta), sd, cd);
-      cs[e] = (float)cd;
-      sn[e] = (float)sd;
+      oda::sincos_angle((double)p * frequency, sd, cd);
+      s_cos[i][pair] = (float)cd;
+      s_sin[i][pair] = (float)sd;
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      cs[e] = 1.f;
-      sn[e] = 0.f;
-    }
+    __syncthreads();
   }
 
-  auto put_k = [&](uint16_t* dst, uint2 lo, uint2 hi) {      // a block of one KV head: [D/8][16][8]
-    const int at = ((sub >> 1) * kBlock + slot0 + r) * 8 + 4 * (sub & 1);
-    *reinterpret_cast<uint2*>(dst + at) = lo;
-    *reinterpret_cast<uint2*>(dst + at + (D / 16) * kBlock * 8) = hi;
-  };
-  auto put_v = [&](uint16_t* dst, uint2 lo, uint2 hi) {      // [D][16]; lo, hi: dimension 4 sub + r of four rows
-    uint16_t* p = dst + (4 * sub + r) * kBlock + slot0;
-    if (all) {
-      *reinterpret_cast<uint2*>(p) = lo;
-      *reinterpret_cast<uint2*>(p + (D / 2) * kBlock) = hi;
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if ((any >> (16 * e) & 1) == 0) continue;
-      p[e] = (uint16_t)((e < 2 ? lo.x : lo.y) >> (16 * (e & 1)));
-      p[(D / 2) * kBlock + e] = (uint16_t)((e < 2 ? hi.x : hi.y) >> (16 * (e & 1)));
-    }
-  };
-
-  for (int s = s0; s < s1; s += kInFlight) {
+  int s = s0 + wave, g = 0;
+  for (int i0 = 0; i0 < items; i0 += kInFlight) {
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
-      if (s + u >= s1) break;
-      const Head h = head_of(s + u);
+      if (i0 + u >= items) break;
       f32x4 lo = Four<In>::wide(x[u][0]), hi = Four<In>::wide(x[u][1]);
-      load(s + u + kInFlight, u);
+      load(u);
+      const Head h = head_of(s);
+      const int slot0 = 4 * (g0 + g), slot = slot0 + r;          // places of the block
+      const bool valid = slot >= first && slot <= last;
+      const int row = row0 + min(max(slot, first), last);
+      if (g + 1 < groups) {
+        ++g;
+      } else {
+        g = 0;
+        s += kWaves;
+      }
       if (h.kind < 2) {
         const float* gain = h.kind == 0 ? a.q_gain : a.k_gain;
         if (gain != nullptr) {
@@ -257,14 +248,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 #pragma unroll
           for (int k = kLanes / 2; k >= 1; k >>= 1) ss += __shfl_xor(ss, k);
           const float inv = rsqrtf(ss / (float)D + a.eps);
-          const f32x4 g0 = *reinterpret_cast<const f32x4*>(gain + 4 * sub), g1 = *reinterpret_cast<const f32x4*>(gain + 4 * sub + D / 2);
+          const f32x4 a0 = *reinterpret_cast<const f32x4*>(gain + 4 * sub), a1 = *reinterpret_cast<const f32x4*>(gain + 4 * sub + D / 2);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            lo[e] = lo[e] * inv * g0[e];
-            hi[e] = hi[e] * inv * g1[e];
+            lo[e] = lo[e] * inv * a0[e];
+            hi[e] = hi[e] * inv * a1[e];
           }
         }
-        if (a.log2_theta != 0.0) {
+        if (turns) {
+          const int at = min(max(slot, first), last);
+          const f32x4 cs = *reinterpret_cast<const f32x4*>(&s_cos[at][4 * sub]), sn = *reinterpret_cast<const f32x4*>(&s_sin[at][4 * sub]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float r1 = lo[e] * cs[e] - hi[e] * sn[e], r2 = hi[e] * cs[e] + lo[e] * sn[e];
@@ -274,6 +267,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
         }
       }
       uint2 lo4 = round4(lo), hi4 = round4(hi);
+      const int64_t head = (int64_t)h.head * kBlock * D, head_stride = (int64_t)a.Hkv * kBlock * D;
       if (h.kind == 0) {
         if (t.bad) lo4 = hi4 = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
         if (valid && h.in) {
@@ -281,20 +275,38 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
           *reinterpret_cast<uint2*>(dst) = lo4;
           *reinterpret_cast<uint2*>(dst + D / 2) = hi4;
         }
-        continue;
+      } else if (h.kind == 1) {
+        // a block of one KV head: [D/8][16][8]
+        const int64_t at = head + ((sub >> 1) * kBlock + slot) * 8 + 4 * (sub & 1), half = (D / 16) * kBlock * 8;
+        if (valid && h.in && blk >= 0) {
+          *reinterpret_cast<uint2*>(a.k_cache + blk * head_stride + at) = lo4;
+          *reinterpret_cast<uint2*>(a.k_cache + blk * head_stride + at + half) = hi4;
+        }
+        if (valid && h.in && ring >= 0) {
+          *reinterpret_cast<uint2*>(a.k_ring + ring * head_stride + at) = lo4;
+          *reinterpret_cast<uint2*>(a.k_ring + ring * head_stride + at + half) = hi4;
+        }
+      } else {
+        // [D][16]: the lane's dimension 4 sub + r of four rows
+        lo4 = transpose4(lo4, r);
+        hi4 = transpose4(hi4, r);
+        auto put = [&](uint16_t* p) {
+          p += head + (4 * sub + r) * kBlock + slot0;
+          if (slot0 >= first && slot0 + 3 <= last) {
+            *reinterpret_cast<uint2*>(p) = lo4;
+            *reinterpret_cast<uint2*>(p + (D / 2) * kBlock) = hi4;
+            return;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (slot0 + e < first || slot0 + e > last) continue;
+            p[e] = (uint16_t)((e < 2 ? lo4.x : lo4.y) >> (16 * (e & 1)));
+            p[(D / 2) * kBlock + e] = (uint16_t)((e < 2 ? hi4.x : hi4.y) >> (16 * (e & 1)));
+          }
+        };
+        if (h.in && blk >= 0) put(a.v_cache + blk * head_stride);
+        if (h.in && ring >= 0) put(a.v_ring + ring * head_stride);
       }
-      const int64_t head = (int64_t)h.head * kBlock * D, head_stride = (int64_t)a.Hkv * kBlock * D;
-      if (h.kind == 1) {
-        if (!valid || !h.in) continue;
-        if (blk >= 0) put_k(a.k_cache + blk * head_stride + head, lo4, hi4);
-        if (ring >= 0) put_k(a.k_ring + ring * head_stride + head, lo4, hi4);
-        continue;
-      }
-      lo4 = transpose4(lo4, r);
-      hi4 = transpose4(hi4, r);
-      if (!h.in) continue;
-      if (blk >= 0) put_v(a.v_cache + blk * head_stride + head, lo4, hi4);
-      if (ring >= 0) put_v(a.v_ring + ring * head_stride + head, lo4, hi4);
     }
   }
 }
@@ -384,7 +396,7 @@ extern "C" oda_status oda_append_qkv(const oda_attn_shape* shape, const oda_prom
   a.slots = (int)(oda::ceil_div(a.Hq, per) + 2 * oda::ceil_div(a.Hkv, per));
   // a request's m rows touch at most m / 16 + 2 blocks, and at most m
   const int64_t tiles = std::min<int64_t>(a.R, (int64_t)a.R / kBlock + 2 * (int64_t)a.B);
-  const int64_t chunks = std::min<int64_t>(oda::ceil_div(a.slots, kInFlight), std::max<int64_t>(1, oda::ceil_div(1024, tiles)));
+  const int64_t chunks = std::min<int64_t>(oda::ceil_div(a.slots, kWaves), std::max<int64_t>(1, oda::ceil_div(512, tiles)));
   a.chunk = (int)oda::ceil_div(a.slots, chunks);
   const dim3 grid((unsigned)tiles, (unsigned)oda::ceil_div(a.slots, a.chunk));
   return desc->qkv_type == ODA_F32 ? launch<float>(a, shape->head_dim, grid, stream)
