@@ -20,7 +20,9 @@ Per step (Alg. 1 with the commit of App. A.5):
 Native Full (always Full, no gate) and standalone Local (no gate, no retry)
 use the same pieces.  DraftDecoder composes the step of many tenants with drafted
 tokens: shared-prefix attention, adapters beside the dense layers, verification
-and the commit of what was accepted.  Stages are lists of pre-marshalled calls, so they can be
+and the commit of what was accepted.  PromptDecoder takes prompts in: chunks of many
+tokens per request through the same layers into the paged cache, from which the
+others go on.  Stages are lists of pre-marshalled calls, so they can be
 launched eagerly or captured as HIP graphs.
 """
 from __future__ import annotations
@@ -330,6 +332,114 @@ class DraftDecoder:
         return (forward, [P.prepare_verify_drafts(verify, B, self.accepted, self.answer, self.ws_verify)],
                 [P.prepare_commit_drafts(self.commit_shape, T, self.k_cache, self.v_cache, self.table, self.seq_lens,
                                          self.k_cand, self.v_cand, self.accepted, True, self.row_lens, self.ws_commit)])
+
+
+class PromptDecoder:
+    """Prompts into the paged cache, a chunk of each request at a time: one forward of
+    the chunk's tokens (causal attention behind what the cache holds already), their
+    K/V appended layer by layer, and, of the last row of each request or of every row,
+    the log probabilities of given tokens, the entropy and the first of the order.
+
+    set_chunk(tokens, row_start, targets) gives the next chunk: rows row_start[b] ..
+    row_start[b + 1] - 1 of `tokens` are request b's (none: it waits); `seq_lens` grows by
+    them and then counts what the cache holds.  Decoder and DraftDecoder count the current
+    token too: add 1 to the lengths before their first step.
+
+    rows: rows of the buffers (chunks may have fewer); rings: (k_ring, v_ring, n_sink,
+    window) to keep the direct rings [L][B][..] current; axis_pairs: rotary axes of
+    `positions` [rows][axes], written before each chunk (None: places of the history);
+    score: "last" or "all" rows; top: alternatives per scored row; native_window: of every
+    layer (0: the whole history)."""
+
+    def __init__(self, shape: DecoderShape, weights: dict, batch: int, rows: int, k_cache, v_cache, block_table, seq_lens,
+                 max_blocks_per_seq: int, max_seq_len: int, num_blocks: int, rings=None, axis_pairs=None, score: str = "last",
+                 top: int = 0, native_window: int = 0):
+        import torch
+        if score not in ("last", "all"):
+            raise ValueError(f"score must be 'last' or 'all' (got {score!r})")
+        s, B = shape, batch
+        dev = k_cache.device
+        self.shape, self.B, self.rows, self.w = s, B, rows, weights
+        self.k_cache, self.v_cache, self.table, self.seq_lens = k_cache, v_cache, block_table, seq_lens
+        self.rings, self.axis_pairs, self.native_window = rings, axis_pairs, native_window
+        f32 = dict(dtype=torch.float32, device=dev)
+        i32 = dict(dtype=torch.int32, device=dev)
+        L, d, Hq, Hkv, D = s.num_layers, s.d_model, s.num_q_heads, s.num_kv_heads, s.head_dim
+        self.tokens = torch.zeros(rows, **i32)
+        self.targets = torch.full((rows,), -1, **i32)
+        self.row_start = torch.zeros(B + 1, **i32)
+        self.positions = None if axis_pairs is None else torch.zeros(rows, len(axis_pairs), **i32)
+        self.listed = torch.zeros(rows, **i32) if score == "last" else None     # scored rows
+        self.n_listed = torch.zeros(1, **i32) if score == "last" else None
+        self.h = torch.zeros(rows, d, **f32)
+        self.state = torch.zeros(rows, d, **f32)       # final-normalised
+        self.qkv = torch.zeros(rows, s.qkv_dim, **f32)
+        self.q = torch.zeros(rows, Hq, D, dtype=torch.bfloat16, device=dev)
+        self.attn = torch.zeros(rows, Hq * D, **f32)
+        self.mlp = torch.zeros(rows, s.d_ffn, **f32)
+        self.logits = torch.zeros(rows, s.vocab, **f32)
+        self.logprob, self.entropy = torch.zeros(rows, **f32), torch.zeros(rows, **f32)
+        self.rank = torch.zeros(rows, **i32)
+        self.top_logprobs = torch.zeros(rows, top, **f32) if top else None
+        self.top_tokens = torch.zeros(rows, top, **i32) if top else None
+        self.scale = 1.0 / math.sqrt(D)
+        self.attn_shape = P.Shape(1, B, Hq, Hkv, D, max_blocks_per_seq, max_seq_len, num_blocks)
+        self.prompt_rows = P.prompt_rows(rows, self.row_start)
+        self.scored = P.logprob_desc(s.vocab, top, self.logits, self.targets)
+
+        def zeros(n):
+            return torch.zeros(max(256, n), dtype=torch.uint8, device=dev)
+
+        self.plan = zeros(P.prompt_plan_size(self.attn_shape, self.prompt_rows))
+        self.ws_attn = zeros(P.prompt_workspace_size(self.attn_shape, self.prompt_rows))
+        self.ws_score = zeros(P.logprob_workspace_size(self.scored, rows))
+
+    def set_chunk(self, tokens, row_start, targets=None) -> None:
+        """The next chunk: tokens [n <= rows], row_start [B + 1], targets [n] (the tokens to score, -1: none)."""
+        import torch
+        n = tokens.numel()
+        if n > self.rows:
+            raise ValueError(f"{n} rows in a chunk, room for {self.rows}")
+        self.tokens.zero_()                             # rows of no request keep a token of the vocabulary
+        self.tokens[:n].copy_(tokens)
+        self.targets.fill_(-1)
+        if targets is not None:
+            self.targets[:n].copy_(targets)
+        self.row_start.copy_(row_start)
+        count = self.row_start[1:] - self.row_start[:-1]
+        self.seq_lens.add_(count)
+        if self.listed is not None:
+            order = torch.argsort((count <= 0).to(torch.int32), stable=True)[:self.rows]     # requests with rows first
+            self.listed[:order.numel()].copy_(self.row_start[1:][order] - 1)
+            self.n_listed.copy_((count > 0).sum())
+
+    def stages(self):
+        """(forward, scores) of one chunk, as prepared calls."""
+        s, w, n = self.shape, self.w, self.rows
+        Hq, Hkv, D, d = s.num_q_heads, s.num_kv_heads, s.head_dim, s.d_model
+        forward = [P.prepare_embed(w["embed"], s.vocab, d, n, self.tokens, self.h),
+                   P.prepare_prompt_plan(self.attn_shape, self.prompt_rows, self.seq_lens, True, self.native_window, self.plan)]
+        for l in range(s.num_layers):
+            rings = () if self.rings is None else (self.rings[0][l], self.rings[1][l], self.rings[2], self.rings[3])
+            desc = P.append_desc(self.qkv, w["q_norm"][l], w["k_norm"][l], s.rms_eps, s.rope_theta, self.positions,
+                                 self.axis_pairs)
+            inp = P.inputs(self.q, self.k_cache[l], self.v_cache[l], self.table, self.seq_lens, self.scale)
+            forward += [
+                P.prepare_dense(P.dense_desc(d, s.qkv_dim, P.DENSE_PLAIN, w["w_qkv"][l], w["attn_norm"][l], s.rms_eps), n,
+                                self.h, None, self.qkv),
+                P.prepare_append_qkv(self.attn_shape, self.prompt_rows, desc, self.k_cache[l], self.v_cache[l], self.table,
+                                     self.seq_lens, self.q, *rings),
+                P.prepare_prompt_attn(self.attn_shape, inp, self.prompt_rows, self.plan, self.attn, None, self.ws_attn),
+                P.prepare_dense(P.dense_desc(Hq * D, d, P.DENSE_PLAIN, w["w_o"][l]), n, self.attn, self.h, self.h),
+                P.prepare_dense(P.dense_desc(d, s.d_ffn, P.DENSE_SWIGLU, w["w_gu"][l], w["mlp_norm"][l], s.rms_eps), n, self.h,
+                                None, self.mlp),
+                P.prepare_dense(P.dense_desc(s.d_ffn, d, P.DENSE_PLAIN, w["w_down"][l]), n, self.mlp, self.h, self.h)]
+        listed = (self.listed, self.n_listed)
+        scores = [P.prepare_rms_norm_rows(n, d, self.h, w["final_norm"], s.rms_eps, self.state, *listed),
+                  P.prepare_dense(P.dense_desc(d, s.vocab, P.DENSE_PLAIN, w["embed"]), n, self.state, None, self.logits, *listed),
+                  P.prepare_token_logprobs(self.scored, n, self.logprob, self.rank, self.entropy, self.top_logprobs,
+                                           self.top_tokens, self.ws_score, *listed)]
+        return forward, scores
 
 
 def run(calls) -> None:
