@@ -378,12 +378,13 @@ struct PromptArgs {
   void* out;                 // [R][Hq][D] fp32 or bf16
   float* lse;                // [R][Hq] or NULL
   float* part_o;             // [Hkv][part_cols][D]
-  float* part_ml;            // [Hkv][part_cols][2]  (reference in exponents of 2, sum)
+  float* part_ml;            // [Hkv][part_cols][2]  (reference in score units, sum)
   int64_t num_blocks;
   int64_t part_cols;
   int32_t B, R, Hq, Hkv, G, MB, max_len;
   int32_t max_items, max_merges;
-  float scale_log2;
+  float scale_log2;          // of a score, for exponents of 2
+  float lag;                 // kLag in score units
 };
 
 __device__ __forceinline__ bool plan_fits(const PromptArgs& a, const PlanHeader& h) {
@@ -413,7 +414,7 @@ template <typename Out>
 constexpr int kPartsOf = std::is_same<Out, float>::value ? 3 : 1;
 
 // A wavefront's columns: o[n][4 i + j] is dimension 32 n + 8 i + 4 h + j of column
-// lane % 32, h = lane / 32; ref the reference of its weights in exponents of 2
+// lane % 32, h = lane / 32; ref the reference of its weights in score units
 // (-infinity: none yet), sum this lane's part of their sum; attended positions [lo, hi).
 template <int D>
 struct Columns {
@@ -473,41 +474,49 @@ __device__ __forceinline__ void weigh_pair(const Parts<P>& part, Columns<D>& w, 
     }
 }
 
+// The weight of a score against a reference.  (The difference first: it is exact where
+// it matters, also for scores whose product with the scale would be off by more than
+// the exponents' range.)
+__device__ __forceinline__ float weight_of(float s, float ref, float scale_log2) {
+  return __builtin_amdgcn_exp2f((s - ref) * scale_log2);
+}
 // Weights of a pair's scores against the column's reference, and the lane's sum.
 //
-// Weights are taken against a reference kLag above the largest score at which it
-// was set and below no later one: at most 1, and their sum 2^-kLag or more.  The
-// largest score is looked for, and sums are rescaled, only where a lane's weights add
-// up to more than 1 or there is no reference yet (its weights come out infinite or
-// NaN).  The reference is kept as the exponent that is taken off, so that all weights
-// of a column are against the same number, to the bit, whatever its size.
+// Weights are taken against a reference kLag (in exponents of 2) above the largest score
+// at which it was set and below no later one: at most 1, and their sum 2^-kLag or more.
+// The largest score is looked for, and sums are rescaled, only where a lane's weights add
+// up to more than 1 or there is no reference yet (its weights come out infinite or NaN).
 constexpr float kLag = 6.f;
-__device__ __forceinline__ float weights_of(float scale_log2, const f32x16& s, float ref, f32x16& p) {
+constexpr float kMaxLag = 1e37f;     // (scores of a scale that small all weigh the same)
+template <int P>
+__device__ __forceinline__ float weights_of(float scale_log2, const f32x16& s, float ref, Parts<P>& part) {
+  f32x16 p;
   float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -ref));
+    p[i] = weight_of(s[i], ref, scale_log2);
     t[i & 3] += p[i];
   }
+  part = parts_of<P>(p);
   return (t[0] + t[1]) + (t[2] + t[3]);
 }
 // The sum's check, after all products of earlier pairs: raises the reference where it fails.
-template <int D>
-__device__ __forceinline__ void settle(float scale_log2, const f32x16& s, Columns<D>& w, f32x16& p, float sum) {
+template <int D, int P>
+__device__ __forceinline__ void settle(float scale_log2, float lag, const f32x16& s, Columns<D>& w, Parts<P>& part, float sum) {
   if (__any(!(sum <= 1.f))) {
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    const float top = fmaxf(w.ref, column_max(mx) * scale_log2 + kLag);
+    const float top = fmaxf(w.ref, fminf(column_max(mx) + lag, FLT_MAX));
     const float ref = top == -INFINITY ? 0.f : top;
-    const float alpha = __builtin_amdgcn_exp2f(w.ref - ref);
+    const float alpha = weight_of(w.ref, ref, scale_log2);
     w.ref = top;
     w.sum *= alpha;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) w.o[n][i] *= alpha;
-    sum = weights_of(scale_log2, s, ref, p);
+    sum = weights_of<P>(scale_log2, s, ref, part);
   }
   w.sum += sum;
 }
@@ -672,7 +681,9 @@ __device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<f
 __device__ __forceinline__ void store4(uint16_t* p, float4 x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(round_pair(x.x, x.y), round_pair(x.z, x.w));
 }
-__device__ __forceinline__ float lse_of(float c, float l) { return l == 0.f ? -INFINITY : (c + __log2f(l)) * kLn2; }
+__device__ __forceinline__ float lse_of(float ref, float l, float scale_log2) {
+  return l == 0.f ? -INFINITY : (ref * scale_log2 + __log2f(l)) * kLn2;
+}
 __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // Where a column goes: a partial, or the outputs.
@@ -732,7 +743,7 @@ __device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g,
 #pragma unroll
     for (int p = 0; p < WP; ++p) {
       const int from = p * WC * kCols + col;
-      const float s = __builtin_amdgcn_exp2f(sm_c[from] - ref);
+      const float s = weight_of(sm_c[from], ref, a.scale_log2);
       const float4 x = *reinterpret_cast<const float4*>(sm_o + from * o_stride(D) + d);
       acc.x += s * x.x;
       acc.y += s * x.y;
@@ -747,7 +758,7 @@ __device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g,
     } else {
       const float inv = inverse_of(l);
       store4(t.out + d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (d == 0 && t.lse) *t.lse = lse_of(ref, l);
+      if (d == 0 && t.lse) *t.lse = lse_of(ref, l, a.scale_log2);
     }
   }
 }
@@ -772,7 +783,7 @@ __device__ __forceinline__ void write_columns(const PromptArgs& a, const Item& i
     }
   if (h != 0) return;
   if (it.part >= 0) *reinterpret_cast<float2*>(t.part_ml) = make_float2(ref, w.sum);
-  else if (t.lse) *t.lse = lse_of(ref, w.sum);
+  else if (t.lse) *t.lse = lse_of(ref, w.sum, a.scale_log2);
 }
 
 // One column tile: the wavefronts take contiguous ranges of pairs, K and V go straight
@@ -828,10 +839,10 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
 #pragma unroll
         for (int b = 0; b < 2; ++b) vr[n][b] = finite_values(first_values(it.n - pos - kBlock * b - 8 * h, vr[n][b]), odd);
     }
-    f32x16 p;
-    const float sum = weights_of(a.scale_log2, s, w.ref, p);
-    settle<D>(a.scale_log2, s, w, p, sum);
-    weigh_pair<D, P>(parts_of<P>(p), w, [&](int n, int b) { return vr[n][b]; });
+    Parts<P> part;
+    const float sum = weights_of<P>(a.scale_log2, s, w.ref, part);
+    settle<D, P>(a.scale_log2, a.lag, s, w, part, sum);
+    weigh_pair<D, P>(part, w, [&](int n, int b) { return vr[n][b]; });
     if (__any(odd)) {
       const uint16_t* v0 = a.v_cache + (int64_t)g * block_elems(D);
       add_odd_values<D>(v0 + b0, v0 + b1, pos, end, w);
@@ -942,18 +953,18 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
   auto full_step = [&](int i, f32x16& s_now, f32x16& s_next) {
     const uint16_t* vs = v_get + stage_of(i - 1);
     bf16x8 vf[D / 32][2];
-    f32x16 p;
+    Parts<P> now;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
     s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
     load_keys(i + 2);
-    const float sum = weights_of(a.scale_log2, s_now, w.ref, p);
+    const float sum = weights_of<P>(a.scale_log2, s_now, w.ref, now);
     weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
     interleave<D, P>();
-    settle<D>(a.scale_log2, s_now, w, p, sum);
-    part = parts_of<P>(p);
+    settle<D, P>(a.scale_log2, a.lag, s_now, w, now, sum);
+    part = now;
   };
   const int full_lo = max(first + 1, (own.all_lo - base_pos + kPair - 1) / kPair);
   const int full_hi = min(last - 1, (min(own.all_hi, end) - base_pos) / kPair);
@@ -976,7 +987,7 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
       mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s_now);
     const uint16_t* vs = v_get + stage_of(fills ? i : i - WP);
     bf16x8 vf[D / 32][2];
-    f32x16 p;
+    Parts<P> now;
     if (WP > 1) load_keys(i + WP);
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
@@ -984,11 +995,11 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
       for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
     const f32x16 s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
     if (WP == 1) load_keys(i + 2);
-    const float sum = weights_of(a.scale_log2, s_now, w.ref, p);
+    const float sum = weights_of<P>(a.scale_log2, s_now, w.ref, now);
     weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
     interleave<D, P>();
-    settle<D>(a.scale_log2, s_now, w, p, sum);
-    part = parts_of<P>(p);
+    settle<D, P>(a.scale_log2, a.lag, s_now, w, now, sum);
+    part = now;
     s_now = s_next;
     if ((odd & 2) != 0 && !fills) add_odd(i - WP);
     if (drains) {
@@ -1119,7 +1130,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
     for (int k = 0; k < kSide; ++k) {
       const float to = ml[k].y == 0.f ? top[k] : fmaxf(top[k], ml[k].x);
       const float ref = to == -INFINITY ? 0.f : to;
-      const float f0 = __builtin_amdgcn_exp2f(top[k] - ref), f1 = ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - ref);
+      const float f0 = weight_of(top[k], ref, a.scale_log2), f1 = ml[k].y == 0.f ? 0.f : weight_of(ml[k].x, ref, a.scale_log2);
       top[k] = to;
       acc[k].x = f0 * acc[k].x + f1 * x[k].x;
       acc[k].y = f0 * acc[k].y + f1 * x[k].y;
@@ -1144,7 +1155,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
     const int64_t row = (int64_t)(mg.row0 + token) * a.Hq + g * a.G + (fc - token * a.G);
     const float inv = inverse_of(l[k]);
     store4(static_cast<Out*>(a.out) + row * D + d, make_float4(acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv));
-    if (d == 0 && a.lse) a.lse[row] = lse_of(top[k] == -INFINITY ? 0.f : top[k], l[k]);
+    if (d == 0 && a.lse) a.lse[row] = lse_of(top[k] == -INFINITY ? 0.f : top[k], l[k], a.scale_log2);
   }
 }
 
@@ -1315,6 +1326,7 @@ extern "C" oda_status oda_prompt_attn(const oda_attn_shape* shape, const oda_att
   a.max_items = z.max_items;
   a.max_merges = z.max_merges;
   a.scale_log2 = in->scale * kLog2e;
+  a.lag = std::min(kLag / a.scale_log2, kMaxLag);
   if (out_type == ODA_F32)
     return shape->head_dim == 128 ? launch_attention<128, float>(a, stream) : launch_attention<64, float>(a, stream);
   return shape->head_dim == 128 ? launch_attention<128, uint16_t>(a, stream) : launch_attention<64, uint16_t>(a, stream);

@@ -236,6 +236,28 @@ def test_large_scores_and_values():
         assert (np.abs(lse - rlse) <= 4e-3 + 2.0 ** -22 * np.abs(rlse)).all()
 
 
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 40, 2.0 ** 90])
+@pytest.mark.parametrize("rows,seq", [([3], [200]), ([300], [900])])
+def test_scores_of_any_size(size, rows, seq):
+    """Scores so large that the largest one takes all, whatever its product with the scale rounds to."""
+    t = Prompt(60, 2, 1, 64, rows, seq)
+    q, k = bf16_to_f64(t.q), bf16_to_f64(t.k)
+    q[:] = 0.0
+    q[..., 0] = 1.5
+    k[:] = 0.0
+    g = S.rng(61, 1)
+    for p in range(seq[0]):                 # multiples of an eighth of `size`, one in twenty at the top
+        k[0, t.table[0, p // 16], 0, 0, p % 16, 0] = size * (1.0 if g.random() < 0.05 else g.integers(0, 8) / 8)
+    k[0, t.table[0, 0], 0, 0, 0, 0] = size
+    t.q = (q.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    t.k = (k.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    ref, rlse, mag = t.oracle()
+    for bf16 in (False, True):
+        out, lse = t.run(bf16)
+        t.compare(out, rlse, ref, rlse, mag, bf16)
+        assert (np.abs(lse - rlse) <= LSE_ABS + 2.0 ** -22 * np.abs(rlse)).all()
+
+
 def test_scores_that_grow_and_fall_along_the_history():
     """Every step raises the reference, then none does."""
     for order in (1, -1):
