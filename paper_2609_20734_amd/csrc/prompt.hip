@@ -262,16 +262,18 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     sum += s_cost[w][lane];
     big = fmaxf(big, s_big[w][lane]);
   }
-  // rounds of items of mean cost, the last one's idle places by half; at least the largest item
+  // rounds of items of mean cost, the last one whole where they are alike; at least the largest item
   const float rounds = (float)a.Hkv * (float)n * (1.f / (float)kCus);
   const float mean = sum / (float)max(n, 1);
-  float est = fmaxf(big + kItemCost, mean * 0.5f * (rounds + ceilf(rounds)));
+  const float alike = fminf(1.f, mean / (big + kItemCost));
+  float est = fmaxf(big + kItemCost, mean * (rounds + alike * (ceilf(rounds) - rounds)));
   if (n - n_tiles > a.extra_items) est = INFINITY;
   float best = est;
 #pragma unroll
   for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
   const uint64_t who = __ballot(est == best);
-  const int pick = who ? 63 - __builtin_clzll(who) : 63;
+  // (of equal ones the smallest: a class's cost is above its tiles', which a larger value would split less)
+  const int pick = who ? __builtin_ctzll(who) : 63;
   const float inv_best = __shfl(inv, pick);
   auto splits_of = [&](const Tile& t) {
     const int blocks = t.hi - t.lo;
@@ -491,14 +493,14 @@ constexpr float kMaxLag = 1e37f;     // (scores of a scale that small all weigh 
 template <int P>
 __device__ __forceinline__ float weights_of(float scale_log2, const f32x16& s, float ref, Parts<P>& part) {
   f32x16 p;
-  float t[4] = {0.f, 0.f, 0.f, 0.f};
+  float t[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     p[i] = weight_of(s[i], ref, scale_log2);
-    t[i & 3] += p[i];
+    t[i & 1] += p[i];
   }
   part = parts_of<P>(p);
-  return (t[0] + t[1]) + (t[2] + t[3]);
+  return t[0] + t[1];
 }
 // The sum's check, after all products of earlier pairs: raises the reference where it fails.
 template <int D, int P>
@@ -572,25 +574,6 @@ __device__ __forceinline__ void add_odd_values(const uint16_t* v0, const uint16_
         if (in && (x & 0x7f80u) == 0x7f80u) w.o[n][r] += __uint_as_float(x << 16);
         __builtin_amdgcn_sched_barrier(0);     // one load at a time: no registers for a rare case
       }
-  }
-}
-
-// The order of a full step: beside each product one operand's read, for a product of
-// the other kind, and a share of the weights' vector operations.
-template <int D, int P>
-__device__ __forceinline__ void interleave() {
-  constexpr int kHalf = D / 16;                             // reads of K, of V
-#pragma unroll
-  for (int i = 0; i < kHalf; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // products
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // reads of LDS
-    __builtin_amdgcn_sched_group_barrier(0x002, 32 / kHalf, 0);    // vector operations
-  }
-#pragma unroll
-  for (int i = 0; i < kHalf; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, P, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, 32 / kHalf, 0);
   }
 }
 
@@ -958,11 +941,12 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
+    __builtin_amdgcn_s_setprio(1);     // products before the other wavefront's (sixteen mixed requests, fp32: 387 us against 410)
     s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
     load_keys(i + 2);
     const float sum = weights_of<P>(a.scale_log2, s_now, w.ref, now);
     weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
-    interleave<D, P>();
+    __builtin_amdgcn_s_setprio(0);
     settle<D, P>(a.scale_log2, a.lag, s_now, w, now, sum);
     part = now;
   };
@@ -993,11 +977,12 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
+    __builtin_amdgcn_s_setprio(1);
     const f32x16 s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
     if (WP == 1) load_keys(i + 2);
     const float sum = weights_of<P>(a.scale_log2, s_now, w.ref, now);
     weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
-    interleave<D, P>();
+    __builtin_amdgcn_s_setprio(0);
     settle<D, P>(a.scale_log2, a.lag, s_now, w, now, sum);
     part = now;
     s_now = s_next;
