@@ -102,8 +102,17 @@ constexpr float kWidePartCost = 36.f;  // of more than half a tile's columns
 constexpr float kLeastCost = 16.f;     // shortest range
 constexpr int kClasses = 256;          // cost classes, eight to a factor of two
 
+// Where there is little work, the length of an item counts: there tiles are one
+// wavefront's 32 columns, whose positions all eight wavefronts share, although K and V
+// are then read once for each (four requests of 100 rows behind 100: 20 us against 31;
+// 64 behind 960 of 16 heads 22 : 28, behind 15,900 35 : 50; 256 behind 3,000 of 32 heads
+// 35 : 43.  Beyond the limits: four of 60 behind 8,000 of 32 heads 73 : 65, 128 behind 16,000
+// 67 : 63, 256 behind 16,000 104 : 90).
+constexpr int kNarrowItems = 2 * kCus;     // narrow tiles of all KV heads together
+constexpr float kNarrowWork = 288.f * kCus; // their blocks, all together
+
 struct PlanRequest {
-  int32_t row0, rows, n, tile;        // tile: the request's first
+  int32_t row0, rows, n, tile, narrow_tile;        // tile: the request's first
 };
 
 __device__ __forceinline__ int class_of(float cost) {
@@ -158,7 +167,8 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
   for (int i = tid; i < 2 * kClasses; i += kPlanThreads) s_class[i] = 0;
 
   // requests: row starts kept in [0, R] and ascending whatever the array holds
-  int n_tiles = 0, carry = 0;
+  int n_tiles = 0, n_narrow = 0, carry = 0;
+  float work = 0.f;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int start = 0, end = 0, n = 0;
@@ -180,15 +190,33 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     for (int w = 0; w < wave; ++w) top = max(top, s_max[w]);
     const int row0 = top, rows = max(end - row0, 0);
     for (int w = 0; w < kPlanThreads / 64; ++w) carry = max(carry, s_max[w]);
+    // (narrow tiles are counted up to more than may be)
     const int tiles = (int)(((int64_t)rows * a.G + kTile - 1) / kTile);
+    const int narrow = (int)min(((int64_t)rows * a.G + kCols - 1) / kCols, (int64_t)kNarrowItems + 1);
     int2 total;
-    const int2 at = block_scan(make_int2(tiles, 0), s_wave, total);
+    const int2 at = block_scan(make_int2(tiles, narrow), s_wave, total);
     if (b < a.B) {
       const bool bad = n < 0 || n > a.max_len || (a.causal && n < rows);
-      s_req[b] = PlanRequest{row0, rows, bad ? -1 : n, n_tiles + at.x};
+      s_req[b] = PlanRequest{row0, rows, bad ? -1 : n, n_tiles + at.x, n_narrow + at.y};
+      if (!bad) {
+        const int reach = a.causal && a.window > 0 && a.window < n - rows ? a.window + rows : n;
+        work += (float)narrow * (float)(reach / kBlock + 1);
+      }
     }
     n_tiles += total.x;
+    n_narrow += total.y;
   }
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) work += __shfl_xor(work, s);
+  __syncthreads();
+  if (lane == 0) s_big[wave][0] = work;
+  __syncthreads();
+  work = 0.f;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) work += s_big[w][0];
+  const bool narrow = n_narrow <= kNarrowItems / a.Hkv && work * (float)a.Hkv <= kNarrowWork;
+  const int width = narrow ? kCols : kTile;
+  if (narrow) n_tiles = n_narrow;
   __syncthreads();
 
   // a tile: its request, columns and blocks
@@ -199,14 +227,14 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     int lo = 0, hi = a.B;            // the last request whose first tile is at or before t (one with rows)
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_req[mid].tile <= t) lo = mid;
+      if ((narrow ? s_req[mid].narrow_tile : s_req[mid].tile) <= t) lo = mid;
       else hi = mid;
     }
     const PlanRequest q = s_req[lo];
     Tile r;
     r.b = lo;
-    r.col0 = (t - q.tile) * kTile;
-    r.ncols = (int)min((int64_t)kTile, (int64_t)q.rows * a.G - r.col0);
+    r.col0 = (t - (narrow ? q.narrow_tile : q.tile)) * width;
+    r.ncols = (int)min((int64_t)width, (int64_t)q.rows * a.G - r.col0);
     r.lo = r.hi = 0;
     if (q.n < 0) return r;
     const int first = q.n - q.rows + r.col0 / a.G, last = q.n - q.rows + (r.col0 + r.ncols - 1) / a.G;
@@ -1169,8 +1197,9 @@ oda_status sizes_of(const oda_attn_shape* s, const oda_prompt_rows* r, Sizes* z)
   if ((int64_t)r->num_rows * s->num_q_heads > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "num_rows * num_q_heads too large");
   z->extra_items = (int)oda::ceil_div(2 * kCus, s->num_kv_heads);
   const int64_t tiles = cols / kTile + s->batch;
-  z->max_items = (int)(tiles + z->extra_items);
-  z->max_merges = (int)std::min<int64_t>(tiles, z->extra_items);
+  // (narrow tiles are no more than kNarrowItems / Hkv, which is no more than the extra items)
+  z->max_items = (int)(std::max<int64_t>(tiles, z->extra_items) + z->extra_items);
+  z->max_merges = (int)std::min<int64_t>(cols / kCols + s->batch, z->extra_items);
   // a split tile has one item more than the extra ones that it takes
   z->part_cols = z->extra_items * std::min<int64_t>(kTile, cols) + std::min<int64_t>(cols, (int64_t)z->extra_items * kTile);
   z->plan_bytes = (size_t)oda::round_up(
