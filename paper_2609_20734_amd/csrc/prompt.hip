@@ -105,7 +105,7 @@ constexpr int kClasses = 256;          // cost classes, eight to a factor of two
 // Where there is little work, the length of an item counts: there tiles are one
 // wavefront's 32 columns, whose positions all eight wavefronts share, although K and V
 // are then read once for each (four requests of 100 rows behind 100: 20 us against 31;
-// 64 behind 960 of 16 heads 22 : 28, behind 15,900 35 : 50; 256 behind 3,000 of 32 heads
+// 64 behind 3,900 of 16 heads 27 : 34, behind 15,900 35 : 50; 256 behind 3,000 of 32 heads
 // 35 : 43.  Beyond the limits: four of 60 behind 8,000 of 32 heads 73 : 65, 128 behind 16,000
 // 67 : 63, 256 behind 16,000 104 : 90).
 constexpr int kNarrowItems = 2 * kCus;     // narrow tiles of all KV heads together
@@ -413,6 +413,7 @@ struct PromptArgs {
   int64_t part_cols;
   int32_t B, R, Hq, Hkv, G, MB, max_len;
   int32_t max_items, max_merges;
+  int32_t merge_parts;       // of kCols columns that a tile may have
   float scale_log2;          // of a score, for exponents of 2
   float lag;                 // kLag in score units
 };
@@ -1113,7 +1114,7 @@ template <int D, typename Out>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
   constexpr int kSide = kCols * (D / 4) / 256;       // columns of a thread
   const PlanHeader h = *reinterpret_cast<const PlanHeader*>(a.plan);
-  const int parts = kTile / kCols;
+  const int parts = a.merge_parts;
   const int part = blockIdx.x % parts, u = blockIdx.x / parts;
   const int i = u / a.Hkv, g = u - i * a.Hkv;
   const Merge mg = reinterpret_cast<const Merge*>(a.plan + merges_at(a.max_items))[i];
@@ -1237,7 +1238,7 @@ void raise_lds_limit(const void* kernel, std::atomic<uint64_t>* done, int bytes)
 template <int D, typename Out>
 oda_status launch_attention(const PromptArgs& a, hipStream_t stream) {
   const int64_t items = (int64_t)a.max_items * a.Hkv;
-  const int64_t merges = (int64_t)a.max_merges * a.Hkv * (kTile / kCols);
+  const int64_t merges = (int64_t)a.max_merges * a.Hkv * a.merge_parts;
   if (items > INT_MAX || merges > INT_MAX) return oda::fail(ODA_ERR_SHAPE, "grid too large");
   const int lds = lds_bytes(D);
   static std::atomic<uint64_t> raised{0};
@@ -1339,6 +1340,7 @@ extern "C" oda_status oda_prompt_attn(const oda_attn_shape* shape, const oda_att
   a.max_len = shape->max_seq_len;
   a.max_items = z.max_items;
   a.max_merges = z.max_merges;
+  a.merge_parts = (int)oda::ceil_div(std::min<int64_t>(kTile, (int64_t)a.R * a.G), kCols);
   a.scale_log2 = in->scale * kLog2e;
   a.lag = std::min(kLag / a.scale_log2, kMaxLag);
   if (out_type == ODA_F32)
