@@ -31,7 +31,7 @@ constexpr int kMaxSplits = 64;                // of a row: one per lane where th
 constexpr int kTickets = 1024;                // rows that may be split
 constexpr int kGroups = 1024;                 // workgroups that split rows make at most
 constexpr int kLeastSplit = kWaves * kBatch / 2;
-constexpr int kGrain = kWaves * 256;           // logits of a wavefront's load, of all of them
+constexpr int kRun = 64;                      // runs of wavefronts are multiples of it
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = 1e30f;                 // stands for an infinite distance (its weight is 0)
 
@@ -51,6 +51,7 @@ struct LogprobArgs {
   uint64_t* parts;         // [slot][splits][2 + top]: (m, S), (T, ahead), then (logit, token)
   int64_t stride;
   int32_t R, V, top, splits, chunk;
+  uint32_t top_inv;        // i * top_inv >> 16 is i / top for i < kMaxSplits * kMaxTop
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -179,11 +180,73 @@ struct Scratch {
   float m[kWaves], s[kWaves], t[kWaves];
   int ahead[kWaves];
   float deep[kWaves];                          // a place of each wavefront's, below
-  float z[kMaxSplits * kMaxTop];               // lists to merge
+  float z[kMaxSplits * kMaxTop];               // lists to join: [list][place]
   int id[kMaxSplits * kMaxTop];
   float pz[kWaves][64];                        // candidates
   int pi[kWaves][64];
+  uint2 cand[kMaxSplits * kMaxTop];            // (logit, token) of a join's candidates
+  float best_z[kMaxTop];                       // the joined list
+  int best_id[kMaxTop];
+  int n, last;
 };
+
+// Sum over the lanes 0 .. 7 of a wavefront, in each of them.
+__device__ __forceinline__ int sum8(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false);     // lane ^ 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, false);     // lane ^ 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false);    // 7 - lane of the eight
+  return x;
+}
+// Before a join (and a barrier): the joined list empty, no candidates.
+__device__ __forceinline__ void clear_join(Scratch& sm) {
+  if (threadIdx.x < kMaxTop) {
+    sm.best_z[threadIdx.x] = -INFINITY;
+    sm.best_id[threadIdx.x] = -1;
+  }
+  if (threadIdx.x == 0) sm.n = 0;
+}
+// Joins sm.z / sm.id, `lists` of k places in order, a list's tokens before the later lists',
+// by the whole workgroup.  Where the c-th places of ceil(k / c) lists reach a bound, k
+// logits do: those that reach it are placed by counting the ones ahead.  (With c about
+// 2 k / lists half of the lists decide; where fewer have that many places, a larger one.)
+__device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  float bound = -INFINITY;
+  for (int c = min(k, (2 * k + lists - 1) / lists);; c = min(k, 2 * c)) {
+    bound = kth_bound(lane < lists ? sm.z[lane * k + c - 1] : -INFINITY, (k + c - 1) / c);
+    if (bound > -INFINITY || c == k) break;
+  }
+  for (int i0 = 0; i0 < lists * k; i0 += kThreads) {
+    const int i = i0 + tid;
+    const float y = i < lists * k ? sm.z[i] : -INFINITY;
+    const bool in = y >= bound && y > -INFINITY;
+    const uint64_t mask = __ballot(in);
+    if (mask == 0) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sm.n, __builtin_popcountll(mask));
+    at = uniform(at) + lanes_before(mask);
+    if (in) sm.cand[at] = make_uint2(__float_as_uint(y), (uint32_t)sm.id[i]);
+  }
+  __syncthreads();
+  const int n = sm.n;
+  for (int i0 = 0; i0 < n; i0 += kThreads / 2) {              // two lanes a candidate
+    const int i = i0 + (tid >> 1);
+    const uint2 own = sm.cand[min(i, n - 1)];
+    const float y = __uint_as_float(own.x);
+    int ahead = 0;
+#pragma unroll 8
+    for (int j = tid & 1; j < n; j += 2) {
+      const uint2 x = sm.cand[j];
+      ahead += (__uint_as_float(x.x) > y) | ((__uint_as_float(x.x) == y) & (x.y < own.y)) ? 1 : 0;
+    }
+    ahead += __builtin_amdgcn_update_dpp(0, ahead, 0xb1, 0xf, 0xf, false);      // the other lane's
+    if ((tid & 1) == 0 && i < n && ahead < k) {
+      sm.best_z[ahead] = y;
+      sm.best_id[ahead] = (int)own.y;
+    }
+  }
+  __syncthreads();
+}
 
 // Outputs of a row: lane i < k of the wavefront holds place i.
 __device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat x, int ahead, float zt, bool known, Best best) {
@@ -214,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
 
   // the wavefront's logits: one run of the split's, in ascending order
   const int begin = min(a.V, split * a.chunk), end = min(a.V, begin + a.chunk);
-  const int run = ((end - begin + kWaves - 1) / kWaves + 255) & ~255;
+  const int run = ((end - begin + kWaves - 1) / kWaves + kRun - 1) & ~(kRun - 1);
   const int from = min(end, begin + wave * run), to = min(end, from + run);
   float z[4 * kLoads], next[4 * kLoads];
   auto load = [&](int v0, float (&x)[4 * kLoads]) {
@@ -341,93 +404,63 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     sm.z[wave * a.top + lane] = best.z;
     sm.id[wave * a.top + lane] = best.id;
   }
+  clear_join(sm);
   __syncthreads();
-  if (wave != 0) return;
 
   // The workgroup's wavefronts joined, then, by the last of a row's workgroups, its splits.
+  if (a.top > 0) join_lists(sm, kWaves, a.top);
   x = lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f};
   ahead = lane < kWaves ? sm.ahead[lane] : 0;
-  const int words = 2 + a.top;
-  const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
-  bool whole = a.splits == 1;       // the lists are all of the row's
-  for (int lists = kWaves;; lists = a.splits) {
-    x = wave_join(x);
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
-    // Lists of k places in LDS, a list's tokens before the later lists'.  Where the first c
-    // of each reach a bound in ceil(k / c) lists, k logits do: those that reach it are put
-    // in order; where these are too many (equal logits), k rounds over the lists' heads.
-    if (a.top > 0) {
-      const bool mine = lane < lists;
-      const int c = (a.top + lists - 1) / lists;
-      const float bound = kth_bound(mine ? sm.z[lane * a.top + c - 1] : -INFINITY, (a.top + c - 1) / c);
-      int n = 0;
-      for (int j = 0; j < a.top && n <= 64; ++j) {
-        const float y = mine ? sm.z[lane * a.top + j] : -INFINITY;
-        const bool in = y >= bound && y > -INFINITY;
-        const uint64_t mask = __ballot(in);
-        if (mask == 0) break;
-        const int at = n + lanes_before(mask);
-        if (in && at < 64) {
-          sm.pz[0][at] = y;
-          sm.pi[0][at] = sm.id[lane * a.top + j];
-        }
-        n += __builtin_popcountll(mask);
-      }
-      oda::wave_lds_fence();
-      best = Best{-INFINITY, -1};
-      if (n <= 64) {
-        best = in_order(sm.pz[0][lane], sm.pi[0][lane], n);
-      } else {
-        int at = 0;
-        for (int i = 0; i < a.top; ++i) {
-          const float head = mine && at < a.top ? sm.z[lane * a.top + at] : -INFINITY;
-          const float most = wave_max(head);
-          const int l = __builtin_ctzll(__ballot(head == most));
-          if (lane == l && most > -INFINITY) {
-            sm.pi[0][i] = sm.id[lane * a.top + at];
-            ++at;
-          }
-          if (lane == i) best.z = most;
-        }
-        oda::wave_lds_fence();
-        if (best.z > -INFINITY) best.id = sm.pi[0][lane];
-      }
+  if (a.splits > 1) {
+    const int words = 2 + a.top;
+    const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
+    if (wave == 0) {
+      x = wave_join(x);
+      ahead = sum8(ahead);
+      uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
+      if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
+      if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
+      if (lane < a.top) publish(part + 2 + lane, pack(sm.best_z[lane], (uint32_t)sm.best_id[lane]));
+      __builtin_amdgcn_s_waitcnt(0);
+      __builtin_amdgcn_wave_barrier();
+      if (lane == 0)
+        sm.last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
+                          (uint32_t)(a.splits - 1)
+                      ? 1
+                      : 0;
     }
-    if (whole) break;
-    whole = true;
-    uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
-    if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
-    if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
-    if (lane < a.top) publish(part + 2 + lane, pack(best.z, (uint32_t)best.id));
-    __builtin_amdgcn_s_waitcnt(0);
-    __builtin_amdgcn_wave_barrier();
-    int last = 0;
-    if (lane == 0)
-      last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
-                     (uint32_t)(a.splits - 1)
-                 ? 1
-                 : 0;
-    if (uniform(last) == 0) return;
-    // (a lane a split; a trip to memory for sixteen places of all)
-    constexpr int kTrip = 16;
+    __syncthreads();
+    if (sm.last == 0) return;
     const uint64_t* list = parts + (int64_t)min(lane, a.splits - 1) * words;
     const uint64_t p0 = published(list), p1 = published(list + 1);
-    for (int j0 = 0; j0 < a.top; j0 += kTrip) {
-      uint64_t p[kTrip];
+    if (a.top > 0) {
+      constexpr int kEach = kMaxSplits * kMaxTop / kThreads;
+      const int all = a.splits * a.top;
+      uint64_t p[kEach];
 #pragma unroll
-      for (int j = 0; j < kTrip; ++j) p[j] = published(list + 2 + min(j0 + j, a.top - 1));
-#pragma unroll
-      for (int j = 0; j < kTrip; ++j) {
-        if (lane >= a.splits || j0 + j >= a.top) continue;
-        sm.z[lane * a.top + j0 + j] = first_of(p[j]);
-        sm.id[lane * a.top + j0 + j] = (int)(uint32_t)p[j];
+      for (int j = 0; j < kEach; ++j) {
+        const int i = min(j * kThreads + tid, all - 1), l = (int)((uint32_t)i * a.top_inv >> 16);
+        p[j] = published(parts + (int64_t)l * words + 2 + (i - l * a.top));
       }
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int i = j * kThreads + tid;
+        if (i >= all) continue;
+        sm.z[i] = first_of(p[j]);
+        sm.id[i] = (int)(uint32_t)p[j];
+      }
+      clear_join(sm);
+      __syncthreads();
+      join_lists(sm, a.splits, a.top);
     }
     x = lane < a.splits ? Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)} : Stat{-INFINITY, 0.f, 0.f};
     ahead = lane < a.splits ? (int)(uint32_t)p1 : 0;
-    oda::wave_lds_fence();
   }
+  if (wave != 0) return;
+  x = wave_join(x);
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
+  best = lane < a.top ? Best{sm.best_z[lane], sm.best_id[lane]} : Best{-INFINITY, -1};
   write_row(a, row, x, uniform(ahead), zt, known, best);
 }
 
@@ -436,7 +469,7 @@ void split_row(int64_t rows, int64_t vocab, int* splits, int* chunk) {
   int64_t n = 1;
   if (rows <= kTickets)
     n = std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, kGroups / rows, vocab / kLeastSplit}));
-  *chunk = (int)oda::round_up(oda::ceil_div(vocab, n), n > 1 ? kGrain : 4);
+  *chunk = (int)oda::round_up(oda::ceil_div(vocab, n), n > 1 ? kWaves * kRun : 4);
   *splits = (int)oda::ceil_div(vocab, *chunk);
 }
 
@@ -498,6 +531,7 @@ extern "C" oda_status oda_token_logprobs(const oda_logprob_desc* desc, int32_t r
   a.R = rows;
   a.V = desc->vocab;
   a.top = desc->top;
+  a.top_inv = (uint32_t)oda::ceil_div(65536, std::max(a.top, 1));
   (void)hipGetLastError();
   hipLaunchKernelGGL(logprob_kernel, dim3((unsigned)rows, (unsigned)a.splits), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();

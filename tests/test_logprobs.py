@@ -105,6 +105,21 @@ def test_ties_go_to_the_lowest_index():
     t.check()
 
 
+def test_long_rows_with_few_tokens_left():
+    """Masks that leave logits in a few parts of a row split over many workgroups, and ties across all of them."""
+    t = Scores(16, 7, 300_001, 32)
+    full = t.z.copy()
+    for r, keep in enumerate(([0, 150_000, 300_000], range(70_000, 70_040), range(11, 300_001, 3_001), range(40_000, 160_000, 4_000))):
+        t.z[r] = -np.inf
+        t.z[r, list(keep)] = full[r, list(keep)]
+    t.z[3, np.isfinite(t.z[3])] = 2.0              # thirty equal ones
+    t.z[4] = -1.5                                  # all equal
+    t.z[5] = np.linspace(5, -5, 300_001, dtype=np.float32)
+    t.z[6] = np.round(full[6])                     # a dozen values
+    t.t[:] = [150_000, 70_001, 12, 44_000, 299_999, 17, 5]
+    t.check()
+
+
 def test_ascending_rows_replace_every_place():
     t = Scores(8, 3, 9000, 32)
     t.z[:] = np.linspace(-5, 5, 9000, dtype=np.float32)
