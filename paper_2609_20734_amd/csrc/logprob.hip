@@ -30,7 +30,7 @@ constexpr int kMaxTop = ODA_MAX_TOP;
 constexpr int kMaxSplits = 64;                // of a row: one per lane where they are joined
 constexpr int kTickets = 1024;                // rows that may be split
 constexpr int kGroups = 1024;                 // workgroups that split rows make at most
-constexpr int kLeastSplit = kWaves * kBatch / 2;
+constexpr int kLeastSplit = kWaves * kBatch / 2;  // (half and twice of it: 15.9 and 15.6 us against 14.4, below)
 constexpr int kRun = 64;                      // runs of wavefronts are multiples of it
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = 1e30f;                 // stands for an infinite distance (its weight is 0)

@@ -123,17 +123,34 @@ __device__ __forceinline__ float class_cost(int c) { return 1.001f * __builtin_a
 // Ranges of a tile of `blocks` blocks where an item may hold `cap` of them, even.
 __device__ __forceinline__ int range_blocks(int blocks, int splits) { return ((blocks + splits - 1) / splits + 1) & ~1; }
 
+// Running sum, and running largest of values >= 0, over the wavefront's lanes: row shifts
+// by 1, 2, 4, 8, then each row's last lane into the next row, then the lower half's into
+// the upper (the lanes that nothing is shifted into get 0).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int shifted(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x += shifted<0x111, 0xf>(x);
+  x += shifted<0x112, 0xf>(x);
+  x += shifted<0x114, 0xf>(x);
+  x += shifted<0x118, 0xf>(x);
+  x += shifted<0x142, 0xa>(x);
+  x += shifted<0x143, 0xc>(x);
+  return x;
+}
+__device__ __forceinline__ int wave_scan_max(int x) {
+  x = max(x, shifted<0x111, 0xf>(x));
+  x = max(x, shifted<0x112, 0xf>(x));
+  x = max(x, shifted<0x114, 0xf>(x));
+  x = max(x, shifted<0x118, 0xf>(x));
+  x = max(x, shifted<0x142, 0xa>(x));
+  x = max(x, shifted<0x143, 0xc>(x));
+  return x;
+}
 __device__ __forceinline__ int2 block_scan(int2 x, int2* s_wave, int2& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int2 v = x;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int a = __shfl_up(v.x, s), b = __shfl_up(v.y, s);
-    if (lane >= s) {
-      v.x += a;
-      v.y += b;
-    }
-  }
+  const int2 v = make_int2(wave_scan(x.x), wave_scan(x.y));
   __syncthreads();       // the sums of the call before have been read
   if (lane == 63) s_wave[wave] = v;
   __syncthreads();
@@ -178,12 +195,7 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
       n = a.seq_lens[b];
     }
     // running largest of all starts up to b, and of the ends up to b
-    int top = max(start, carry);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int y = __shfl_up(top, s);
-      if (lane >= s) top = max(top, y);
-    }
+    int top = wave_scan_max(max(start, carry));
     __syncthreads();
     if (lane == 63) s_max[wave] = top;
     __syncthreads();
@@ -242,12 +254,13 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     r.lo = a.causal && a.window > 0 ? max(0, first - a.window + 1) / kBlock : 0;
     return r;
   };
+  const Tile own = tid < n_tiles ? tile_at(tid) : Tile{};
   auto is_wide = [&](const Tile& t) { return t.ncols > kTile / 2; };
   auto cost_of = [&](const Tile& t) { return (float)(t.hi - t.lo) * (is_wide(t) ? kWideCost : 1.f); };
 
   int most = 0;
   for (int t = tid; t < n_tiles; t += kPlanThreads) {
-    const Tile r = tile_at(t);
+    const Tile r = t == tid ? own : tile_at(t);
     const int c = class_of(cost_of(r));
     atomicAdd(&s_class[(is_wide(r) ? kClasses : 0) + c], 1);
     most = max(most, c);
@@ -265,10 +278,12 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
   const float inv = 1.f / cap;
   int n = 0;
   float sum = 0.f, big = 0.f;
-  for (int c0 = 64 * wave; c0 < 2 * kClasses; c0 += kPlanThreads) {
+  // (classes that are there lie side by side: the wavefronts take them in turn)
+  for (int c0 = 0; c0 < 2 * kClasses; c0 += 64) {
+    if ((c0 & (kClasses - 1)) > most) continue;
     const int here = s_class[c0 + lane];
     const float part = c0 >= kClasses ? kWidePartCost : kPartCost;
-    for (uint64_t todo = __ballot(here != 0); todo != 0; todo &= todo - 1) {
+    for (uint64_t todo = __ballot(here != 0 && (lane & (kPlanThreads / 64 - 1)) == wave); todo != 0; todo &= todo - 1) {
       const int i = __builtin_ctzll(todo);
       const int count = __builtin_amdgcn_readlane(here, i);
       const float cost = class_cost((c0 + i) & (kClasses - 1));
@@ -316,7 +331,7 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
   for (int i = tid; i < kClasses; i += kPlanThreads) s_class[i] = 0;
   __syncthreads();
   for (int t = tid; t < n_tiles; t += kPlanThreads) {
-    const Tile r = tile_at(t);
+    const Tile r = t == tid ? own : tile_at(t);
     const int splits = splits_of(r);
     atomicAdd(&s_class[class_of(cost_of(r) / (float)splits)], splits);
   }
@@ -348,7 +363,7 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     Tile r{};
     int splits = 0;
     if (t < n_tiles) {
-      r = tile_at(t);
+      r = t == tid ? own : tile_at(t);
       splits = splits_of(r);
     }
     const bool merged = splits > 1;
