@@ -8,7 +8,11 @@
 // token is counted and the first k tokens are kept on the way.  A row is split over
 // workgroups where rows are few; the last of a row's workgroups joins them.
 //
-// Bound by HBM: four bytes a logit, about a dozen vector instructions.
+// Many rows are bound by HBM and, close behind, the vector operations (four bytes and
+// about a dozen instructions a logit): 1,024 rows of 50,257 with five alternatives in
+// 49.5 us, 4.2 TB/s.  Few rows are bound by one chain: four of 151,936 with twenty take
+// 14.4 us, of which a wavefront's logits and first places take 5, the joins 4, the trips
+// between workgroups 3, start and end 2 (without alternatives 6.8).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
