@@ -401,6 +401,8 @@ extern "C" oda_status oda_append_qkv(const oda_attn_shape* shape, const oda_prom
   a.slots = (int)(oda::ceil_div(a.Hq, per) + 2 * oda::ceil_div(a.Hkv, per));
   // a request's m rows touch at most m / 16 + 2 blocks, and at most m
   const int64_t tiles = std::min<int64_t>(a.R, (int64_t)a.R / kBlock + 2 * (int64_t)a.B);
+  // heads shared out while there are fewer than 512 workgroups (one workgroup a block: 2,048
+  // rows 21.8 us against 18.1, eight 7.4 against 5.2; 256 or 1,024 within 2%)
   const int64_t chunks = std::min<int64_t>(oda::ceil_div(a.slots, kWaves), std::max<int64_t>(1, oda::ceil_div(512, tiles)));
   a.chunk = (int)oda::ceil_div(a.slots, chunks);
   const dim3 grid((unsigned)tiles, (unsigned)oda::ceil_div(a.slots, a.chunk));

@@ -746,10 +746,9 @@ __device__ __forceinline__ Target<Out> target_of(const PromptArgs& a, const Item
   return t;
 }
 
-// Joins position ranges (wavefront = range * WC + column tile) and writes.
-template <int D, int WC, typename Out>
+// Joins the wavefronts' position ranges and writes.
+template <int D, typename Out>
 __device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g, Columns<D>& w, char* smem) {
-  constexpr int WP = kWaves / WC;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   float* sm_o = reinterpret_cast<float*>(smem);                      // [waves][32][D + 4]
   float* sm_c = reinterpret_cast<float*>(smem + data_bytes(D));      // [waves][32]
@@ -767,18 +766,18 @@ __device__ __forceinline__ void join(const PromptArgs& a, const Item& it, int g,
       *reinterpret_cast<float4*>(dst + 32 * n + 8 * i) =
           make_float4(w.o[n][4 * i], w.o[n][4 * i + 1], w.o[n][4 * i + 2], w.o[n][4 * i + 3]);
   __syncthreads();
-  for (int e = threadIdx.x; e < WC * kCols * (D / 4); e += kThreads) {
+  for (int e = threadIdx.x; e < kCols * (D / 4); e += kThreads) {
     const int d = e % (D / 4) * 4, col = e / (D / 4);
     if (col >= it.ncols) break;
     float top = -INFINITY;
 #pragma unroll
-    for (int p = 0; p < WP; ++p) top = fmaxf(top, sm_c[p * WC * kCols + col]);
+    for (int p = 0; p < kWaves; ++p) top = fmaxf(top, sm_c[p * kCols + col]);
     const float ref = top == -INFINITY ? 0.f : top;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
-    for (int p = 0; p < WP; ++p) {
-      const int from = p * WC * kCols + col;
+    for (int p = 0; p < kWaves; ++p) {
+      const int from = p * kCols + col;
       const float s = weight_of(sm_c[from], ref, a.scale_log2);
       const float4 x = *reinterpret_cast<const float4*>(sm_o + from * o_stride(D) + d);
       acc.x += s * x.x;
@@ -885,32 +884,31 @@ __device__ __forceinline__ void run_narrow(const PromptArgs& a, const PlanHeader
     }
   }
   w.sum += __shfl_xor(w.sum, 32);
-  join<D, 1, Out>(a, it, g, w, smem);
+  join<D, Out>(a, it, g, w, smem);
 }
 
-// More column tiles: K and V are staged through LDS, four blocks a stage, a wavefront
-// bringing one of them.  Up to 128 columns two position ranges share a stage's pairs;
-// more: every wavefront goes through all pairs with its 32 columns.
+// More columns: K and V are staged through LDS, four blocks a stage, a wavefront
+// bringing one of them, and every wavefront that has columns goes through all pairs with
+// its 32.  (Two position ranges where there are up to 128 columns: 64 requests of 64 columns
+// behind 2,000 120 us against 116.)
 //
 // While the weights of pair i are formed (vector operations), the matrix cores form the
 // scores of the wavefront's next pair and add the products of the one before: round st
 // reads K of stages st and st + 1 and V of st - 1 and st, one barrier a round.  K of
 // st + 3 and V of st + 2 are asked for in round st, so that a load has two rounds.
-template <int D, int WC, typename Out>
+template <int D, typename Out>
 __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& head, const Item& it, int g, char* smem) {
   constexpr int P = kPartsOf<Out>;
-  constexpr int WP = kWaves / WC;                    // 1 or 2
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int h = lane >> 5, m = lane & 31;
-  const int wc = wave & (WC - 1), wp = wave / WC;
   const int blocks = it.blk_hi - it.blk_lo;
   const int stages = (blocks + kStageBlocks - 1) / kStageBlocks;
   const int32_t* table = a.block_table + (int64_t)it.request * a.MB + it.blk_lo;
   int entry = lane < blocks ? table[lane] : 0;       // 64 blocks, sixteen stages
   Columns<D> w;
   bf16x8 qf[D / 16];
-  load_columns<D>(a, head, it, g, wc * kCols, w, qf);
-  const Reach own = reach_of(a, head, it, wc * kCols, kCols), all = reach_of(a, head, it, 0, it.ncols);
+  load_columns<D>(a, head, it, g, wave * kCols, w, qf);
+  const Reach own = reach_of(a, head, it, wave * kCols, kCols), all = reach_of(a, head, it, 0, it.ncols);
   const int base_pos = it.blk_lo * kBlock, end = it.blk_hi * kBlock;
   // the column tile's pairs
   const int own_end = min(own.any_hi, end) - base_pos;
@@ -1011,35 +1009,34 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
   // taken out of its stage (bit 0) and of that of the pair before (bit 1).
   auto step = [&](int i, int bad, int odd, f32x16& s_now) {
     if (i < first || i >= last) return;
-    const bool fills = i - WP < first, drains = i + WP >= last;
+    const bool fills = i - 1 < first, drains = i + 1 >= last;
     if (fills) {
       const uint16_t* ks = k_get + stage_of(i);
       s_now = score_pair<D>(qf, [&](int kk) { return load16(ks + kk * 2 * kBlock * 8); });
-      if (WP == 1) load_keys(i + 1);
+      load_keys(i + 1);
 #pragma unroll
       for (int q = 0; q < P; ++q) part.x[q][0] = part.x[q][1] = bf16x8{};
     }
     const int pos = base_pos + i * kPair;
     if (bad != 0 || pos < own.all_lo || pos + kPair > min(own.all_hi, end))
       mask_scores(pos + 8 * h, w.lo, min(w.hi, end), bad, s_now);
-    const uint16_t* vs = v_get + stage_of(fills ? i : i - WP);
+    const uint16_t* vs = v_get + stage_of(fills ? i : i - 1);
     bf16x8 vf[D / 32][2];
     Parts<P> now;
-    if (WP > 1) load_keys(i + WP);
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
       for (int b = 0; b < 2; ++b) vf[n][b] = load16(vs + b * block_elems(D) + n * 32 * kBlock);
     __builtin_amdgcn_s_setprio(1);
     const f32x16 s_next = score_pair<D>(qf, [&](int kk) { return kf[kk]; });
-    if (WP == 1) load_keys(i + 2);
+    load_keys(i + 2);
     const float sum = weights_of<P>(a.scale_log2, s_now, w.ref, now);
     weigh_pair<D, P>(part, w, [&](int n, int b) { return vf[n][b]; });
     __builtin_amdgcn_s_setprio(0);
     settle<D, P>(a.scale_log2, a.lag, s_now, w, now, sum);
     part = now;
     s_now = s_next;
-    if ((odd & 2) != 0 && !fills) add_odd(i - WP);
+    if ((odd & 2) != 0 && !fills) add_odd(i - 1);
     if (drains) {
       vs = v_get + stage_of(i);
       weigh_pair<D, P>(part, w, [&](int n, int b) { return load16(vs + b * block_elems(D) + n * 32 * kBlock); });
@@ -1063,7 +1060,7 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
         const int* f = sm_odd + (st & (kStages - 1)) * kStageBlocks;
         odd |= uniform(f[0] | f[1] | f[2] | f[3]) != 0 ? 1 : 0;
       }
-      return uniform(WP == 1 && bad == 0 && odd == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi ? 1 : 0) != 0;
+      return uniform(bad == 0 && odd == 0 && 2 * st >= full_lo && 2 * st + 1 < full_hi ? 1 : 0) != 0;
     };
     auto end_round = [&](int st) {     // what the round asked for may still be on its way
       wait_loads<D>(st + lead < stages);
@@ -1082,20 +1079,14 @@ __device__ __forceinline__ void run_wide(const PromptArgs& a, const PlanHeader& 
       }
       while (!full && st < stages) {
 #pragma unroll 1
-        for (int e = WP == 1 ? 0 : wp; e < (WP == 1 ? 2 : wp + 1); ++e)
-          step(2 * st + e, (bad >> (2 * e)) & 3, WP == 1 && e == 1 ? odd << 1 | (odd & 1) : odd, s);
+        for (int e = 0; e < 2; ++e) step(2 * st + e, (bad >> (2 * e)) & 3, e == 1 ? odd << 1 | (odd & 1) : odd, s);
         end_round(st);
         full = begin_round(++st);
       }
     }
   }
   w.sum += __shfl_xor(w.sum, 32);
-  if (WP > 1) {
-    __syncthreads();
-    join<D, WC, Out>(a, it, g, w, smem);
-  } else {
-    write_columns<D, Out>(a, it, g, wc * kCols, w);
-  }
+  write_columns<D, Out>(a, it, g, wave * kCols, w);
 }
 
 __device__ __forceinline__ void put_nan(float* p) { *p = __builtin_nanf(""); }
@@ -1125,10 +1116,8 @@ void prompt_attn_kernel(PromptArgs a) {
     }
     return;
   }
-  const int tiles = (it.ncols + kCols - 1) / kCols;
-  if (tiles == 1) run_narrow<D, Out>(a, h, it, g, smem);
-  else if (tiles <= kWaves / 2) run_wide<D, kWaves / 2, Out>(a, h, it, g, smem);
-  else run_wide<D, kWaves, Out>(a, h, it, g, smem);
+  if (it.ncols <= kCols) run_narrow<D, Out>(a, h, it, g, smem);
+  else run_wide<D, Out>(a, h, it, g, smem);
 }
 
 // One workgroup per (split tile, KV head, kCols columns): the ranges in order, two at a
