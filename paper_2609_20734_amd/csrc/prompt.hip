@@ -685,25 +685,26 @@ static_assert(2 * kStageBlocks == kWaves, "a wavefront brings one block of K or 
 // (In assembly, as the compiler would wait for all of them before any read of LDS.  No
 // registers are written; the address is read when the load is issued; the caller waits
 // with wait_loads and a barrier before the block is read.)
+constexpr int kLoadBytes = 64 * 16;
 template <int D>
 __device__ __forceinline__ void load_to_lds(const uint16_t* src, uint32_t dst) {
   if constexpr (D == 128)
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
         "global_load_lds_dwordx4 %0, off\n\t"
-        "global_load_lds_dwordx4 %0, off offset:1024\n\t"
-        "global_load_lds_dwordx4 %0, off offset:2048\n\t"
-        "global_load_lds_dwordx4 %0, off offset:3072"
+        "global_load_lds_dwordx4 %0, off offset:%2\n\t"
+        "global_load_lds_dwordx4 %0, off offset:2*%2\n\t"
+        "global_load_lds_dwordx4 %0, off offset:3*%2"
         :
-        : "v"(src), "s"(dst)
+        : "v"(src), "s"(dst), "n"(kLoadBytes)
         : "memory", "m0");
   else
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
         "global_load_lds_dwordx4 %0, off\n\t"
-        "global_load_lds_dwordx4 %0, off offset:1024"
+        "global_load_lds_dwordx4 %0, off offset:%2"
         :
-        : "v"(src), "s"(dst)
+        : "v"(src), "s"(dst), "n"(kLoadBytes)
         : "memory", "m0");
 }
 // Waits for all of this wavefront's loads but one block's (the one issued last), or all.
