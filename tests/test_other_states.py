@@ -144,3 +144,44 @@ def test_a_captured_step_with_other_rows_and_states():
         graph.replay()
         torch.cuda.synchronize()
         t.check(x, False, tokens)
+
+
+def test_two_graphs_share_their_workspaces():
+    """Two captured steps of other sizes with one workspace each for attention and scores, replayed in turn."""
+    t = States(33, [2000, 900, 40], 8, 2, 64, V=40_000)
+    t.encode()
+    P, side = t.P, torch.cuda.Stream()
+    ws = lws = None
+    steps = []
+    with torch.cuda.stream(side):
+        for rows in ([30, 1, 2], [1, 1, 1]):
+            cap = sum(rows)
+            t.step(rows, False, cap)
+            ws = ws if ws is not None else torch.zeros(P.prompt_workspace_size(t.shape, P.prompt_rows(cap, t.dstart)),
+                                                       dtype=torch.uint8, device="cuda")
+            desc = P.logprob_desc(t.V, 3, t.z, t.tok)
+            lws = lws if lws is not None else torch.zeros(P.logprob_workspace_size(desc, cap), dtype=torch.uint8, device="cuda")
+            top = torch.zeros(cap, 3, device="cuda"), torch.zeros(cap, 3, dtype=torch.int32, device="cuda")
+            r = P.prompt_rows(cap, t.dstart)
+            plan = torch.zeros(P.prompt_plan_size(t.shape, r), dtype=torch.uint8, device="cuda")
+            calls = [t.calls[0], P.prepare_prompt_plan(t.shape, r, t.dlen, False, 0, plan),
+                     P.prepare_prompt_attn(t.shape, P.inputs(t.q, t.dk, t.dv, t.dtab, None, t.scale), r, plan, t.out, t.lse, ws),
+                     P.prepare_token_logprobs(desc, cap, t.lp, None, None, *top, lws)]
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                for c in calls:
+                    c()
+            steps.append((graph, calls, top, {n: getattr(t, n) for n in ("start", "cap", "x", "tok", "q", "out", "lse", "z", "lp")}))
+    for _ in range(3):
+        for graph, _, top, own in steps:
+            t.__dict__.update(own)
+            x, tokens = t.fill(), t.g.integers(0, t.V, size=t.cap)
+            t.tok.copy_(torch.from_numpy(tokens.astype(np.int32)))
+            z = t.g.standard_normal((t.cap, t.V)).astype(np.float32)
+            t.z.copy_(torch.from_numpy(z))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            t.check(x, False, tokens)
+            np.testing.assert_array_equal(top[1].cpu().numpy(), OP.token_logprobs(z.astype(np.float64), tokens, 3)[4])
