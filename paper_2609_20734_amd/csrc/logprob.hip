@@ -125,6 +125,11 @@ struct Best {
   float z;
   int id;
 };
+// Larger the earlier a (logit, token) comes, above 0.  (-0 as 0.)
+__device__ __forceinline__ uint64_t key_of(float z, int id) {
+  const uint32_t u = __float_as_uint(z + 0.f);
+  return (uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32 | (uint32_t)~id;
+}
 // A number that at least k lanes' values reach (-infinity where fewer are above it), near
 // the k-th of them: the upper half of its bits, in the order of floats, found bit by bit.
 __device__ __forceinline__ float kth_bound(float x, int k) {
@@ -154,14 +159,14 @@ __device__ __forceinline__ void insert(Best& best, float z, int id) {
 __device__ __forceinline__ Best in_order(float z, int id, int n) {
   const int lane = threadIdx.x & 63;
   z = lane < n ? z : -INFINITY;
-  id = lane < n ? id : INT_MAX;
+  const uint64_t key = lane < n ? key_of(z, id) : 0;
   int ahead = 0;
   for (int j0 = 0; j0 < n; j0 += 4) {                 // (past the last candidate none is ahead of one)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float zj = lane_value(z, j0 + j);
-      const int ij = __builtin_amdgcn_readlane(id, j0 + j);
-      ahead += (zj > z) | ((zj == z) & (ij < id)) ? 1 : 0;
+      const uint64_t kj = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(key >> 32), j0 + j) << 32 |
+                          (uint32_t)__builtin_amdgcn_readlane((uint32_t)key, j0 + j);
+      ahead += kj > key ? 1 : 0;
     }
   }
   const int to = 4 * (lane < n ? ahead : lane);
@@ -188,7 +193,7 @@ struct Scratch {
   int id[kMaxSplits * kMaxTop];
   float pz[kWaves][64];                        // candidates
   int pi[kWaves][64];
-  uint2 cand[kMaxSplits * kMaxTop];            // (logit, token) of a join's candidates
+  uint64_t cand[kMaxSplits * kMaxTop];         // keys of a join's candidates
   float best_z[kMaxTop];                       // the joined list
   int best_id[kMaxTop];
   int n, last;
@@ -229,24 +234,21 @@ __device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k) {
     int at = 0;
     if (lane == 0) at = atomicAdd(&sm.n, __builtin_popcountll(mask));
     at = uniform(at) + lanes_before(mask);
-    if (in) sm.cand[at] = make_uint2(__float_as_uint(y), (uint32_t)sm.id[i]);
+    if (in) sm.cand[at] = key_of(y, sm.id[i]);
   }
   __syncthreads();
   const int n = sm.n;
   for (int i0 = 0; i0 < n; i0 += kThreads / 2) {              // two lanes a candidate
     const int i = i0 + (tid >> 1);
-    const uint2 own = sm.cand[min(i, n - 1)];
-    const float y = __uint_as_float(own.x);
+    const uint64_t own = sm.cand[min(i, n - 1)];
     int ahead = 0;
 #pragma unroll 8
-    for (int j = tid & 1; j < n; j += 2) {
-      const uint2 x = sm.cand[j];
-      ahead += (__uint_as_float(x.x) > y) | ((__uint_as_float(x.x) == y) & (x.y < own.y)) ? 1 : 0;
-    }
+    for (int j = tid & 1; j < n; j += 2) ahead += sm.cand[j] > own ? 1 : 0;
     ahead += __builtin_amdgcn_update_dpp(0, ahead, 0xb1, 0xf, 0xf, false);      // the other lane's
     if ((tid & 1) == 0 && i < n && ahead < k) {
-      sm.best_z[ahead] = y;
-      sm.best_id[ahead] = (int)own.y;
+      const uint32_t u = (uint32_t)(own >> 32);
+      sm.best_z[ahead] = __uint_as_float(u ^ (~(uint32_t)((int32_t)u >> 31) | 0x80000000u));
+      sm.best_id[ahead] = (int)~(uint32_t)own;
     }
   }
   __syncthreads();
