@@ -197,15 +197,11 @@ struct Scratch {
   float best_z[kMaxTop];                       // the joined list
   int best_id[kMaxTop];
   int n, last;
+  Stat all;                                    // of the workgroup or the row
+  double log_s;
+  int all_ahead;
 };
 
-// Sum over the lanes 0 .. 7 of a wavefront, in each of them.
-__device__ __forceinline__ int sum8(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false);     // lane ^ 1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, false);     // lane ^ 2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false);    // 7 - lane of the eight
-  return x;
-}
 // Before a join (and a barrier): the joined list empty, no candidates.
 __device__ __forceinline__ void clear_join(Scratch& sm) {
   if (threadIdx.x < kMaxTop) {
@@ -218,8 +214,15 @@ __device__ __forceinline__ void clear_join(Scratch& sm) {
 // by the whole workgroup.  Where the c-th places of ceil(k / c) lists reach a bound, k
 // logits do: those that reach it are placed by counting the ones ahead.  (With c about
 // 2 k / lists half of the lists decide; where fewer have that many places, a larger one.)
-__device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k) {
+// The last wavefront, which seldom has a candidate, does `beside` meanwhile.
+template <typename F>
+__device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k, F beside) {
   const int tid = threadIdx.x, lane = tid & 63;
+  if (k == 0) {
+    if (uniform(tid >> 6) == kWaves - 1) beside();
+    __syncthreads();
+    return;
+  }
   float bound = -INFINITY;
   for (int c = min(k, (2 * k + lists - 1) / lists);; c = min(k, 2 * c)) {
     bound = kth_bound(lane < lists ? sm.z[lane * k + c - 1] : -INFINITY, (k + c - 1) / c);
@@ -238,8 +241,9 @@ __device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k) {
   }
   __syncthreads();
   const int n = sm.n;
-  for (int i0 = 0; i0 < n; i0 += kThreads / 2) {              // two lanes a candidate
-    const int i = i0 + (tid >> 1);
+  if (uniform(tid >> 6) == kWaves - 1) beside();
+  for (int i0 = uniform(tid >> 6) * 32; i0 < n; i0 += kThreads / 2) {              // two lanes a candidate
+    const int i = i0 + (lane >> 1);
     const uint64_t own = sm.cand[min(i, n - 1)];
     int ahead = 0;
 #pragma unroll 8
@@ -254,19 +258,20 @@ __device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k) {
   __syncthreads();
 }
 
-// Outputs of a row: lane i < k of the wavefront holds place i.
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat x, int ahead, float zt, bool known, Best best) {
+// Outputs of a row, by one wavefront.
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, const Scratch& sm, float zt, bool known) {
   const int lane = threadIdx.x & 63;
-  const double log_s = log((double)x.s);
+  const Stat x = sm.all;
+  const double log_s = sm.log_s;
   if (lane < a.top) {
-    const bool there = best.z > -INFINITY;
-    a.top_logprobs[(int64_t)row * a.top + lane] = there ? log_prob(best.z, x.m, log_s) : -INFINITY;
-    a.top_tokens[(int64_t)row * a.top + lane] = there ? best.id : -1;
+    const float z = sm.best_z[lane];
+    a.top_logprobs[(int64_t)row * a.top + lane] = z > -INFINITY ? log_prob(z, x.m, log_s) : -INFINITY;
+    a.top_tokens[(int64_t)row * a.top + lane] = sm.best_id[lane];
   }
   if (lane != 0) return;
   if (a.entropy) a.entropy[row] = x.m == -INFINITY ? __builtin_nanf("") : (float)(log_s + (double)x.t / (double)x.s);
   if (a.logprob) a.logprob[row] = known ? log_prob(zt, x.m, log_s) : __builtin_nanf("");
-  if (a.rank) a.rank[row] = known ? ahead + 1 : 0;
+  if (a.rank) a.rank[row] = known ? sm.all_ahead + 1 : 0;
 }
 
 // (Every workgroup runs most of the code once, so its size counts: one path for
@@ -414,18 +419,29 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
   __syncthreads();
 
   // The workgroup's wavefronts joined, then, by the last of a row's workgroups, its splits.
-  if (a.top > 0) join_lists(sm, kWaves, a.top);
-  x = lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f};
-  ahead = lane < kWaves ? sm.ahead[lane] : 0;
+  // Lane l's part of the statistics, joined; of all of the row with the sum's logarithm.
+  auto join_stats = [&](Stat part, int part_ahead, bool whole) {
+    part = wave_join(part);
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) part_ahead += __shfl_xor(part_ahead, s);
+    if (lane == 0) {
+      sm.all = part;
+      sm.all_ahead = part_ahead;
+      if (whole) sm.log_s = log((double)part.s);
+    }
+  };
+  auto join_waves = [&] {
+    join_stats(lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f},
+               lane < kWaves ? sm.ahead[lane] : 0, a.splits == 1);
+  };
+  join_lists(sm, kWaves, a.top, join_waves);
   if (a.splits > 1) {
     const int words = 2 + a.top;
     const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
     if (wave == 0) {
-      x = wave_join(x);
-      ahead = sum8(ahead);
       uint64_t* part = a.parts + ((int64_t)slot * a.splits + split) * words;
-      if (lane == 0) publish(part, pack(x.m, __float_as_uint(x.s)));
-      if (lane == 1) publish(part + 1, pack(x.t, (uint32_t)ahead));
+      if (lane == 0) publish(part, pack(sm.all.m, __float_as_uint(sm.all.s)));
+      if (lane == 1) publish(part + 1, pack(sm.all.t, (uint32_t)sm.all_ahead));
       if (lane < a.top) publish(part + 2 + lane, pack(sm.best_z[lane], (uint32_t)sm.best_id[lane]));
       __builtin_amdgcn_s_waitcnt(0);
       __builtin_amdgcn_wave_barrier();
@@ -439,35 +455,31 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     if (sm.last == 0) return;
     const uint64_t* list = parts + (int64_t)min(lane, a.splits - 1) * words;
     const uint64_t p0 = published(list), p1 = published(list + 1);
+    constexpr int kEach = kMaxSplits * kMaxTop / kThreads;
+    const int all = a.splits * a.top;
+    uint64_t p[kEach];
     if (a.top > 0) {
-      constexpr int kEach = kMaxSplits * kMaxTop / kThreads;
-      const int all = a.splits * a.top;
-      uint64_t p[kEach];
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
         const int i = min(j * kThreads + tid, all - 1), l = (int)((uint32_t)i * a.top_inv >> 16);
         p[j] = published(parts + (int64_t)l * words + 2 + (i - l * a.top));
       }
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int i = j * kThreads + tid;
-        if (i >= all) continue;
-        sm.z[i] = first_of(p[j]);
-        sm.id[i] = (int)(uint32_t)p[j];
-      }
-      clear_join(sm);
-      __syncthreads();
-      join_lists(sm, a.splits, a.top);
     }
-    x = lane < a.splits ? Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)} : Stat{-INFINITY, 0.f, 0.f};
-    ahead = lane < a.splits ? (int)(uint32_t)p1 : 0;
-  }
-  if (wave != 0) return;
-  x = wave_join(x);
 #pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) ahead += __shfl_xor(ahead, s);
-  best = lane < a.top ? Best{sm.best_z[lane], sm.best_id[lane]} : Best{-INFINITY, -1};
-  write_row(a, row, x, uniform(ahead), zt, known, best);
+    for (int j = 0; j < kEach; ++j) {
+      const int i = j * kThreads + tid;
+      if (i >= all) continue;
+      sm.z[i] = first_of(p[j]);
+      sm.id[i] = (int)(uint32_t)p[j];
+    }
+    clear_join(sm);
+    __syncthreads();
+    join_lists(sm, a.splits, a.top, [&] {
+      join_stats(lane < a.splits ? Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)} : Stat{-INFINITY, 0.f, 0.f},
+                 lane < a.splits ? (int)(uint32_t)p1 : 0, true);
+    });
+  }
+  if (wave == 0) write_row(a, row, sm, zt, known);
 }
 
 // Workgroups of a row: at most kGroups in all, each of at least kLeastSplit logits.
