@@ -10,9 +10,9 @@
 //
 // Many rows are bound by HBM and, close behind, the vector operations (four bytes and
 // about a dozen instructions a logit): 1,024 rows of 50,257 with five alternatives in
-// 49.5 us, 4.2 TB/s.  Few rows are bound by one chain: four of 151,936 with twenty take
-// 14.4 us, of which a wavefront's logits and first places take 5, the joins 4, the trips
-// between workgroups 3, start and end 2 (without alternatives 6.8).
+// 48.8 us, 4.2 TB/s.  Few rows are bound by one chain: four of 151,936 with twenty take
+// 12.4 us, of which a wavefront's logits and first places take 5, the joins 3, the trips
+// between workgroups 2.5, start and end 2 (without alternatives 6.6).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -33,8 +33,9 @@ constexpr int kBatch = 64 * 4 * kLoads;       // logits of a wavefront's batch
 constexpr int kMaxTop = ODA_MAX_TOP;
 constexpr int kMaxSplits = 64;                // of a row: one per lane where they are joined
 constexpr int kTickets = 1024;                // rows that may be split
+constexpr int kTicketStride = 32;             // words: a cache line each (side by side: sixteen rows of 151,936 12.2 us against 8.6)
 constexpr int kGroups = 1024;                 // workgroups that split rows make at most
-constexpr int kLeastSplit = kWaves * kBatch / 2;  // (half and twice of it: 15.9 and 15.6 us against 14.4, below)
+constexpr int kLeastSplit = kWaves * kBatch / 2;  // (half and twice of it: 10% slower for four rows of 151,936)
 constexpr int kRun = 64;                      // runs of wavefronts are multiples of it
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = 1e30f;                 // stands for an infinite distance (its weight is 0)
@@ -51,7 +52,7 @@ struct LogprobArgs {
   int32_t* top_tokens;
   const int32_t* work_list;
   const int32_t* n_work;
-  uint32_t* tickets;       // [kTickets], zero between calls
+  uint32_t* tickets;       // [kTickets][kTicketStride], zero between calls
   uint64_t* parts;         // [slot][splits][2 + top]: (m, S), (T, ahead), then (logit, token)
   int64_t stride;
   int32_t R, V, top, splits, chunk;
@@ -218,11 +219,6 @@ __device__ __forceinline__ void clear_join(Scratch& sm) {
 template <typename F>
 __device__ __forceinline__ void join_lists(Scratch& sm, int lists, int k, F beside) {
   const int tid = threadIdx.x, lane = tid & 63;
-  if (k == 0) {
-    if (uniform(tid >> 6) == kWaves - 1) beside();
-    __syncthreads();
-    return;
-  }
   float bound = -INFINITY;
   for (int c = min(k, (2 * k + lists - 1) / lists);; c = min(k, 2 * c)) {
     bound = kth_bound(lane < lists ? sm.z[lane * k + c - 1] : -INFINITY, (k + c - 1) / c);
@@ -434,7 +430,23 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     join_stats(lane < kWaves ? Stat{sm.m[lane], sm.s[lane], sm.t[lane]} : Stat{-INFINITY, 0.f, 0.f},
                lane < kWaves ? sm.ahead[lane] : 0, a.splits == 1);
   };
-  join_lists(sm, kWaves, a.top, join_waves);
+  // (Without alternatives the first wavefront is alone from here on: four rows 7.6 us
+  // against 7.8 where all stay.)
+  const bool alone = a.top == 0;
+  if (alone && wave != 0) return;
+  auto sync = [&] {
+    if (alone) oda::wave_lds_fence();
+    else __syncthreads();
+  };
+  auto join = [&](int lists, auto beside) {
+    if (!alone) {
+      join_lists(sm, lists, a.top, beside);
+    } else {
+      beside();
+      oda::wave_lds_fence();
+    }
+  };
+  join(kWaves, join_waves);
   if (a.splits > 1) {
     const int words = 2 + a.top;
     const uint64_t* parts = a.parts + (int64_t)slot * a.splits * words;
@@ -446,12 +458,12 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
       __builtin_amdgcn_s_waitcnt(0);
       __builtin_amdgcn_wave_barrier();
       if (lane == 0)
-        sm.last = __builtin_amdgcn_atomic_inc32(a.tickets + slot, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
+        sm.last = __builtin_amdgcn_atomic_inc32(a.tickets + slot * kTicketStride, (uint32_t)(a.splits - 1), __ATOMIC_RELAXED, "agent") ==
                           (uint32_t)(a.splits - 1)
                       ? 1
                       : 0;
     }
-    __syncthreads();
+    sync();
     if (sm.last == 0) return;
     const uint64_t* list = parts + (int64_t)min(lane, a.splits - 1) * words;
     const uint64_t p0 = published(list), p1 = published(list + 1);
@@ -473,8 +485,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
       sm.id[i] = (int)(uint32_t)p[j];
     }
     clear_join(sm);
-    __syncthreads();
-    join_lists(sm, a.splits, a.top, [&] {
+    sync();
+    join(a.splits, [&] {
       join_stats(lane < a.splits ? Stat{first_of(p0), __uint_as_float((uint32_t)p0), first_of(p1)} : Stat{-INFINITY, 0.f, 0.f},
                  lane < a.splits ? (int)(uint32_t)p1 : 0, true);
     });
@@ -500,7 +512,7 @@ oda_status check(const oda_logprob_desc* desc, int32_t rows, size_t* bytes, int*
     return oda::fail(ODA_ERR_SHAPE, "row_stride must be 0 or at least vocab");
   split_row(rows, desc->vocab, splits, chunk);
   // (rows that are split have kGroups parts at most, whatever the call's sizes)
-  *bytes = kTickets * 4 + (size_t)kGroups * (2 + ODA_MAX_TOP) * 8;
+  *bytes = kTickets * kTicketStride * 4 + (size_t)kGroups * (2 + ODA_MAX_TOP) * 8;
   return ODA_OK;
 }
 
@@ -544,7 +556,7 @@ extern "C" oda_status oda_token_logprobs(const oda_logprob_desc* desc, int32_t r
   a.work_list = work_list;
   a.n_work = n_work;
   a.tickets = static_cast<uint32_t*>(workspace);
-  a.parts = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + kTickets * 4);
+  a.parts = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + kTickets * kTicketStride * 4);
   a.stride = desc->row_stride != 0 ? desc->row_stride : desc->vocab;
   a.R = rows;
   a.V = desc->vocab;
