@@ -684,13 +684,15 @@ static_assert(2 * kStageBlocks == kWaves, "a wavefront brings one block of K or 
 // A block from memory straight to LDS: 1 KiB per load, lane i's 16 bytes to place i.
 // (In assembly, as the compiler would wait for all of them before any read of LDS.  No
 // registers are written; the address is read when the load is issued; the caller waits
-// with wait_loads and a barrier before the block is read.)
+// with wait_loads and a barrier before the block is read.  A load to LDS needs a wait
+// state behind a scalar write of M0, which nobody puts into an asm block but its author.)
 constexpr int kLoadBytes = 64 * 16;
 template <int D>
 __device__ __forceinline__ void load_to_lds(const uint16_t* src, uint32_t dst) {
   if constexpr (D == 128)
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
         "global_load_lds_dwordx4 %0, off\n\t"
         "global_load_lds_dwordx4 %0, off offset:%2\n\t"
         "global_load_lds_dwordx4 %0, off offset:2*%2\n\t"
@@ -701,6 +703,7 @@ __device__ __forceinline__ void load_to_lds(const uint16_t* src, uint32_t dst) {
   else
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
         "global_load_lds_dwordx4 %0, off\n\t"
         "global_load_lds_dwordx4 %0, off offset:%2"
         :
