@@ -657,8 +657,8 @@ typedef struct {
  *   k_ring, v_ring, n_sink, window: as in oda_commit_kv_ring, or NULL, 0, 0
  * A request whose length is outside [0, max_seq_len] or shorter than its rows gets
  * NaN queries and appends nothing; a table entry outside [0, num_blocks) drops the
- * K/V of its places.  Places are written once: requests must not share the blocks
- * that they append to. */
+ * K/V of its places, from the rings too.  Places are written once: requests must not
+ * share the blocks that they append to. */
 oda_status oda_append_qkv(const oda_attn_shape *shape, const oda_prompt_rows *rows, const oda_append_desc *desc,
                           uint16_t *k_cache, uint16_t *v_cache, const int32_t *block_table, const int32_t *seq_lens,
                           uint16_t *q_out, uint16_t *k_ring, uint16_t *v_ring, int32_t n_sink, int32_t window,

@@ -201,13 +201,13 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     for (int u = 0; u < kInFlight; ++u) load(u);
   }
 
-  // block and ring block of the rows
+  // block and ring block of the rows (places without a block are in the ring neither)
   int64_t blk = -1, ring = -1;
   if (a.Hkv > 0 && !t.bad && s1 > q_slots) {
     const int e = a.block_table[(int64_t)t.request * a.MB + t.block];
     blk = e >= 0 && e < a.num_blocks ? e : -1;
     const int end = (t.place0 + t.rows - 1) / kBlock;
-    if (a.k_ring != nullptr && (t.block < a.sink_blocks || t.block > end - a.ring_blocks))
+    if (blk >= 0 && a.k_ring != nullptr && (t.block < a.sink_blocks || t.block > end - a.ring_blocks))
       ring = (int64_t)t.request * (a.sink_blocks + a.ring_blocks) +
              (t.block < a.sink_blocks ? t.block : a.sink_blocks + t.block % a.ring_blocks);
   }
