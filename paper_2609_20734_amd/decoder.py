@@ -395,17 +395,24 @@ class PromptDecoder:
         self.ws_score = zeros(P.logprob_workspace_size(self.scored, rows))
 
     def set_chunk(self, tokens, row_start, targets=None) -> None:
-        """The next chunk: tokens [n <= rows], row_start [B + 1], targets [n] (the tokens to score, -1: none)."""
+        """The next chunk: tokens [n <= rows], row_start [B + 1], targets [n] (the tokens to score, -1: none).  Starts are
+        taken into [0, n] and as ascending, as the kernels take them: lengths grow by the rows that are appended; tokens
+        in front of the first or behind the last request's rows are no request's, and their scores mean nothing.  A
+        request that outgrows max_seq_len has NaN scores from then on."""
         import torch
         n = tokens.numel()
         if n > self.rows:
             raise ValueError(f"{n} rows in a chunk, room for {self.rows}")
+        if row_start.numel() != self.B + 1:
+            raise ValueError(f"{self.B} requests need {self.B + 1} row starts (got {row_start.numel()})")
+        if targets is not None and targets.numel() != n:
+            raise ValueError(f"{targets.numel()} targets for {n} tokens")
         self.tokens.zero_()                             # rows of no request keep a token of the vocabulary
         self.tokens[:n].copy_(tokens)
         self.targets.fill_(-1)
         if targets is not None:
             self.targets[:n].copy_(targets)
-        self.row_start.copy_(row_start)
+        self.row_start.copy_(row_start.clamp(0, n).cummax(0).values)
         count = self.row_start[1:] - self.row_start[:-1]
         self.seq_lens.add_(count)
         if self.listed is not None:
