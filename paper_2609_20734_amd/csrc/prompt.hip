@@ -285,7 +285,9 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
   const float top = fmaxf(class_cost(most), kLeastCost);
   const float cap = lane == 63 ? top : kLeastCost * __builtin_amdgcn_exp2f(__log2f(top / kLeastCost) * (float)lane * (1.f / 63.f));
   const float inv = 1.f / cap;
-  int n = 0;
+  // (items beyond the tiles are counted up to more than may be: what is above is refused below)
+  const int limit = a.extra_items + 1;
+  int more = 0;
   float sum = 0.f, big = 0.f;
   // (classes that are there lie side by side: the wavefronts take them in turn)
   for (int c0 = 0; c0 < 2 * kClasses; c0 += 64) {
@@ -297,29 +299,30 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
       const int count = __builtin_amdgcn_readlane(here, i);
       const float cost = class_cost((c0 + i) & (kClasses - 1));
       const int splits = lane == 63 ? 1 : max(1, (int)ceilf(cost * inv));
-      n += count * splits;
+      more += min(count, limit) * min(splits - 1, limit);
       big = fmaxf(big, cost * __builtin_amdgcn_rcpf((float)splits));
       sum += (float)count * (cost + (float)splits * (kItemCost + (splits > 1 ? part : 0.f)));
     }
   }
-  s_count[wave][lane] = n;
+  s_count[wave][lane] = more;
   s_cost[wave][lane] = sum;
   s_big[wave][lane] = big;
   __syncthreads();
-  n = 0;
+  more = 0;
   sum = 0.f;
 #pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
-    n += s_count[w][lane];
+    more += s_count[w][lane];
     sum += s_cost[w][lane];
     big = fmaxf(big, s_big[w][lane]);
   }
   // rounds of items of mean cost, the last one whole where they are alike; at least the largest item
+  const int n = n_tiles + more;
   const float rounds = (float)a.Hkv * (float)n * (1.f / (float)kCus);
   const float mean = sum / (float)max(n, 1);
   const float alike = fminf(1.f, mean / (big + kItemCost));
   float est = fmaxf(big + kItemCost, mean * (rounds + alike * (ceilf(rounds) - rounds)));
-  if (n - n_tiles > a.extra_items) est = INFINITY;
+  if (more > a.extra_items) est = INFINITY;
   float best = est;
 #pragma unroll
   for (int s = 32; s >= 1; s >>= 1) best = fminf(best, __shfl_xor(best, s));
