@@ -692,12 +692,13 @@ oda_status oda_prompt_plan(const oda_attn_shape *shape, const oda_prompt_rows *r
  *        fp32 output hold all of their 24 bits, as in decode attention; those of a bf16
  *        output are rounded to bf16, which takes half the matrix operations
  *   lse  fp32 [num_rows][Hq] (natural log), or NULL
- * A request whose length is outside [0, max_seq_len] or (causal) shorter than its
- * rows gets NaN rows, and so does a row that attends a block whose table entry is
- * outside [0, num_blocks); other rows do not see it.  Slots that no row attends may
- * hold anything; a value that is not finite reaches the rows that attend it alone.
- * A plan made for another batch, num_rows, head counts, table width or max_seq_len
- * gives NaN throughout.  workspace: >= oda_prompt_workspace_size bytes, 256-byte
+ * A request whose length is outside [0, max_seq_len] (or above 2^31 - 65) or
+ * (causal) shorter than its rows gets NaN rows, and so does a row that attends a
+ * block whose table entry is outside [0, num_blocks); other rows do not see it.
+ * Slots that no row attends may hold anything; a value that is not finite reaches
+ * the rows that attend it alone.  A plan made for another batch, num_rows, head
+ * counts, table width or max_seq_len gives NaN throughout.
+ * workspace: >= oda_prompt_workspace_size bytes, 256-byte
  * aligned; calls that may overlap in time need separate ones (a plan may be shared). */
 oda_status oda_prompt_attn(const oda_attn_shape *shape, const oda_attn_inputs *in, const oda_prompt_rows *rows,
                            const void *plan, size_t plan_bytes, void *out, int32_t out_type, float *lse,

@@ -53,6 +53,7 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kTile = kWaves * kCols; // columns of an item
 constexpr int kStageBlocks = 4;       // blocks staged together: one of K or V per wavefront
 constexpr int kMaxBatch = 2048;
+constexpr int kLongest = INT_MAX - 64;   // positions up to a stage behind the last are counted in 32 bits
 constexpr int kCus = 256;
 constexpr int kPlanThreads = 256;
 constexpr uint32_t kMagic = 0x0da9f3u;
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PlanArgs a) {
     int2 total;
     const int2 at = block_scan(make_int2(tiles, narrow), s_wave, total);
     if (b < a.B) {
-      const bool bad = n < 0 || n > a.max_len || (a.causal && n < rows);
+      const bool bad = n < 0 || n > min(a.max_len, kLongest) || (a.causal && n < rows);
       s_req[b] = PlanRequest{row0, rows, bad ? -1 : n, n_tiles + at.x, n_narrow + at.y};
       if (!bad) {
         const int reach = a.causal && a.window > 0 && a.window < n - rows ? a.window + rows : n;

@@ -81,3 +81,15 @@ def test_mixes(seed):
     causal = bool(g.integers(0, 3))
     window = int(np.exp(g.uniform(0, 9))) if causal and g.integers(0, 2) else 0
     check(rows, [(r if causal else 0) + h for r, h in zip(rows, hist)], Hkv * int(g.choice([1, 4, 5])), Hkv, 64, causal, window)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,good", [(2 ** 31 - 1, False), (2 ** 31 - 16, False), (2 ** 31 - 64, False), (2 ** 31 - 65, True)])
+def test_lengths_next_to_32_bits(n, good, causal):
+    """Positions behind the last that a stage reaches are counted too: the longest lengths are out of range."""
+    items, _ = planned([3], [n], 2, 1, 64, causal, max_len=2 ** 31 - 1)
+    if good:
+        lo, hi = items[:, 4], items[:, 5]
+        assert (items[:, 7] == n).all() and lo.min() == 0 and hi.max() == -(-n // 16) and (hi > lo).all()
+    else:
+        assert items[:, 7].tolist() == [-1] and items[0, 3] == 6
