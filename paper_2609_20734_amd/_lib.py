@@ -523,13 +523,19 @@ def commit_drafts(shape: Shape, tokens: int, k_cache, v_cache, block_table, seq_
                           row_lens, workspace, k_ring, v_ring, n_sink, window, workspace_bytes, stream)()
 
 
-def _type(t, name: str) -> int:
-    """oda_type of a tensor (None and a plain address count as fp32)."""
-    if t is None or isinstance(t, int) or t.dtype == torch.float32:
-        return F32
-    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
-        return BF16
-    raise ValueError(f"{name} must be fp32 or bf16 (got {t.dtype})")
+def _type(t, name: str, given: int | None = None) -> int:
+    """oda_type of a tensor; of a plain address (or None) the one that is given, or fp32."""
+    if t is None or isinstance(t, int):
+        return F32 if given is None else given
+    if t.dtype == torch.float32:
+        own = F32
+    elif t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        own = BF16
+    else:
+        raise ValueError(f"{name} must be fp32 or bf16 (got {t.dtype})")
+    if given not in (None, own):
+        raise ValueError(f"{name} is {t.dtype}, not of the type given")
+    return own
 
 
 def prompt_rows(num_rows: int, row_start) -> PromptRows:
@@ -539,13 +545,14 @@ def prompt_rows(num_rows: int, row_start) -> PromptRows:
     return s
 
 
-def append_desc(qkv, q_gain, k_gain, rms_eps: float, rope_theta: float, positions=None, axis_pairs=None) -> AppendDesc:
-    """The C description of rows to append (qkv fp32 or bf16); it keeps the tensors alive.  axis_pairs: pairs of each
-    axis of `positions` [rows][axes], or None for one axis."""
+def append_desc(qkv, q_gain, k_gain, rms_eps: float, rope_theta: float, positions=None, axis_pairs=None,
+                qkv_type: int | None = None) -> AppendDesc:
+    """The C description of rows to append (qkv fp32 or bf16; qkv_type says which where it is a plain address); it keeps
+    the tensors alive.  axis_pairs: pairs of each axis of `positions` [rows][axes], or None for one axis."""
     axes = [] if axis_pairs is None else list(axis_pairs)
     if len(axes) > MAX_AXES:
         raise ValueError(f"positions have up to {MAX_AXES} axes (got {len(axes)})")
-    s = AppendDesc(_ptr(qkv), _type(qkv, "qkv"), float(rms_eps), _ptr(q_gain), _ptr(k_gain), float(rope_theta), _ptr(positions),
+    s = AppendDesc(_ptr(qkv), _type(qkv, "qkv", qkv_type), float(rms_eps), _ptr(q_gain), _ptr(k_gain), float(rope_theta), _ptr(positions),
                    max(1, len(axes)), (ctypes.c_int32 * MAX_AXES)(*axes))
     s._keep = (qkv, q_gain, k_gain, positions)
     return s
@@ -575,8 +582,8 @@ def prompt_plan(shape: Shape, rows: PromptRows, seq_lens, causal: bool, native_w
 
 
 def prompt_attn(shape: Shape, inp: AttnInputs, rows: PromptRows, plan, out, lse, workspace, plan_bytes: int | None = None,
-                workspace_bytes: int | None = None, stream=None) -> None:
-    prepare_prompt_attn(shape, inp, rows, plan, out, lse, workspace, plan_bytes, workspace_bytes, stream)()
+                workspace_bytes: int | None = None, stream=None, out_type: int | None = None) -> None:
+    prepare_prompt_attn(shape, inp, rows, plan, out, lse, workspace, plan_bytes, workspace_bytes, stream, out_type)()
 
 
 def logprob_desc(vocab: int, top: int, logits, tokens=None, row_stride: int = 0) -> LogprobDesc:
@@ -791,10 +798,11 @@ def prepare_prompt_plan(shape: Shape, rows: PromptRows, seq_lens, causal: bool, 
 
 
 def prepare_prompt_attn(shape: Shape, inp: AttnInputs, rows: PromptRows, plan, out, lse, workspace,
-                        plan_bytes: int | None = None, workspace_bytes: int | None = None, stream=None) -> Call:
+                        plan_bytes: int | None = None, workspace_bytes: int | None = None, stream=None,
+                        out_type: int | None = None) -> Call:
     cs = shape.c()
     args = (ctypes.byref(cs), ctypes.byref(inp), ctypes.byref(rows), _ptr(plan), _nbytes(plan, plan_bytes), _ptr(out),
-            _type(out, "out"), _ptr(lse), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
+            _type(out, "out", out_type), _ptr(lse), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream))
     return Call(_lib.oda_prompt_attn, args, (cs, inp, rows, plan, out, lse, workspace))
 
 
