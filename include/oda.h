@@ -632,7 +632,9 @@ typedef struct {
  *   positions  int32 [num_rows][num_axes]: p of a pair is its axis's position; NULL
  *              (one axis): the row's place in the history
  *   axis_pairs pairs of each axis (time, height, width ...): the first axis_pairs[0]
- *              pairs take the first, and so on; their sum is D/2.  Ignored for one axis */
+ *              pairs take the first, and so on; their sum is D/2.  Ignored for one axis
+ * All of D turns, by these frequencies as they are: axes that alternate from pair to
+ * pair, rotations of a part of D and rescaled frequencies are the caller's (theta 0). */
 #define ODA_MAX_AXES 4
 typedef struct {
   const void *qkv;

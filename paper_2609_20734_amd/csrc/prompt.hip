@@ -19,11 +19,13 @@
 // lengths by one workgroup, once for all layers of a step.
 //
 // Bound by the matrix cores and the vector operations beside them: 8,192 tokens of 32
-// heads over 8 KV heads in 516 us, 1.07 PFLOP/s (a large library product of this card:
-// 1.26), 512 behind 65,001 in 490 (1.13).  A pair of blocks takes a wavefront 32 products
-// and, of its 16 scores a lane, 16 exponentials and about 100 other vector operations; two
-// wavefronts a SIMD take turns.  Single rows against states are bound by HBM: 32 requests,
-// 123 MB, in 23 us (5.3 TB/s) behind the plan.
+// heads over 8 KV heads in 518 us with bf16 outputs, 1.06 PFLOP/s (a large library product
+// of this card: 1.26), 512 behind 65,001 in 482 (1.14).  Of 128 dimensions a pair of blocks
+// takes a wavefront 16 products (8 of scores, 8 of values) and, of its 16 scores a lane, 16
+// exponentials and about 100 other vector operations; two wavefronts a SIMD take turns.
+// With fp32 outputs, whose weights have three parts, it is 32 products: 887 and 849 us with
+// the plan, 1.24 and 1.29 PFLOP/s of the products that are made.  Single rows against states
+// are bound by HBM: 32 requests, 123 MB, in 23 us (5.3 TB/s) behind the plan.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -345,11 +345,12 @@ class PromptDecoder:
     them and then counts what the cache holds.  Decoder and DraftDecoder count the current
     token too: add 1 to the lengths before their first step.
 
-    rows: rows of the buffers (chunks may have fewer); rings: (k_ring, v_ring, n_sink,
-    window) to keep the direct rings [L][B][..] current; axis_pairs: rotary axes of
-    `positions` [rows][axes], written before each chunk (None: places of the history);
-    score: "last" or "all" rows; top: alternatives per scored row; native_window: of every
-    layer (0: the whole history)."""
+    rows: rows of the buffers (chunks may have fewer, but the dense layers go through all of
+    them, and `logits` has a row of the vocabulary for each, whatever is scored: choose them
+    for the chunks that come); rings: (k_ring, v_ring, n_sink, window) to keep the direct
+    rings [L][B][..] current; axis_pairs: rotary axes of `positions` [rows][axes], written
+    before each chunk (None: places of the history); score: "last" or "all" rows; top:
+    alternatives per scored row; native_window: of every layer (0: the whole history)."""
 
     def __init__(self, shape: DecoderShape, weights: dict, batch: int, rows: int, k_cache, v_cache, block_table, seq_lens,
                  max_blocks_per_seq: int, max_seq_len: int, num_blocks: int, rings=None, axis_pairs=None, score: str = "last",
